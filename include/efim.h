@@ -257,6 +257,77 @@ int efim_decode_step_fp8_table(const efim_batch_t* batch, const void* q, const v
                                void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Append with norms of queries and keys.  Models that norm every query and key head row in front of
+ * the rotation take this call in place of efim_rope_append_table; the cache is the same and
+ * efim_extend_attention reads it.  For every row x of a query or key head
+ *   y = x * (mean(x^2) + norm_eps)^(-1/2) * w,   rotated as by efim_rope_append_table,
+ * squares, norm and rotation in fp32 (the angle in fp64), rounded once to bf16.  Values are copied.
+ *   q         DEVICE bf16 [T, Hq, D]   raw queries (read only unless q_out is q).  NULL: keys only
+ *   q_out     DEVICE bf16 [T, Hq, D]   normed and rotated queries; may be q; NULL where q is
+ *   q_weight, k_weight  DEVICE bf16 [D]  w of the query and of the key rows; NULL: ones
+ *   norm_eps  finite, >= 0
+ *   inv_freq, rotary_dim, rope_interleaved  as efim_rope_append_table
+ * The _fp8 form appends to an 8-bit cache as efim_rope_append_fp8 does.  No host state is kept and only kernels
+ * are launched: both may be captured into a HIP graph.
+ * Errors: as efim_rope_append_table; EFIM_ERR_INVALID_ARG also for norm_eps and for q without q_out or the reverse;
+ * EFIM_ERR_UNSUPPORTED for 2^26 new tokens or more.
+ * ------------------------------------------------------------------------------------- */
+int efim_norm_rope_append(const efim_batch_t* batch, const void* q, void* q_out, const void* k_new, const void* v_new,
+                          const void* q_weight, const void* k_weight, float norm_eps, void* k_cache, void* v_cache,
+                          const double* inv_freq, int rotary_dim, int rope_interleaved, void* stream);
+int efim_norm_rope_append_fp8(const efim_batch_t* batch, const void* q, void* q_out, const void* k_new,
+                              const void* v_new, const void* q_weight, const void* k_weight, float norm_eps,
+                              void* k_cache, void* v_cache, const double* inv_freq, int rotary_dim,
+                              int rope_interleaved, float k_scale, float v_scale, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Latent cache.  Models with latent attention keep one row a token for all heads: a latent vector
+ * c of 512 elements and a rotated key part r of 64.  Head h of a token has
+ *   key [ W_uk,h c | r ]  (128 + 64 elements)   and   value W_uv,h c  (128 elements).
+ * The cache holds the rows:  latent_cache  DEVICE bf16 [num_pages, P, 576].
+ *
+ * batch: as for the other calls with num_kv_heads = 1 and head_dim = 576; num_q_heads (H) 1 .. 256,
+ * any number.  EFIM_ERR_UNSUPPORTED for other head layouts.
+ * None of these calls keeps host state and all launch only kernels: they may be captured into a HIP graph.
+ * ------------------------------------------------------------------------------------- */
+
+/*
+ * efim_latent_append -- norms the new tokens' latents, rotates the 64 rotary elements of their keys and queries at
+ * positions C_r + i and appends the rows to the cache:
+ *   row = [ c * (mean(c^2) + norm_eps)^(-1/2) * w | rot(r) ],   q_out = rot(q_rope)
+ * in fp32 (the angle in fp64), rounded once to bf16.
+ *   q_rope    DEVICE bf16  the 64 rotary elements of head h of token t at (t * H + h) * q_stride elements (a slice
+ *             of the query projection).  NULL: keys only
+ *   q_out     DEVICE bf16  where they go, at (t * H + h) * q_out_stride.  q_rope itself (with the same stride): in place
+ *   kv_new    DEVICE bf16  token t's raw latent and, behind it, rotary key part at t * kv_stride elements
+ *   strides   multiples of 8 elements, at least 64 (kv_stride: 576)
+ *   norm_weight DEVICE bf16 [512]; NULL: ones
+ *   inv_freq  HOST double[32], finite;   rope_interleaved as efim_rope_append
+ * Errors as efim_norm_rope_append.
+ */
+int efim_latent_append(const efim_batch_t* batch, const void* q_rope, int64_t q_stride, void* q_out,
+                       int64_t q_out_stride, const void* kv_new, int64_t kv_stride, const void* norm_weight,
+                       float norm_eps, void* latent_cache, const double* inv_freq, int rope_interleaved,
+                       void* stream);
+
+/*
+ * efim_latent_attention -- causal attention over the latent cache, absorbed form: queries that the caller has multiplied
+ * by W_uk,h meet the rows themselves, and the outputs are left in latent space for the caller's W_uv,h:
+ *   s_j = sm_scale * <q_i, row_j>,  p = softmax_j(s),  out_i = sum_j p_j row_j[:512],   j = 0 .. C_r + i
+ *   q         DEVICE bf16 [T, H, 576]   512 absorbed elements and the 64 rotated ones (efim_latent_append's q_out)
+ *   out       DEVICE bf16 [T, H, 512]   must not alias q or the cache
+ *   sm_scale  finite, > 0 (the scale of the unabsorbed heads, e.g. 192^-1/2)
+ *   workspace DEVICE, 256-byte aligned, at least efim_latent_workspace_bytes(batch) bytes, contents irrelevant; not to
+ *             be used by an overlapping call
+ * Scores and sums are fp32; probabilities enter the second product as bf16.  A row's result does not depend on the run, only
+ * on the batch.  Slots at or beyond C_r + N_r may hold anything.
+ * efim_latent_workspace_bytes is a pure host function: at least 256, 0 for an invalid batch.
+ */
+size_t efim_latent_workspace_bytes(const efim_batch_t* batch);
+int efim_latent_attention(const efim_batch_t* batch, const void* q, const void* latent_cache, void* out,
+                          float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Session pool: the FIM -> EFIM prompt rewrite in front of the engine (Sec. 3.1, steps 1-5
  * of the prompt transformation figure).  Host code only; no device is touched.
  *

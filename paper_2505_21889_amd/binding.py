@@ -132,6 +132,16 @@ def _load():
     lib.efim_decode_step_fp8_table.argtypes = [bp, vp, vp, vp, vp, vp, vp, f64p, i32, i32, f32, f32, f32, vp,
                                                ctypes.c_size_t, vp]
     lib.efim_decode_step_fp8_table.restype = i32
+    lib.efim_norm_rope_append.argtypes = [bp, vp, vp, vp, vp, vp, vp, f32, vp, vp, f64p, i32, i32, vp]
+    lib.efim_norm_rope_append.restype = i32
+    lib.efim_norm_rope_append_fp8.argtypes = [bp, vp, vp, vp, vp, vp, vp, f32, vp, vp, f64p, i32, i32, f32, f32, vp]
+    lib.efim_norm_rope_append_fp8.restype = i32
+    lib.efim_latent_append.argtypes = [bp, vp, i64, vp, i64, vp, i64, vp, f32, vp, f64p, i32, vp]
+    lib.efim_latent_append.restype = i32
+    lib.efim_latent_workspace_bytes.argtypes = [bp]
+    lib.efim_latent_workspace_bytes.restype = ctypes.c_size_t
+    lib.efim_latent_attention.argtypes = [bp, vp, vp, vp, f32, vp, ctypes.c_size_t, vp]
+    lib.efim_latent_attention.restype = i32
     lib.efim_extend_plan_items.argtypes = [bp, vp, i64]
     lib.efim_extend_plan_items.restype = i64
     lib.efim_plan_info.argtypes = [bp, i32, ctypes.POINTER(EfimPlanInfo)]
@@ -170,6 +180,8 @@ EXPORTED_SYMBOLS = (
     "efim_decode_workspace_bytes", "efim_decode_step", "efim_decode_step_table",
     "efim_rope_append_fp8", "efim_extend_attention_fp8", "efim_decode_step_fp8",
     "efim_rope_append_fp8_table", "efim_decode_step_fp8_table",
+    "efim_norm_rope_append", "efim_norm_rope_append_fp8",
+    "efim_latent_append", "efim_latent_workspace_bytes", "efim_latent_attention",
     "efim_extend_plan_items", "efim_plan_info", "efim_set_tuning", "efim_set_kernel_events", "efim_status_string",
     "efim_last_hip_error", "efim_version", "efim_source_digest", "efim_stream_release",
     "efim_plan_create", "efim_plan_destroy", "efim_plan_workspace_bytes", "efim_plan_upload",
@@ -387,6 +399,50 @@ def efim_decode_step_fp8_table(batch, q, k_new, v_new, k_cache, v_cache, out, in
                                            int(rope_interleaved), float(sm_scale), float(k_scale), float(v_scale),
                                            _ptr(workspace), int(workspace_bytes), _stream_ptr(stream)),
            "efim_decode_step_fp8_table")
+
+
+def efim_norm_rope_append(batch, q, q_out, k_new, v_new, q_weight, k_weight, norm_eps, k_cache, v_cache, inv_freq,
+                          rotary_dim, rope_interleaved=0, stream=None):
+    table = _freq_table(inv_freq, rotary_dim)
+    _check(_lib.efim_norm_rope_append(ctypes.byref(batch.c), _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new),
+                                      _ptr(q_weight), _ptr(k_weight), float(norm_eps), _ptr(k_cache), _ptr(v_cache),
+                                      table.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), int(rotary_dim),
+                                      int(rope_interleaved), _stream_ptr(stream)),
+           "efim_norm_rope_append")
+
+
+def efim_norm_rope_append_fp8(batch, q, q_out, k_new, v_new, q_weight, k_weight, norm_eps, k_cache, v_cache, inv_freq,
+                              rotary_dim, rope_interleaved, k_scale, v_scale, stream=None):
+    table = _freq_table(inv_freq, rotary_dim)
+    _check(_lib.efim_norm_rope_append_fp8(ctypes.byref(batch.c), _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new),
+                                          _ptr(q_weight), _ptr(k_weight), float(norm_eps), _ptr(k_cache),
+                                          _ptr(v_cache), table.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                          int(rotary_dim), int(rope_interleaved), float(k_scale), float(v_scale),
+                                          _stream_ptr(stream)),
+           "efim_norm_rope_append_fp8")
+
+
+EFIM_LATENT_ROPE = 64
+
+
+def efim_latent_append(batch, q_rope, q_stride, q_out, q_out_stride, kv_new, kv_stride, norm_weight, norm_eps,
+                       latent_cache, inv_freq, rope_interleaved=0, stream=None):
+    table = _freq_table(inv_freq, EFIM_LATENT_ROPE)
+    _check(_lib.efim_latent_append(ctypes.byref(batch.c), _ptr(q_rope), int(q_stride), _ptr(q_out), int(q_out_stride),
+                                   _ptr(kv_new), int(kv_stride), _ptr(norm_weight), float(norm_eps),
+                                   _ptr(latent_cache), table.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                   int(rope_interleaved), _stream_ptr(stream)),
+           "efim_latent_append")
+
+
+def efim_latent_workspace_bytes(batch):
+    return int(_lib.efim_latent_workspace_bytes(ctypes.byref(batch.c)))
+
+
+def efim_latent_attention(batch, q, latent_cache, out, sm_scale, workspace, workspace_bytes, stream=None):
+    _check(_lib.efim_latent_attention(ctypes.byref(batch.c), _ptr(q), _ptr(latent_cache), _ptr(out), float(sm_scale),
+                                      _ptr(workspace), int(workspace_bytes), _stream_ptr(stream)),
+           "efim_latent_attention")
 
 
 def efim_extend_plan_items(batch):

@@ -4,13 +4,16 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libefim.so")
-SOURCES = ["api.hip", "planner.cpp", "session_pool.cpp", "rope_append.hip", "extend_attention.hip"]
+SOURCES = ["api.hip", "planner.cpp", "session_pool.cpp", "rope_append.hip", "extend_attention.hip",
+           "norm_append.hip", "latent_append.hip", "latent_plan.cpp", "latent_attention.hip"]
 # measured-ceiling kernels of the benchmark: a library of their own, never part of libefim.so
 CEILINGS_PATH = os.path.join(LIB_DIR, "libefim_ceilings.so")
 CEILINGS_SOURCES = ["ceilings.hip"]
@@ -38,25 +41,7 @@ def source_digest():
     return h.hexdigest()
 
 
-def build_library(verbose=False, extra_flags=()):
-    """Compile every source of the library for gfx950 and link libefim.so."""
-    os.makedirs(LIB_DIR, exist_ok=True)
-    cmd = [
-        hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-        "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-        "-Wno-unused-command-line-argument",
-        # leading kernel arguments arrive in scalar registers (extend_attention.hip)
-        "-mllvm", "-amdgpu-kernarg-preload-count=16",
-        "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-        '-DEFIM_SOURCE_DIGEST="%s"' % source_digest(),
-    ]
-    cmd += list(extra_flags)
-    for s in SOURCES:
-        if s.endswith(".cpp"):
-            cmd += ["-x", "hip", os.path.join(CSRC, s)]
-        else:
-            cmd += [os.path.join(CSRC, s)]
-    cmd += ["-o", LIB_PATH]
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd))
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -66,6 +51,33 @@ def build_library(verbose=False, extra_flags=()):
         raise RuntimeError("hipcc failed:\n" + err)
     if verbose and err.strip():
         print(err)
+
+
+def build_library(verbose=False, extra_flags=()):
+    """Compile every source of the library for gfx950, side by side, and link libefim.so."""
+    os.makedirs(LIB_DIR, exist_ok=True)
+    flags = [
+        "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+        "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+        "-Wno-unused-command-line-argument",
+        # leading kernel arguments arrive in scalar registers (extend_attention.hip)
+        "-mllvm", "-amdgpu-kernarg-preload-count=16",
+        "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+        '-DEFIM_SOURCE_DIGEST="%s"' % source_digest(),
+    ] + list(extra_flags)
+    with tempfile.TemporaryDirectory() as folder:
+        def compile_one(name):
+            obj = os.path.join(folder, name + ".o")
+            source = ["-x", "hip"] if name.endswith(".cpp") else []
+            _run([hipcc_path()] + flags + ["-c"] + source + [os.path.join(CSRC, name), "-o", obj], verbose)
+            return obj
+
+        # (a compiler takes up to 1 GB; the attention kernels, which take longest, start first)
+        order = sorted(SOURCES, key=lambda n: -os.path.getsize(os.path.join(CSRC, n)))
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            objects = dict(zip(order, pool.map(compile_one, order)))
+        _run([hipcc_path(), "--offload-arch=gfx950", "-fPIC", "-shared"] + [objects[n] for n in SOURCES] + ["-o", LIB_PATH],
+             verbose)
     return LIB_PATH
 
 

@@ -1,4 +1,5 @@
 // C ABI entry points of libefim: argument checks, planning, staging of the work list.
+#include <atomic>
 #include <cstring>
 #include <mutex>
 #include <new>
@@ -19,25 +20,11 @@ namespace {
 
 thread_local int g_last_hip_error = 0;
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // Concurrent workgroup slots the planner balances for: two attention workgroups fit on a
-// compute unit (64 KB of LDS each).  Falls back to the MI355X figure when no device is
-// visible so that the pure host functions also work on a machine without a GPU.
+// compute unit (64 KB of LDS each).
 int num_slots() {
   if (tuning().num_slots > 0) return tuning().num_slots;
-  static int cached = 0;
-  if (cached == 0) {
-    int dev = 0, cus = 0;
-    if (hipGetDevice(&dev) == hipSuccess &&
-        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0)
-      cached = 2 * cus;
-    else {
-      (void)hipGetLastError();
-      return 512;
-    }
-  }
-  return cached;
+  return 2 * compute_units();
 }
 
 #define EFIM_HIP(expr)                                  \
@@ -367,6 +354,21 @@ const Plan& fp8_plan(const efim_batch_t* b) {
 
 void set_last_hip_error(hipError_t e) { g_last_hip_error = (int)e; }
 
+int compute_units() {
+  static std::atomic<int> cached{0};
+  int cus = cached.load(std::memory_order_relaxed);
+  if (cus == 0) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess ||
+        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) {
+      (void)hipGetLastError();
+      return 256;
+    }
+    cached.store(cus, std::memory_order_relaxed);
+  }
+  return cus;
+}
+
 }  // namespace efim
 
 using namespace efim;
@@ -386,9 +388,6 @@ int rope_append_checked(const efim_batch_t* batch, void* q, const void* k_new, c
   return launch_rope_append(batch, total, q, k_new, v_new, k_cache, v_cache, inv_freq, rotary_dim,
                             rope_interleaved, fmt, static_cast<hipStream_t>(stream));
 }
-
-// Scales of an 8-bit cache: finite and positive.
-bool scale_ok(float s) { return s > 0.f && s - s == 0.f; }
 
 int rope_append_base(const efim_batch_t* batch, void* q, const void* k_new, const void* v_new, void* k_cache,
                      void* v_cache, double rope_base, int rope_interleaved, void* stream, const CacheFormat& fmt) {

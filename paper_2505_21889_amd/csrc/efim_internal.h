@@ -122,6 +122,18 @@ struct CacheFormat {
 // Validates the host-visible part of a batch. total_new receives T.
 int validate_batch(const efim_batch_t* b, int64_t* total_new);
 
+// Latent caches: one row of kLatentRank latent and kLatentRope rotated elements a token, shared by all heads.
+constexpr int kLatentRank = 512;
+constexpr int kLatentRope = 64;
+constexpr int kLatentRow = kLatentRank + kLatentRope;
+constexpr int kMaxLatentHeads = 256;
+// Width of a head's key outside its rotated part, and of its value, where they are expanded from the latent.
+constexpr int kLatentNope = 128;
+constexpr int kLatentValue = 128;
+
+// The same for a batch over a latent cache.
+int validate_latent_batch(const efim_batch_t* b, int64_t* total_new);
+
 // Whether a launch with a counter draws the plan's queued items.  A draw costs a workgroup 1 to 1.5 us before it can
 // start: 16..24 tiles per item 0.8-4.5 % slower drawn (17 requests of 714..1181 +
 // 69..230 tokens, 32/32 heads 110 / 115 us), 28 and more 1-7.5 % faster (57 requests of 5319..16384 keys, one new
@@ -204,5 +216,23 @@ int launch_zero_words(int32_t* words, size_t count, hipStream_t stream);
 bool plan_merges_in_kernel(const Plan& plan);
 
 void set_last_hip_error(hipError_t e);
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Scales of an 8-bit cache: finite and positive.
+inline bool scale_ok(float s) { return s > 0.f && s - s == 0.f; }
+
+// A rotary table of the caller: rotary_dim / 2 finite frequencies.
+inline bool frequencies_ok(const double* inv_freq, int rotary_dim) {
+  if (!inv_freq) return false;
+  for (int j = 0; j < rotary_dim / 2; ++j)
+    if (!(inv_freq[j] - inv_freq[j] == 0.0)) return false;  // NaN / inf
+  return true;
+}
+
+// Compute units of the current device; the MI355X's number where no device is visible, so that pure host functions
+// also work on a machine without a GPU.
+int compute_units();
 
 }  // namespace efim

@@ -50,4 +50,30 @@ __device__ __forceinline__ uint32_t bf16_bits_to_e4m3(uint32_t bits16, double in
   return f != f ? 0x7Fu : e4m3_pair<false>(f, f, 0u) & 0xFFu;
 }
 
+typedef uint32_t e4m3_source __attribute__((ext_vector_type(4)));  // eight bf16 values
+typedef uint32_t e4m3_codes __attribute__((ext_vector_type(2)));   // and their codes
+
+// E4M3 codes of eight bf16 values; inv = 1 / (double)scale.
+__device__ __forceinline__ e4m3_codes quantize8(e4m3_source x, double inv) {
+  float f[8];
+  bool nan = false;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    f[2 * t] = bf16_quotient(x[t] << 16, inv);
+    f[2 * t + 1] = bf16_quotient(x[t] & 0xFFFF0000u, inv);
+    nan |= __builtin_isunordered(f[2 * t], f[2 * t + 1]);
+  }
+  e4m3_codes r;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    r[t] = e4m3_pair<true>(f[4 * t + 2], f[4 * t + 3], e4m3_pair<false>(f[4 * t], f[4 * t + 1], 0u));
+  if (nan) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      r[t] = f32_to_e4m3(f[4 * t]) | (f32_to_e4m3(f[4 * t + 1]) << 8) | (f32_to_e4m3(f[4 * t + 2]) << 16) |
+             (f32_to_e4m3(f[4 * t + 3]) << 24);
+  }
+  return r;
+}
+
 }  // namespace efim

@@ -1,0 +1,65 @@
+// How the absorbed latent attention cuts a batch into work items.  Host code without state: a call derives everything from
+// the lengths and hands the kernel a table of the requests, from which each workgroup works its item out.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "efim.h"
+
+namespace efim {
+
+constexpr int kLatentTileKeys = 32;     // keys of a tile
+constexpr int kLatentTableReqs = 128;   // requests of a launch (kernel arguments end at 4 KB)
+constexpr int kLatentRangeStep = 128;   // key ranges are multiples of this: a tile for each of four waves
+
+struct LatentReq {
+  int32_t req;         // block table row
+  int32_t cached;      // C_r
+  int32_t new_len;     // N_r > 0
+  int32_t row_start;   // first packed new-token row
+  int32_t item_start;  // first work item in the launch
+  int32_t slot_start;  // first partial result in the launch, where the key range is cut
+};
+
+struct LatentTable {
+  LatentReq req[kLatentTableReqs];
+  int32_t nreq;
+  int32_t items;       // of the launch
+  int32_t heads;
+  int32_t range;       // keys of a range
+  int32_t max_pages;
+  int32_t page_shift;
+  int32_t split_rows;  // most rows of a request whose range is cut, 0: none is
+};
+
+#if defined(__HIPCC__) || defined(__HIP__)
+#define EFIM_HOST_DEVICE __host__ __device__
+#else
+#define EFIM_HOST_DEVICE
+#endif
+
+// Ranges of a request of `keys` keys.
+EFIM_HOST_DEVICE inline int latent_splits(int keys, int range) { return (int)(((int64_t)keys + range - 1) / range); }
+
+struct LatentPlan {
+  int row_tile = 0;      // query rows of an item: 16 or 32 (waves share the rows), 128 (a wave has 32 of them)
+  int range = 0;         // keys of a range
+  int64_t slots = 0;     // partial results of the largest launch
+};
+LatentPlan plan_latent(const efim_batch_t* b, int units);
+
+// Workspace: partial outputs [slots][row_tile][512] and their (reference, sum).
+struct LatentBytes {
+  size_t off_o = 0, off_ml = 0, total = 0;
+};
+LatentBytes latent_bytes(const LatentPlan& plan);
+
+// Where the next launch of a batch begins.
+struct LatentCursor {
+  int req = 0;
+  int64_t row = 0;
+};
+// Fills the table of the next launch; false where no request with new tokens is left.
+bool latent_next(const efim_batch_t* b, const LatentPlan& plan, LatentCursor* at, LatentTable* table);
+
+}  // namespace efim

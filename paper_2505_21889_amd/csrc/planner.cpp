@@ -19,17 +19,25 @@ Tuning& tuning() {
   return t;
 }
 
-int validate_batch(const efim_batch_t* b, int64_t* total_new) {
+namespace {
+
+// The checks that both kinds of cache share, the head layout aside: signs, page size.
+int validate_scalars(const efim_batch_t* b) {
   if (!b) return EFIM_ERR_INVALID_ARG;
   if (b->batch < 0 || b->num_q_heads <= 0 || b->num_kv_heads <= 0 || b->head_dim <= 0 ||
       b->page_size <= 0 || b->max_pages_per_req < 0 || b->num_pages < 0)
     return EFIM_ERR_INVALID_ARG;
   if (b->num_q_heads % b->num_kv_heads != 0) return EFIM_ERR_INVALID_ARG;
-  if (b->head_dim != 64 && b->head_dim != 128) return EFIM_ERR_UNSUPPORTED;
-  // pages are powers of two; a 1 KB gather (4 or 8 tokens of one head) must not cross one
-  if (b->page_size < kMinPageSize || b->page_size > kMaxPageSize || (b->page_size & (b->page_size - 1)) != 0)
-    return EFIM_ERR_UNSUPPORTED;
-  if (b->num_q_heads / b->num_kv_heads > 64) return EFIM_ERR_UNSUPPORTED;
+  return EFIM_OK;
+}
+
+// Pages are powers of two; a 1 KB gather (4 or 8 tokens of one head) must not cross one.
+bool page_size_ok(int page_size) {
+  return page_size >= kMinPageSize && page_size <= kMaxPageSize && (page_size & (page_size - 1)) == 0;
+}
+
+// Lengths against the table and the cache; total_new receives T.
+int validate_lengths(const efim_batch_t* b, int64_t* total_new) {
   int64_t total = 0;
   if (b->batch > 0) {
     if (!b->cached_len || !b->new_len) return EFIM_ERR_INVALID_ARG;
@@ -48,6 +56,24 @@ int validate_batch(const efim_batch_t* b, int64_t* total_new) {
   }
   if (total_new) *total_new = total;
   return EFIM_OK;
+}
+
+}  // namespace
+
+int validate_batch(const efim_batch_t* b, int64_t* total_new) {
+  const int rc = validate_scalars(b);
+  if (rc != EFIM_OK) return rc;
+  if (b->head_dim != 64 && b->head_dim != 128) return EFIM_ERR_UNSUPPORTED;
+  if (!page_size_ok(b->page_size) || b->num_q_heads / b->num_kv_heads > 64) return EFIM_ERR_UNSUPPORTED;
+  return validate_lengths(b, total_new);
+}
+
+int validate_latent_batch(const efim_batch_t* b, int64_t* total_new) {
+  const int rc = validate_scalars(b);
+  if (rc != EFIM_OK) return rc;
+  if (b->num_kv_heads != 1 || b->head_dim != kLatentRow || b->num_q_heads > kMaxLatentHeads) return EFIM_ERR_UNSUPPORTED;
+  if (!page_size_ok(b->page_size)) return EFIM_ERR_UNSUPPORTED;
+  return validate_lengths(b, total_new);
 }
 
 namespace {

@@ -42,29 +42,6 @@ struct RopeArgs {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// E4M3 codes of eight bf16 values; inv = 1 / (double)scale.
-__device__ __forceinline__ u32x2 quantize8(u32x4 x, double inv) {
-  float f[8];
-  bool nan = false;
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    f[2 * t] = bf16_quotient(x[t] << 16, inv);
-    f[2 * t + 1] = bf16_quotient(x[t] & 0xFFFF0000u, inv);
-    nan |= __builtin_isunordered(f[2 * t], f[2 * t + 1]);
-  }
-  u32x2 r;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-    r[t] = e4m3_pair<true>(f[4 * t + 2], f[4 * t + 3], e4m3_pair<false>(f[4 * t], f[4 * t + 1], 0u));
-  if (nan) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-      r[t] = f32_to_e4m3(f[4 * t]) | (f32_to_e4m3(f[4 * t + 1]) << 8) | (f32_to_e4m3(f[4 * t + 2]) << 16) |
-             (f32_to_e4m3(f[4 * t + 3]) << 24);
-  }
-  return r;
-}
-
 // Rotates the eight pairs of a unit.  The results go through fp32 two at a time; the one pattern for
 // which that could round twice is looked for once per unit (one unit in 4000 has it) and the unit
 // then done again value by value.  (With the check and the integer rounding at every value they
