@@ -327,6 +327,51 @@ size_t efim_latent_workspace_bytes(const efim_batch_t* batch);
 int efim_latent_attention(const efim_batch_t* batch, const void* q, const void* latent_cache, void* out,
                           float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * efim_latent_attention_expanded -- the same attention with keys and values per head, expanded from the cached latents by
+ * w_kv: for whole prompts and long increments (from about 170 new tokens per request on it costs less than the absorbed form).
+ *   s_j = sm_scale * <q_i, [ W_uk,h row_j[:512] | row_j[512:] ]>,  p = softmax_j(s),  out_i = sum_j p_j W_uv,h row_j[:512]
+ *   q         DEVICE bf16 [T, H, 192]   128 plain elements and the 64 rotated ones
+ *   w_kv      DEVICE bf16 [H, 256, 512] rows 0..127 of a head are W_uk,h, rows 128..255 W_uv,h
+ *   out       DEVICE bf16 [T, H, 128]   must not alias q, w_kv or the cache
+ *   workspace as above, efim_latent_expanded_workspace_bytes(batch) bytes: the expanded keys and values of all requests with
+ *             new tokens, 640 bytes a key and head (0: an invalid batch or one beyond a launch's reach)
+ * Expanded keys and values are rounded to bf16; all sums are fp32.
+ */
+size_t efim_latent_expanded_workspace_bytes(const efim_batch_t* batch);
+int efim_latent_attention_expanded(const efim_batch_t* batch, const void* q, const void* latent_cache,
+                                   const void* w_kv, void* out, float sm_scale, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * efim_verify_drafts -- the end of a step with drafted tokens (a short step of up to 16 new tokens per request computes their
+ * probabilities): accepts or refuses them against the target's probabilities and draws the token that follows, so that
+ * the tokens are distributed as the target's own.  For request r with n = num_drafts[r] drafted tokens x_0 .. x_{n-1}:
+ *   x_i stays while  u_i q_i(x_i) < p_i(x_i);  a = number of tokens in front of the first that does not;
+ *   the next token is drawn from p_n where all stayed, else from max(p_a - q_a, 0), with u_n: the first token j with
+ *   w_0 + .. + w_j > u_n (w_0 + .. + w_{V-1}).
+ * Weights are probabilities in whole numbers of 2^-40 (rounded down; negative and NaN as 0, above 1 as 1) and u_n in whole
+ * numbers of 2^-24: the sums are exact and the result does not depend on their order.  Where nothing is left of p_a
+ * the token is drawn from p_a itself, where p_a holds nothing either it is -1.  A drafted token outside [0, V) is refused.
+ *   batch, num_drafts  B >= 0;  HOST [B], 0 <= n <= 63, read before the call returns
+ *   target_probs  DEVICE float, row stride target_stride >= vocab elements: the n + 1 rows of request 0, of request 1, ...
+ *   draft_probs   DEVICE float, row stride draft_stride: the n rows of request 0, ...  NULL: the draft is certain of its
+ *                 tokens (q(x_i) = 1), as one that looks them up
+ *   draft_tokens  DEVICE int32, packed as the rows of draft_probs
+ *   uniforms      DEVICE float in [0, 1), packed as the rows of target_probs: u_0 .. u_n of request 0, ...
+ *   tokens        DEVICE int32, packed likewise: the a accepted tokens, the drawn one, then -1
+ *   accepted      DEVICE int32 [B]: a
+ *   workspace     DEVICE, 256-byte aligned, efim_verify_workspace_bytes(batch, vocab) bytes, contents irrelevant
+ * Only kernels are launched and no host state is kept: the call may be captured into a HIP graph.
+ * Errors: EFIM_ERR_INVALID_ARG, EFIM_ERR_UNSUPPORTED (more than 63 drafted tokens of a request, a vocabulary above
+ * 2^22), EFIM_ERR_WORKSPACE, EFIM_ERR_LAUNCH.
+ * ------------------------------------------------------------------------------------- */
+size_t efim_verify_workspace_bytes(int batch, int vocab);
+int efim_verify_drafts(int batch, const int32_t* num_drafts, int vocab, const void* target_probs, int64_t target_stride,
+                       const void* draft_probs, int64_t draft_stride, const int32_t* draft_tokens,
+                       const void* uniforms, int32_t* tokens, int32_t* accepted, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------------------
  * Session pool: the FIM -> EFIM prompt rewrite in front of the engine (Sec. 3.1, steps 1-5
  * of the prompt transformation figure).  Host code only; no device is touched.

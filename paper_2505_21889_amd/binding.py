@@ -142,6 +142,14 @@ def _load():
     lib.efim_latent_workspace_bytes.restype = ctypes.c_size_t
     lib.efim_latent_attention.argtypes = [bp, vp, vp, vp, f32, vp, ctypes.c_size_t, vp]
     lib.efim_latent_attention.restype = i32
+    lib.efim_latent_expanded_workspace_bytes.argtypes = [bp]
+    lib.efim_latent_expanded_workspace_bytes.restype = ctypes.c_size_t
+    lib.efim_latent_attention_expanded.argtypes = [bp, vp, vp, vp, vp, f32, vp, ctypes.c_size_t, vp]
+    lib.efim_latent_attention_expanded.restype = i32
+    lib.efim_verify_workspace_bytes.argtypes = [i32, i32]
+    lib.efim_verify_workspace_bytes.restype = ctypes.c_size_t
+    lib.efim_verify_drafts.argtypes = [i32, vp, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.efim_verify_drafts.restype = i32
     lib.efim_extend_plan_items.argtypes = [bp, vp, i64]
     lib.efim_extend_plan_items.restype = i64
     lib.efim_plan_info.argtypes = [bp, i32, ctypes.POINTER(EfimPlanInfo)]
@@ -182,6 +190,8 @@ EXPORTED_SYMBOLS = (
     "efim_rope_append_fp8_table", "efim_decode_step_fp8_table",
     "efim_norm_rope_append", "efim_norm_rope_append_fp8",
     "efim_latent_append", "efim_latent_workspace_bytes", "efim_latent_attention",
+    "efim_latent_expanded_workspace_bytes", "efim_latent_attention_expanded",
+    "efim_verify_workspace_bytes", "efim_verify_drafts",
     "efim_extend_plan_items", "efim_plan_info", "efim_set_tuning", "efim_set_kernel_events", "efim_status_string",
     "efim_last_hip_error", "efim_version", "efim_source_digest", "efim_stream_release",
     "efim_plan_create", "efim_plan_destroy", "efim_plan_workspace_bytes", "efim_plan_upload",
@@ -443,6 +453,32 @@ def efim_latent_attention(batch, q, latent_cache, out, sm_scale, workspace, work
     _check(_lib.efim_latent_attention(ctypes.byref(batch.c), _ptr(q), _ptr(latent_cache), _ptr(out), float(sm_scale),
                                       _ptr(workspace), int(workspace_bytes), _stream_ptr(stream)),
            "efim_latent_attention")
+
+
+def efim_latent_expanded_workspace_bytes(batch):
+    return int(_lib.efim_latent_expanded_workspace_bytes(ctypes.byref(batch.c)))
+
+
+def efim_latent_attention_expanded(batch, q, latent_cache, w_kv, out, sm_scale, workspace, workspace_bytes, stream=None):
+    _check(_lib.efim_latent_attention_expanded(ctypes.byref(batch.c), _ptr(q), _ptr(latent_cache), _ptr(w_kv), _ptr(out),
+                                               float(sm_scale), _ptr(workspace), int(workspace_bytes),
+                                               _stream_ptr(stream)),
+           "efim_latent_attention_expanded")
+
+
+def efim_verify_workspace_bytes(batch, vocab):
+    return int(_lib.efim_verify_workspace_bytes(int(batch), int(vocab)))
+
+
+def efim_verify_drafts(num_drafts, vocab, target_probs, target_stride, draft_probs, draft_stride, draft_tokens, uniforms,
+                       tokens, accepted, workspace, workspace_bytes, stream=None):
+    """num_drafts: host sequence, one entry per request (the C call's batch is its length)."""
+    counts = np.ascontiguousarray(num_drafts, dtype=np.int32)
+    _check(_lib.efim_verify_drafts(int(counts.size), counts.ctypes.data if counts.size else None, int(vocab),
+                                   _ptr(target_probs), int(target_stride), _ptr(draft_probs), int(draft_stride),
+                                   _ptr(draft_tokens), _ptr(uniforms), _ptr(tokens), _ptr(accepted), _ptr(workspace),
+                                   int(workspace_bytes), _stream_ptr(stream)),
+           "efim_verify_drafts")
 
 
 def efim_extend_plan_items(batch):

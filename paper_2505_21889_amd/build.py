@@ -13,7 +13,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libefim.so")
 SOURCES = ["api.hip", "planner.cpp", "session_pool.cpp", "rope_append.hip", "extend_attention.hip",
-           "norm_append.hip", "latent_append.hip", "latent_plan.cpp", "latent_attention.hip"]
+           "norm_append.hip", "latent_append.hip", "latent_plan.cpp", "latent_attention.hip",
+           "latent_expanded.hip", "verify_drafts.hip"]
 # measured-ceiling kernels of the benchmark: a library of their own, never part of libefim.so
 CEILINGS_PATH = os.path.join(LIB_DIR, "libefim_ceilings.so")
 CEILINGS_SOURCES = ["ceilings.hip"]

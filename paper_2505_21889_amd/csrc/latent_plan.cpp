@@ -97,4 +97,52 @@ bool latent_next(const efim_batch_t* b, const LatentPlan& plan, LatentCursor* at
   return t->nreq > 0;
 }
 
+ExpandedPlan plan_expanded(const efim_batch_t* b, int units) {
+  ExpandedPlan plan;
+  // 256 rows share a gathered tile once more than 128 do, 128 leave more workgroups and less of a short last tile empty:
+  // the larger one where it still leaves every unit two of them.
+  int64_t large = 0;
+  for (int r = 0; r < b->batch; ++r) large += ((int64_t)b->new_len[r] + 255) / 256 * b->num_q_heads;
+  plan.row_tile = large >= 2 * (int64_t)units ? 256 : 128;
+  plan.ok = true;
+  LatentTable table;
+  LatentCursor at;
+  int row_items = 0;
+  while (expanded_next(b, plan, &at, &table, &row_items)) {
+    const int64_t heads = b->num_q_heads;
+    // (a request alone can pass the limit of threads of a launch)
+    if ((int64_t)table.items / 2 * heads > INT32_MAX / 512 || row_items * heads > INT32_MAX / 512) plan.ok = false;
+    const size_t bytes = (size_t)table.items * (size_t)heads * kExpandedTileBytes;
+    if (bytes > plan.bytes) plan.bytes = bytes;
+  }
+  return plan;
+}
+
+bool expanded_next(const efim_batch_t* b, const ExpandedPlan& plan, LatentCursor* at, LatentTable* t, int* row_items) {
+  t->nreq = 0;
+  t->heads = b->num_q_heads;
+  t->range = 0;
+  t->split_rows = 0;
+  t->max_pages = b->max_pages_per_req;
+  t->page_shift = 0;
+  while ((1 << t->page_shift) < b->page_size) ++t->page_shift;
+  int64_t key_tiles = 0, row_tiles = 0;
+  for (; at->req < b->batch && t->nreq < kLatentTableReqs; ++at->req) {
+    const int n = b->new_len[at->req];
+    if (n == 0) continue;
+    const int64_t more_keys = ((int64_t)b->cached_len[at->req] + n + 2 * kExpandedTileKeys - 1) / (2 * kExpandedTileKeys) * 2;
+    const int64_t more_rows = ((int64_t)n + plan.row_tile - 1) / plan.row_tile;
+    if (t->nreq > 0 && ((key_tiles + more_keys) * b->num_q_heads > INT32_MAX / 512 ||
+                        (row_tiles + more_rows) * b->num_q_heads > INT32_MAX / 512))
+      break;
+    t->req[t->nreq++] = LatentReq{at->req, b->cached_len[at->req], n, (int32_t)at->row, (int32_t)row_tiles, (int32_t)key_tiles};
+    key_tiles += more_keys;
+    row_tiles += more_rows;
+    at->row += n;
+  }
+  t->items = (int32_t)key_tiles;
+  *row_items = (int)row_tiles;
+  return t->nreq > 0;
+}
+
 }  // namespace efim

@@ -62,4 +62,18 @@ struct LatentCursor {
 // Fills the table of the next launch; false where no request with new tokens is left.
 bool latent_next(const efim_batch_t* b, const LatentPlan& plan, LatentCursor* at, LatentTable* table);
 
+// --- expanded form ---------------------------------------------------------------------------------------------------------
+// The table's item_start counts tiles of query rows and slot_start tiles of keys, of one head each; `items` is the key
+// tiles of a head.  A request has an even number of key tiles: the expansion makes them in pairs.
+constexpr int kExpandedTileKeys = 64;
+constexpr int kExpandedTileBytes = 64 * (192 + 128) * 2;
+
+struct ExpandedPlan {
+  bool ok = false;       // every launch's numbers of workgroups are within a launch's reach
+  int row_tile = 0;      // query rows of a workgroup: 128 or 256
+  size_t bytes = 0;      // workspace: the expanded tiles of the largest launch
+};
+ExpandedPlan plan_expanded(const efim_batch_t* b, int units);
+bool expanded_next(const efim_batch_t* b, const ExpandedPlan& plan, LatentCursor* at, LatentTable* table, int* row_items);
+
 }  // namespace efim
