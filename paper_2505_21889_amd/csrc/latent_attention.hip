@@ -73,41 +73,15 @@ __device__ __forceinline__ float scale_accumulator(float x, float f) {
   return x;
 }
 
-// The item of a workgroup.
-struct Item {
-  int req;         // block table row
-  int cached;
-  int row0;        // first query row of the tile, in rows (token x head) of the request
-  int rows;        // rows of the tile
-  int64_t first;   // packed query row of the request's row 0
-  int k0, k1;      // key range
-  int slot;        // partial result, -1: the whole range
-};
-
-template <int TILE>
-__device__ __forceinline__ Item find_item(const LatentTable& t, int item, int lane) {
+// The request of a work item.
+__device__ __forceinline__ LatentReq find_request(const LatentTable& t, int item, int lane) {
   int r = -1;
 #pragma unroll
   for (int i = 0; i < kLatentTableReqs / 64; ++i) {
     const int at = i * 64 + lane;
     r += __popcll(__ballot(at < t.nreq && t.req[min(at, t.nreq - 1)].item_start <= item));
   }
-  r = __builtin_amdgcn_readfirstlane(r);
-  const LatentReq q = t.req[r];
-  const int splits = latent_splits(q.cached + q.new_len, t.range);
-  const int within = item - q.item_start;
-  const int tile = within / splits, split = within - tile * splits;
-  Item it;
-  it.req = q.req;
-  it.cached = q.cached;
-  it.row0 = tile * TILE;
-  it.rows = min(TILE, q.new_len * t.heads - it.row0);
-  it.first = (int64_t)q.row_start * t.heads;
-  const int key_end = q.cached + (it.row0 + it.rows - 1) / t.heads + 1;
-  it.k0 = split * t.range;
-  it.k1 = min(it.k0 + t.range, key_end);
-  it.slot = splits > 1 ? q.slot_start + within : -1;
-  return it;
+  return t.req[__builtin_amdgcn_readfirstlane(r)];
 }
 
 // ROWS: query rows of a wave, 32 or 16, which is also the shape of its products.  KEYS: the four waves take the same rows and
@@ -121,14 +95,17 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
   constexpr bool R32 = ROWS == 32;
   constexpr int kSteps = R32 ? kLatentRow / 16 : kLatentRow / 32;  // products along a row
   constexpr int kBlocks = kLatentRank / (R32 ? 32 : 16);           // output blocks
-  __shared__ __attribute__((aligned(1024))) char lds[kWaves * kTileBytes];
+  constexpr int kZeros = kWaves * kTileBytes;  // 1 KB of zeros, in place of values that are not finite
+  __shared__ __attribute__((aligned(1024))) char lds[kZeros + 1024];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const LatentTable& t = args.table;
-  const Item it = find_item<TILE>(t, blockIdx.x, lane);
+  const LatentReq rq = find_request(t, blockIdx.x, lane);
+  const LatentItem it = latent_item(t, rq, blockIdx.x, TILE);
   const int heads = t.heads;
+  const int64_t first = (int64_t)rq.row_start * heads;  // packed query row of the request's row 0
   if (it.k0 >= it.k1) {
     // a range behind the tile's last key: no weight in the join
     if (it.slot >= 0 && tid < TILE) {
@@ -138,7 +115,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
     }
     return;
   }
-  const int32_t* pages = block_table + (int64_t)it.req * t.max_pages;
+  const int32_t* pages = block_table + (int64_t)rq.req * t.max_pages;
   const int page_shift = t.page_shift, page_mask = (1 << page_shift) - 1;
   const int ntiles = (it.k1 - it.k0 + kTileKeys - 1) / kTileKeys;
 
@@ -168,6 +145,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
     }
   };
 
+  // (every wave writes all the zeros: it reads them behind its own writes)
+  *reinterpret_cast<u32x4*>(lds + kZeros + lane * 16) = u32x4{0, 0, 0, 0};
+
   // first tiles
   const int step = KEYS ? kWaves : 1;
   int32_t ids[kGroups];
@@ -188,23 +168,24 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
   // the wave's query rows as operands; rows behind the tile's last are copies of it
   const int i = lane % ROWS, part = lane / ROWS;
   const int row = min((KEYS ? 0 : wave * ROWS) + i, it.rows - 1);
-  const uint16_t* q_row = q + (it.first + it.row0 + row) * kLatentRow + part * 8;
+  const uint16_t* q_row = q + (first + it.row0 + row) * kLatentRow + part * 8;
   bf16x8 qb[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) qb[s] = *reinterpret_cast<const bf16x8*>(q_row + s * (R32 ? 16 : 32));
-  const int visible = it.cached + (it.row0 + row) / heads + 1;
-  const int least = it.cached + (it.row0 + min((KEYS ? 0 : wave * ROWS), it.rows - 1)) / heads + 1;  // of the wave's first row
+  const int visible = rq.cached + (it.row0 + row) / heads + 1;
+  const int least = rq.cached + (it.row0 + min((KEYS ? 0 : wave * ROWS), it.rows - 1)) / heads + 1;  // of the wave's first row
 
   // LDS addresses of the operands, in a tile at 0: the chunk's low bits take part in the swizzle and need an address each,
   // all else goes into the offset field of the read
   constexpr int kKeyAddrs = R32 ? 4 : 2, kValueAddrs = R32 ? 2 : 4;
   uint32_t key_at[kKeyAddrs], value_at[kValueAddrs], value_at8[kValueAddrs];
+  const int value_key = R32 ? (lane >> 5) * 4 + ((lane & 15) >> 2) : (lane >> 4) * 4 + ((lane & 15) >> 2);
 #pragma unroll
   for (int s = 0; s < kKeyAddrs; ++s)
     key_at[s] = i * kRowBytes + ((((R32 ? 2 : 4) * s + part) ^ swizzle(i)) << 4);
   {
     const int w16 = lane & 15, blk = lane >> 4;
-    const int key = R32 ? (blk >> 1) * 4 + (w16 >> 2) : blk * 4 + (w16 >> 2);
+    const int key = value_key;
     const int chunk = (R32 ? 2 * (blk & 1) : 0) + ((w16 & 3) >> 1);
 #pragma unroll
     for (int d = 0; d < kValueAddrs; ++d) {
@@ -274,7 +255,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
 #pragma unroll
     for (int r = 0; r < kAcc * kKeyBlocks; ++r) sc[r] = acc[r / kAcc][r % kAcc];
     constexpr int kScores = R32 ? 16 : 8;
+    uint32_t unfit = 0;
     if (key0 + kTileKeys > least) {
+      unfit = unfit_keys<ROWS>(sc);
 #pragma unroll
       for (int r = 0; r < kScores; ++r) {
         const int key = key0 + (R32 ? (r >> 2) * 8 : (r >> 2) * 16) + part * 4 + (r & 3);
@@ -307,14 +290,26 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
       pb[r >> 3][(r & 7) >> 1] = two;
       l_run += __uint_as_float(two << 16) + __uint_as_float(two & 0xFFFF0000u);
     }
-    // values
+    // values: the addresses of the operands' keys `group` eighths (R32) or halves (R16) into the tile
+    constexpr int kKeyGroups = R32 ? 4 : 2, kGroupRows = R32 ? 8 : 16;
+    uint32_t at[kKeyGroups][kValueAddrs];
+#pragma unroll
+    for (int g = 0; g < kKeyGroups; ++g)
+#pragma unroll
+      for (int d = 0; d < kValueAddrs; ++d)
+        at[g][d] = buf + (R32 && (g & 1) ? value_at8[d] + (g - 1) * kGroupRows * kRowBytes : value_at[d] + g * kGroupRows * kRowBytes);
+    if (unfit) {
+#pragma unroll
+      for (int g = 0; g < kKeyGroups; ++g)
+#pragma unroll
+        for (int d = 0; d < kValueAddrs; ++d)
+          if (unfit >> (value_key + g * kGroupRows) & 1) at[g][d] = lds0 + kZeros;
+    }
     bf16x8 va[kAhead];
     auto read_value = [&](int n) __attribute__((always_inline)) {
-      const int k = n / kBlocks, d = n % kBlocks;
-      const uint32_t at = buf + k * 16 * kRowBytes + (d / kValueAddrs) * 128;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + value_at[d % kValueAddrs]));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-          (LDS_PTR(bf16x4))(uintptr_t)(at + (R32 ? value_at8[d % kValueAddrs] : value_at[d % kValueAddrs] + 16 * kRowBytes)));
+      const int k = n / kBlocks, d = n % kBlocks, c = (d / kValueAddrs) * 128;
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at[2 * k][d % kValueAddrs] + c));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at[2 * k + 1][d % kValueAddrs] + c));
       va[n % kAhead] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     constexpr int kValueSteps = kScores / 8 * kBlocks;
@@ -343,7 +338,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
       *reinterpret_cast<f32x4*>(args.part_o + ((int64_t)it.slot * TILE + tile_row) * kLatentRank + col) = v;
     } else {
       const u32x2 w = {pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
-      *reinterpret_cast<u32x2*>(out + (it.first + it.row0 + tile_row) * kLatentRank + col) = w;
+      *reinterpret_cast<u32x2*>(out + (first + it.row0 + tile_row) * kLatentRank + col) = w;
     }
   };
 

@@ -44,6 +44,17 @@ constexpr float kNoReference = -3.0e38f;
 __device__ __forceinline__ int key_swizzle(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int value_swizzle(int row) { return (row & 3) << 2; }
 
+// An operand of the value product without the keys named in `unfit`, by the bits of its elements 0..3 and 8 on.
+__device__ __forceinline__ bf16x8 without_keys(bf16x8 x, uint32_t unfit) {
+  u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t two = unfit >> (j < 2 ? 2 * j : 2 * j + 4);
+    w[j] &= (two & 1 ? 0u : 0xFFFFu) | (two & 2 ? 0u : 0xFFFF0000u);
+  }
+  return __builtin_bit_cast(bf16x8, w);
+}
+
 __device__ __forceinline__ LatentReq find_request(const LatentTable& t, int at, int lane, int LatentReq::*start) {
   int r = -1;
 #pragma unroll
@@ -242,7 +253,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m_run = kNoReference, l_run = 0.f;
 
-  for (int tile = 0; tile < ntiles; ++tile) {
+  auto work_off = [&](int tile, auto masked) __attribute__((always_inline)) {
+    constexpr bool kMasked = decltype(masked)::value;
     if (kStages == 3 && tile + 1 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -258,7 +270,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
       for (int s = 0; s < kSteps; ++s)
         sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
             *(const LDS_PTR(bf16x8))(uintptr_t)(buf + key_at[s & 3] + (s >> 2) * 128 + half * 32 * kKeyBytes), qb[s], sc, 0, 0, 0);
-      if (key0 + 32 > least) {
+      uint32_t unfit = 0;
+      if constexpr (kMasked) {
+        float raw[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) raw[r] = sc[r];
+        unfit = unfit_keys<32>(raw);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (key0 + (r >> 2) * 8 + part * 4 + (r & 3) >= visible) sc[r] = -__builtin_inff();
@@ -292,11 +309,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
           const uint32_t v = buf + value_at[d] + (half * 32 + k * 16) * kValueBytes;
           const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v));
           const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v + 8 * kValueBytes));
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7),
-                                                         __builtin_bit_cast(bf16x8, pb[k]), o[d], 0, 0, 0);
+          bf16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          if constexpr (kMasked)
+            if (unfit) a = without_keys(a, unfit >> (16 * k + 4 * part));
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, pb[k]), o[d], 0, 0, 0);
         }
     }
-  }
+  };
+  // Tiles that all rows of the wave see, then those that some see a part of.
+  const int plain = min(ntiles, least / kTileKeys);
+  for (int tile = 0; tile < plain; ++tile) work_off(tile, std::false_type{});
+  for (int tile = plain; tile < ntiles; ++tile) work_off(tile, std::true_type{});
   const float inv = 1.f / cross_half_sum(l_run);
   if (wave * 32 + i >= rows) return;
   uint16_t* dst = out + (packed * heads + head) * kLatentValue;

@@ -41,6 +41,27 @@ struct LatentTable {
 // Ranges of a request of `keys` keys.
 EFIM_HOST_DEVICE inline int latent_splits(int keys, int range) { return (int)(((int64_t)keys + range - 1) / range); }
 
+// A work item: a tile of a request's query rows (token x head) against a range of its keys.
+struct LatentItem {
+  int row0, rows;      // of the request
+  int k0, k1;          // empty (k0 >= k1) where the range lies behind the last key that the tile sees
+  int slot;            // partial result, -1: the range is whole
+};
+EFIM_HOST_DEVICE inline LatentItem latent_item(const LatentTable& t, const LatentReq& q, int item, int row_tile) {
+  const int splits = latent_splits(q.cached + q.new_len, t.range);
+  const int within = item - q.item_start;
+  const int tile = within / splits, split = within - tile * splits;
+  const int left = q.new_len * t.heads - tile * row_tile;
+  LatentItem it;
+  it.row0 = tile * row_tile;
+  it.rows = left < row_tile ? left : row_tile;
+  const int key_end = q.cached + (it.row0 + it.rows - 1) / t.heads + 1;
+  it.k0 = split * t.range;
+  it.k1 = key_end - it.k0 < t.range ? key_end : it.k0 + t.range;
+  it.slot = splits > 1 ? q.slot_start + within : -1;
+  return it;
+}
+
 struct LatentPlan {
   int row_tile = 0;      // query rows of an item: 16 or 32 (waves share the rows), 128 (a wave has 32 of them)
   int range = 0;         // keys of a range

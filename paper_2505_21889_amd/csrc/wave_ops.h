@@ -116,4 +116,29 @@ __device__ __forceinline__ void load_coherent(const float* at, float* a, float* 
   *b = __uint_as_float((uint32_t)(bits >> 32));
 }
 
+// A key whose row is not finite must not reach, as zero times infinity, the outputs of rows that do not see it.  Where a
+// tile holds keys that some row of the wave does not see, `unfit_keys` names those whose scores are finite for none of
+// the rows (as bits of the tile's 32 keys; a query row that is not finite makes its own scores so, not the others').  The
+// value product then takes zeros in place of their rows.  A row that does see such a key has a score, and so a weight,
+// that is no number, and keeps it.
+// ROWS 32: element r is key (r / 4) * 8 + lane / 32 * 4 + r % 4; ROWS 16: key (r / 4) * 16 + lane / 16 * 4 + r % 4.
+template <int ROWS, int N>
+__device__ __forceinline__ uint32_t unfit_keys(const float (&scores)[N]) {
+  float probe = 0.f;
+#pragma unroll
+  for (int r = 0; r < N; ++r) probe = __builtin_fmaf(scores[r], 0.f, probe);
+  uint32_t unfit = 0;
+  if (__any(probe != probe)) {
+    constexpr uint64_t kAll = ROWS == 32 ? 0xFFFFFFFFull : 0xFFFFull;
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const uint64_t lanes = __ballot(!__builtin_isfinite(scores[r]));
+#pragma unroll
+      for (int part = 0; part < 64 / ROWS; ++part)
+        if ((lanes >> (ROWS * part) & kAll) == kAll) unfit |= 1u << ((r >> 2) * (ROWS == 32 ? 8 : 16) + part * 4 + (r & 3));
+    }
+  }
+  return unfit;
+}
+
 }  // namespace efim
