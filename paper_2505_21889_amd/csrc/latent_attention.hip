@@ -46,8 +46,11 @@ static_assert(kGroupKeys <= kMinPageSize && kGroupLoads == 9, "a group of rows l
 struct LatentArgs {
   LatentTable table;
   float scale_log2;  // sm_scale * log2(e)
-  float* part_o;     // [slot][row tile][512] unnormalised outputs of the ranges of split tiles
-  float* part_ml;    // [slot][row tile][2] reference (log2 units) and sum
+  // Partial results of the ranges of split tiles, [slot][row tile]: the unnormalised output O as binary16 values O / a with
+  // a = 2^-15 max |O| over the row, and (reference in log2 units, sum, a, -).  Half the bytes of fp32; what is within 2^-29 of
+  // the row's largest keeps 11 significant bits, a fraction of what the output's own rounding to bf16 costs.
+  uint16_t* part_o;
+  float* part_ml;
 };
 
 // Swizzle of a tile row's chunks (exclusive or on the chunk's low three bits).  A row is 72 chunks, so neighbouring rows
@@ -73,320 +76,641 @@ __device__ __forceinline__ float scale_accumulator(float x, float f) {
   return x;
 }
 
-// The request of a work item.
-__device__ __forceinline__ LatentReq find_request(const LatentTable& t, int item, int lane) {
+// The request that a unit lies in.
+__device__ __forceinline__ int find_request(const LatentTable& t, int64_t unit, int lane) {
   int r = -1;
 #pragma unroll
   for (int i = 0; i < kLatentTableReqs / 64; ++i) {
     const int at = i * 64 + lane;
-    r += __popcll(__ballot(at < t.nreq && t.req[min(at, t.nreq - 1)].item_start <= item));
+    r += __popcll(__ballot(at < t.nreq && t.req[min(at, t.nreq - 1)].unit_start <= unit));
   }
-  return t.req[__builtin_amdgcn_readfirstlane(r)];
+  return __builtin_amdgcn_readfirstlane(r);
 }
 
-// ROWS: query rows of a wave, 32 or 16, which is also the shape of its products.  KEYS: the four waves take the same rows and
-// every fourth key tile each, in LDS of their own, and join their results at the end; else they take rows of their own and
-// share the tiles, three ahead.
-template <int ROWS, bool KEYS>
-__global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
-    const LatentArgs args, const uint16_t* __restrict__ q, const uint16_t* __restrict__ cache,
-    const int32_t* __restrict__ block_table, uint16_t* __restrict__ out) {
-  constexpr int TILE = KEYS ? ROWS : ROWS * kWaves;
-  constexpr bool R32 = ROWS == 32;
-  constexpr int kSteps = R32 ? kLatentRow / 16 : kLatentRow / 32;  // products along a row
-  constexpr int kBlocks = kLatentRank / (R32 ? 32 : 16);           // output blocks
-  constexpr int kZeros = kWaves * kTileBytes;  // 1 KB of zeros, in place of values that are not finite
-  __shared__ __attribute__((aligned(1024))) char lds[kZeros + 1024];
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
-
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const LatentTable& t = args.table;
-  const LatentReq rq = find_request(t, blockIdx.x, lane);
-  const LatentItem it = latent_item(t, rq, blockIdx.x, TILE);
-  const int heads = t.heads;
-  const int64_t first = (int64_t)rq.row_start * heads;  // packed query row of the request's row 0
-  if (it.k0 >= it.k1) {
-    // a range behind the tile's last key: no weight in the join
-    if (it.slot >= 0 && tid < TILE) {
-      float* ml = args.part_ml + ((int64_t)it.slot * TILE + tid) * 2;
-      ml[0] = kNoReference;
-      ml[1] = 0.f;
-    }
-    return;
-  }
-  const int32_t* pages = block_table + (int64_t)rq.req * t.max_pages;
-  const int page_shift = t.page_shift, page_mask = (1 << page_shift) - 1;
-  const int ntiles = (it.k1 - it.k0 + kTileKeys - 1) / kTileKeys;
-
-  // the lane's place in the nine loads of a group whose rows have an even eighth
-  uint32_t off[kGroupLoads];
+// The tile that a unit lies in, by the whole wave: 64 tiles of the request at a time.
+struct Place {
+  int r;           // request of the launch
+  int tile;
+  int units;       // of the tile
+  int64_t first;   // unit of the launch at which the tile begins
+};
+template <int TILE>
+__device__ __forceinline__ Place find_tile(const LatentTable& t, int64_t unit, int lane) {
+  Place at;
+  at.r = find_request(t, unit, lane);
+  const LatentReq& q = t.req[at.r];
+  at.first = q.unit_start;
+  at.tile = 0;
+  at.units = latent_units_of(q, t.heads, TILE, 0);
+  const int tiles = latent_tiles(q, t.heads, TILE);
+  if (tiles == 1) return at;
+  for (int t0 = 0; t0 < tiles; t0 += 64) {
+    const int mine = t0 + lane < tiles ? latent_units_of(q, t.heads, TILE, t0 + lane) : 0;
+    int upto = mine;  // of the lanes up to this one (64 tiles of at most 2^25 units)
 #pragma unroll
-  for (int j = 0; j < kGroupLoads; ++j) off[j] = (uint32_t)((lane ^ swizzle((j * 64 + lane) / kRowChunks)) << 4);
-  auto page_of = [&](int tile, int g) { return pages[min(it.k0 + tile * kTileKeys + g * kGroupKeys, it.k1 - 1) >> page_shift]; };
-  // group g of a tile into LDS at `to`; rows behind the range are copies of its last row
-  auto gather = [&](int tile, int g, int32_t page, uint32_t to) __attribute__((always_inline)) {
-    const int key = it.k0 + tile * kTileKeys + g * kGroupKeys;
-    if (key + kGroupKeys <= it.k1) {
-      const char* base = reinterpret_cast<const char*>(cache) + (((int64_t)page << page_shift) + (key & page_mask)) * kRowBytes;
-      const uint32_t flip = (g & 1) << 4;
-      load_to_lds_4x16(base, off[0] ^ flip, off[1] ^ flip, off[2] ^ flip, off[3] ^ flip, to);
-      load_to_lds_4x16(base + 4096, off[4] ^ flip, off[5] ^ flip, off[6] ^ flip, off[7] ^ flip, to + 4096);
-      load_to_lds_16(base + 8192, off[8] ^ flip, to + 8192);
+    for (int by = 1; by < 64; by <<= 1) {
+      const int other = __shfl_up(upto, by);
+      if (lane >= by) upto += other;
+    }
+    const uint64_t in_front = __ballot(at.first + upto <= unit);  // tiles that end in front of the unit
+    if (in_front != ~0ull) {
+      const int k = __popcll(in_front);
+      at.tile = t0 + k;
+      at.units = __builtin_amdgcn_readlane(mine, k);
+      at.first += __builtin_amdgcn_readlane(upto, k) - at.units;
+      return at;
+    }
+    at.first += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return at;
+}
+
+// A workgroup's share of the units, a tile's part at a time.
+template <int TILE>
+struct Share {
+  const LatentTable& t;
+  Place at;
+  int group;
+  int64_t next, end;   // units
+  bool first;
+  // the part at hand
+  LatentReq rq;
+  int row0, rows;      // of the request
+  int k0, k1;          // keys
+  int slot;            // partial result, -1: the workgroup has the whole tile
+  int64_t packed;      // packed query row of the tile's first row
+
+  __device__ __forceinline__ Share(const LatentTable& table, int lane) : t(table) {
+    // an XCD takes neighbouring shares, which have rows of the cache in common
+    group = (int)(blockIdx.x % kXcds) * (int)(gridDim.x / kXcds) + (int)(blockIdx.x / kXcds);
+    next = end = 0;
+    if (group >= t.groups) return;
+    next = t.first_unit(group);
+    end = t.first_unit(group + 1);
+    at = find_tile<TILE>(t, next, lane);
+    first = true;
+    part();
+  }
+  __device__ __forceinline__ bool done() const { return next >= end; }
+  __device__ __forceinline__ void part() {
+    rq = t.req[at.r];
+    row0 = at.tile * TILE;
+    rows = latent_rows_of(rq, t.heads, TILE, at.tile);
+    const int u0 = (int)(next - at.first), u1 = (int)min((int64_t)at.units, end - at.first);
+    k0 = u0 * kTileKeys;
+    k1 = min(u1 * kTileKeys, latent_keys_of(rq, t.heads, TILE, at.tile));
+    slot = u0 == 0 && u1 == at.units ? -1 : latent_slot(group, first);
+    packed = (int64_t)rq.row_start * t.heads + row0;
+  }
+  __device__ __forceinline__ void advance() {
+    first = false;
+    next = at.first + at.units;
+    if (done()) return;
+    at.first = next;
+    ++at.tile;
+    if (at.tile == latent_tiles(rq, t.heads, TILE)) {
+      ++at.r;
+      at.tile = 0;
+    }
+    at.units = latent_units_of(t.req[at.r], t.heads, TILE, at.tile);
+    part();
+  }
+};
+
+// Copies of cache rows into a tile, eight rows (a group) at a time: nine loads of 1 KB.
+struct Gather {
+  const char* cache;
+  int k1, page_shift, page_mask;
+  uint32_t swizzles;  // two bits for each of the nine loads: the swizzle of the row that this lane's chunk lies in, halved
+  uint32_t lane16;
+
+  __device__ __forceinline__ Gather(const uint16_t* rows, int end, int shift, int lane)
+      : cache(reinterpret_cast<const char*>(rows)), k1(end), page_shift(shift), page_mask((1 << shift) - 1), swizzles(0), lane16(lane * 16) {
+#pragma unroll
+    for (int j = 0; j < kGroupLoads; ++j) swizzles |= (uint32_t)(swizzle((j * 64 + lane) / kRowChunks) >> 1) << (2 * j);
+  }
+  // byte offset of load j in a group (its multiple of 1 KB aside) whose tile row divided by eight is even or odd
+  __device__ __forceinline__ uint32_t offset(int j, int odd) const { return lane16 ^ (((swizzles >> (2 * j)) & 3) << 5) ^ (odd << 4); }
+  __device__ __forceinline__ const char* row_at(int32_t page, int key) const {
+    return cache + (((int64_t)page << page_shift) + (key & page_mask)) * kRowBytes;
+  }
+  __device__ __forceinline__ bool whole(int key) const { return key + kGroupKeys <= k1; }
+  // group `key` .. key + 7, which is group g of its tile, to LDS at `to`; rows at or behind k1 become copies of the last one's
+  __device__ __forceinline__ void group(int key, int g, int32_t page, uint32_t to) const {
+    if (whole(key)) {
+      const char* base = row_at(page, key);
+      load_to_lds_4x16(base, offset(0, g & 1), offset(1, g & 1), offset(2, g & 1), offset(3, g & 1), to);
+      load_to_lds_4x16(base + 4096, offset(4, g & 1), offset(5, g & 1), offset(6, g & 1), offset(7, g & 1), to + 4096);
+      load_to_lds_16(base + 8192, offset(8, g & 1), to + 8192);
     } else {
-      const int last = it.k1 - 1, from = min(key, last & ~(kGroupKeys - 1));
-      const char* base = reinterpret_cast<const char*>(cache) + (((int64_t)page << page_shift) + (from & page_mask)) * kRowBytes;
-      const int most = last - from;
+      const int last = k1 - 1, from = min(key, last & ~(kGroupKeys - 1)), most = last - from;
+      const char* base = row_at(page, from);
 #pragma unroll 1
       for (int j = 0; j < kGroupLoads; ++j) {
-        const int n = j * 64 + lane, row = n / kRowChunks, chunk = n - row * kRowChunks;
+        const int n = j * 64 + (int)(lane16 >> 4), row = n / kRowChunks, chunk = n - row * kRowChunks;
         load_to_lds_16(base, (uint32_t)(min(row, most) * kRowBytes + ((chunk ^ swizzle(g * kGroupKeys + row)) << 4)), to + j * 1024);
       }
     }
-  };
-
-  // (every wave writes all the zeros: it reads them behind its own writes)
-  *reinterpret_cast<u32x4*>(lds + kZeros + lane * 16) = u32x4{0, 0, 0, 0};
-
-  // first tiles
-  const int step = KEYS ? kWaves : 1;
-  int32_t ids[kGroups];
-  if constexpr (KEYS) {
-    if (wave < ntiles) {
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) ids[g] = page_of(wave, g);
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) gather(wave, g, ids[g], lds0 + wave * kTileBytes + g * (kGroupKeys * kRowBytes));
-    }
-  } else {
-#pragma unroll
-    for (int a = 0; a < kWaves - 1; ++a)
-      if (a < ntiles) gather(a, wave, page_of(a, wave), lds0 + a * kTileBytes + wave * (kGroupKeys * kRowBytes));
-    ids[0] = page_of(kWaves - 1, wave);
   }
+};
 
-  // the wave's query rows as operands; rows behind the tile's last are copies of it
-  const int i = lane % ROWS, part = lane / ROWS;
-  const int row = min((KEYS ? 0 : wave * ROWS) + i, it.rows - 1);
-  const uint16_t* q_row = q + (first + it.row0 + row) * kLatentRow + part * 8;
-  bf16x8 qb[kSteps];
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) qb[s] = *reinterpret_cast<const bf16x8*>(q_row + s * (R32 ? 16 : 32));
-  const int visible = rq.cached + (it.row0 + row) / heads + 1;
-  const int least = rq.cached + (it.row0 + min((KEYS ? 0 : wave * ROWS), it.rows - 1)) / heads + 1;  // of the wave's first row
+constexpr float kPartScale = 0x1p-15f;
+constexpr float kOver = 256.f;  // 2^kSlack: a sum of rounded probabilities is never below its largest one
+constexpr int kGroupBytes = kGroupKeys * kRowBytes;
+constexpr int kZeros = kWaves * kTileBytes;  // 1 KB of zeros behind the tiles, in place of values that are not finite
+constexpr int kLdsBytes = kZeros + 1024;
 
-  // LDS addresses of the operands, in a tile at 0: the chunk's low bits take part in the swizzle and need an address each,
-  // all else goes into the offset field of the read
-  constexpr int kKeyAddrs = R32 ? 4 : 2, kValueAddrs = R32 ? 2 : 4;
-  uint32_t key_at[kKeyAddrs], value_at[kValueAddrs], value_at8[kValueAddrs];
-  const int value_key = R32 ? (lane >> 5) * 4 + ((lane & 15) >> 2) : (lane >> 4) * 4 + ((lane & 15) >> 2);
-#pragma unroll
-  for (int s = 0; s < kKeyAddrs; ++s)
-    key_at[s] = i * kRowBytes + ((((R32 ? 2 : 4) * s + part) ^ swizzle(i)) << 4);
-  {
-    const int w16 = lane & 15, blk = lane >> 4;
-    const int key = value_key;
-    const int chunk = (R32 ? 2 * (blk & 1) : 0) + ((w16 & 3) >> 1);
-#pragma unroll
-    for (int d = 0; d < kValueAddrs; ++d) {
-      const int c = (R32 ? 4 : 2) * d + chunk;
-      value_at[d] = key * kRowBytes + ((c ^ swizzle(key)) << 4) + (w16 & 1) * 8;
-      value_at8[d] = (key + 8) * kRowBytes + ((c ^ swizzle(key + 8)) << 4) + (w16 & 1) * 8;
-    }
-  }
-
+// LDS addresses of a wave's operands in a tile at 0.  The low bits of a chunk take part in the swizzle and need an address
+// each, all else goes into the offset field of the read.
+template <int ROWS>
+struct Operands {
+  static constexpr bool R32 = ROWS == 32;
+  static constexpr int kSteps = R32 ? kLatentRow / 16 : kLatentRow / 32;  // products along a row
+  static constexpr int kBlocks = kLatentRank / ROWS;                       // output blocks
+  static constexpr int kKeyBlocks = kTileKeys / ROWS;                      // of a tile
+  static constexpr int kKeyAddrs = R32 ? 4 : 2, kValueAddrs = R32 ? 2 : 4;
+  static constexpr int kKeyGroups = R32 ? 4 : 2, kGroupRows = R32 ? 8 : 16;  // rows of a value operand: value_key + multiples
   using Acc = std::conditional_t<R32, f32x16, f32x4>;
-  constexpr int kAcc = R32 ? 16 : 4;
-  Acc o[kBlocks];
-#pragma unroll
-  for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-    for (int r = 0; r < kAcc; ++r) o[d][r] = 0.f;
-  float m_run = kNoReference, l_run = 0.f;
-  auto product = [](bf16x8 a, bf16x8 b, Acc c) __attribute__((always_inline)) {
+  static constexpr int kAcc = R32 ? 16 : 4;
+  static constexpr int kScores = kAcc * kKeyBlocks;
+  uint32_t key_at, value_at;  // of the first; the others differ in the swizzled bits, 4 to 6
+  int value_key;
+
+  __device__ __forceinline__ explicit Operands(int lane) {
+    const int i = lane % ROWS, part = lane / ROWS;
+    key_at = i * kRowBytes + ((part ^ swizzle(i)) << 4);
+    const int w16 = lane & 15, blk = lane >> 4;
+    value_key = (R32 ? (blk >> 1) * 4 : blk * 4) + (w16 >> 2);
+    const int chunk = (R32 ? 2 * (blk & 1) : 0) + ((w16 & 3) >> 1);
+    value_at = value_key * kRowBytes + ((chunk ^ swizzle(value_key)) << 4) + (w16 & 1) * 8;
+  }
+  // (formed again in every tile: held through the loop the derived addresses cost the registers that operands wait in)
+  __device__ __forceinline__ void forget() { asm volatile("" : "+v"(key_at), "+v"(value_at)); }
+  static_assert(kRowBytes % 128 == 0, "rows leave the swizzled bits alone");
+  static __device__ __forceinline__ Acc product(bf16x8 a, bf16x8 b, Acc c) {
     if constexpr (R32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-  };
-  constexpr int kAhead = 4;  // operands read in front of their products
+  }
+  static constexpr int kKeyProducts = kSteps * kKeyBlocks, kValueProducts = kScores / 8 * kBlocks;
+};
 
-  for (int tile = KEYS ? wave : 0; tile < ntiles; tile += step) {
-    uint32_t buf;
-    if constexpr (KEYS) {
-      buf = lds0 + wave * kTileBytes;
+// Addresses of the key operands of the tile at `buf`.
+template <int ROWS>
+struct Keys {
+  using Op = Operands<ROWS>;
+  uint32_t at[Op::kKeyAddrs];
+  __device__ __forceinline__ Keys(const Op& op, uint32_t buf) {
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) ids[g] = page_of(tile + kWaves, g);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    } else {
-      buf = lds0 + (tile % kWaves) * kTileBytes;
-      const int ahead = min(ntiles - 1 - tile, kWaves - 2);
-      if (ahead == 2) asm volatile("s_waitcnt vmcnt(18)" ::: "memory");
-      else if (ahead == 1) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      const int next = tile + kWaves - 1;
-      if (next < ntiles)
-        gather(next, wave, ids[0], lds0 + (next % kWaves) * kTileBytes + wave * (kGroupKeys * kRowBytes));
-      ids[0] = page_of(next + 1, wave);
-    }
-    const int key0 = it.k0 + tile * kTileKeys;
+    for (int s = 0; s < Op::kKeyAddrs; ++s) at[s] = buf + (op.key_at ^ (s * (Op::R32 ? 32 : 64)));
+  }
+  // operand of score product n
+  __device__ __forceinline__ bf16x8 read(int n) const {
+    const int s = n / Op::kKeyBlocks, b = n % Op::kKeyBlocks;
+    return *(const LDS_PTR(bf16x8))(uintptr_t)(at[s % Op::kKeyAddrs] + (s / Op::kKeyAddrs) * 128 + b * 16 * kRowBytes);
+  }
+};
 
-    // scores: R32 lane i, half `part`: element r is key (r / 4) * 8 + part * 4 + r % 4; R16 lane i, quarter `part`: element r of
-    // block b is key b * 16 + part * 4 + r
-    float sc[R32 ? 16 : 8];
-    constexpr int kKeyBlocks = R32 ? 1 : 2;  // of a tile
-    bf16x8 ka[kAhead];
-    auto read_key = [&](int n) __attribute__((always_inline)) {  // operand of product n
-      const int s = n / kKeyBlocks, b = n % kKeyBlocks;
-      ka[n % kAhead] = *(const LDS_PTR(bf16x8))(uintptr_t)(buf + key_at[s % kKeyAddrs] + (s / kKeyAddrs) * 128 + b * 16 * kRowBytes);
-    };
-    Acc acc[kKeyBlocks];
+// Addresses of the value operands of the tile at `buf`, without the rows of its keys named in `unfit`.
+template <int ROWS>
+struct Values {
+  using Op = Operands<ROWS>;
+  uint32_t at[Op::kKeyGroups][Op::kValueAddrs];
+  __device__ __forceinline__ Values(const Op& op, uint32_t buf, uint32_t unfit, uint32_t zeros) {
+    // (the swizzle of a row eight further on differs in its lowest bit, sixteen further on it is the same)
 #pragma unroll
-    for (int b = 0; b < kKeyBlocks; ++b)
+    for (int g = 0; g < Op::kKeyGroups; ++g)
 #pragma unroll
-      for (int r = 0; r < kAcc; ++r) acc[b][r] = 0.f;
-#pragma unroll
-    for (int n = 0; n < kAhead; ++n) read_key(n);
-#pragma unroll
-    for (int n = 0; n < kSteps * kKeyBlocks; ++n) {
-      acc[n % kKeyBlocks] = product(ka[n % kAhead], qb[n / kKeyBlocks], acc[n % kKeyBlocks]);
-      if (n + kAhead < kSteps * kKeyBlocks) read_key(n + kAhead);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int r = 0; r < kAcc * kKeyBlocks; ++r) sc[r] = acc[r / kAcc][r % kAcc];
-    constexpr int kScores = R32 ? 16 : 8;
-    uint32_t unfit = 0;
-    if (key0 + kTileKeys > least) {
-      unfit = unfit_keys<ROWS>(sc);
-#pragma unroll
-      for (int r = 0; r < kScores; ++r) {
-        const int key = key0 + (R32 ? (r >> 2) * 8 : (r >> 2) * 16) + part * 4 + (r & 3);
-        sc[r] = key < visible ? sc[r] : -__builtin_inff();
-      }
-    }
-    float mx = sc[0];
-#pragma unroll
-    for (int r = 1; r < kScores; ++r) mx = fmaxf(mx, sc[r]);
-    if constexpr (!R32) mx = cross_quarter_max(mx);
-    mx = cross_half_max(mx) * args.scale_log2;
-    if (__any(mx > m_run + kSlack)) {
-      const float m_new = mx > m_run + kSlack ? mx : m_run;
-      const float f = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-      l_run *= f;
-      after_products();
-#pragma unroll
-      for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-        for (int r = 0; r < kAcc; ++r) o[d][r] = scale_accumulator(o[d][r], f);
-      before_products();
-      m_run = m_new;
-    }
-    u32x4 pb[kScores / 8];
-#pragma unroll
-    for (int r = 0; r < kScores; r += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(sc[r] * args.scale_log2 - m_run);
-      const float p1 = __builtin_amdgcn_exp2f(sc[r + 1] * args.scale_log2 - m_run);
-      const uint32_t two = pack_bf16(p0, p1);
-      pb[r >> 3][(r & 7) >> 1] = two;
-      l_run += __uint_as_float(two << 16) + __uint_as_float(two & 0xFFFF0000u);
-    }
-    // values: the addresses of the operands' keys `group` eighths (R32) or halves (R16) into the tile
-    constexpr int kKeyGroups = R32 ? 4 : 2, kGroupRows = R32 ? 8 : 16;
-    uint32_t at[kKeyGroups][kValueAddrs];
-#pragma unroll
-    for (int g = 0; g < kKeyGroups; ++g)
-#pragma unroll
-      for (int d = 0; d < kValueAddrs; ++d)
-        at[g][d] = buf + (R32 && (g & 1) ? value_at8[d] + (g - 1) * kGroupRows * kRowBytes : value_at[d] + g * kGroupRows * kRowBytes);
+      for (int d = 0; d < Op::kValueAddrs; ++d)
+        at[g][d] = buf + ((op.value_at ^ (d * (Op::R32 ? 64 : 32)) ^ (Op::R32 ? (g & 1) * 16 : 0)) + g * Op::kGroupRows * kRowBytes);
     if (unfit) {
 #pragma unroll
-      for (int g = 0; g < kKeyGroups; ++g)
+      for (int g = 0; g < Op::kKeyGroups; ++g)
 #pragma unroll
-        for (int d = 0; d < kValueAddrs; ++d)
-          if (unfit >> (value_key + g * kGroupRows) & 1) at[g][d] = lds0 + kZeros;
-    }
-    bf16x8 va[kAhead];
-    auto read_value = [&](int n) __attribute__((always_inline)) {
-      const int k = n / kBlocks, d = n % kBlocks, c = (d / kValueAddrs) * 128;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at[2 * k][d % kValueAddrs] + c));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at[2 * k + 1][d % kValueAddrs] + c));
-      va[n % kAhead] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    constexpr int kValueSteps = kScores / 8 * kBlocks;
-#pragma unroll
-    for (int n = 0; n < kAhead; ++n) read_value(n);
-#pragma unroll
-    for (int n = 0; n < kValueSteps; ++n) {
-      o[n % kBlocks] = product(va[n % kAhead], __builtin_bit_cast(bf16x8, pb[n / kBlocks]), o[n % kBlocks]);
-      if (n + kAhead < kValueSteps) read_value(n + kAhead);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (KEYS) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
-      if (tile + kWaves < ntiles)
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) gather(tile + kWaves, g, ids[g], buf + g * (kGroupKeys * kRowBytes));
+        for (int d = 0; d < Op::kValueAddrs; ++d)
+          if (unfit >> (op.value_key + g * Op::kGroupRows) & 1) at[g][d] = zeros;
     }
   }
-  if constexpr (!R32) l_run = cross_quarter_sum(l_run);
-  l_run = cross_half_sum(l_run);
+  // operand of value product n
+  __device__ __forceinline__ bf16x8 read(int n) const {
+    const int k = n / Op::kBlocks, d = n % Op::kBlocks, c = (d / Op::kValueAddrs) * 128;
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at[2 * k][d % Op::kValueAddrs] + c));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at[2 * k + 1][d % Op::kValueAddrs] + c));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+};
 
-  // Element r of block d is column d * ROWS + column(r) .. + 3 of row i.
-  auto column = [&](int d, int r4) { return R32 ? d * 32 + r4 * 8 + part * 4 : d * 16 + part * 4; };
-  auto write4 = [&](int tile_row, int col, f32x4 v, float inv) {
-    if (it.slot >= 0) {
-      *reinterpret_cast<f32x4*>(args.part_o + ((int64_t)it.slot * TILE + tile_row) * kLatentRank + col) = v;
-    } else {
-      const u32x2 w = {pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
-      *reinterpret_cast<u32x2*>(out + (first + it.row0 + tile_row) * kLatentRank + col) = w;
-    }
-  };
+// Scores of 32 keys for 32 rows: the sum of the products over n steps, `key(n)` and `query(n)` their operands.  Written out,
+// because the compiler gives every product accumulation registers once some have them, and the outputs take all of those.
+// It does not count wait states for it: a product's sum goes straight into the next, and whoever reads the last waits.
+template <int AHEAD, int STEPS, typename Key, typename Query>
+__device__ __forceinline__ f32x16 score_products(Key key, Query query) {
+  bf16x8 ka[AHEAD];
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n) ka[n] = key(n);
+  __builtin_amdgcn_sched_barrier(0);
+  f32x16 acc;
+#pragma unroll
+  for (int n = 0; n < STEPS; ++n) {
+    if (n == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(ka[0]), "v"(query(0)));
+    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(ka[n % AHEAD]), "v"(query(n)));
+    if (n + AHEAD < STEPS) ka[n % AHEAD] = key(n + AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(acc));
+  return acc;
+}
 
-  if constexpr (!KEYS) {
-    const int tile_row = wave * ROWS + i;
-    if (tile_row < it.rows) {
-      if (it.slot >= 0 && part == 0) {
-        float* ml = args.part_ml + ((int64_t)it.slot * TILE + tile_row) * 2;
-        ml[0] = m_run;
-        ml[1] = l_run;
+// Masks the scores of the tile whose first key is key0 for a row that sees keys in front of `visible`; returns its unfit keys.
+// R32: element r of lane i, half `part` is key (r / 4) * 8 + part * 4 + r % 4; R16: (r / 4) * 16 + part * 4 + r % 4.
+template <int ROWS, int N>
+__device__ __forceinline__ uint32_t mask_scores(float (&sc)[N], int key0, int visible, int part) {
+  const uint32_t unfit = unfit_keys<ROWS>(sc);
+#pragma unroll
+  for (int r = 0; r < N; ++r) {
+    const int key = key0 + (r >> 2) * (ROWS == 32 ? 8 : 16) + part * 4 + (r & 3);
+    sc[r] = key < visible ? sc[r] : -__builtin_inff();
+  }
+  return unfit;
+}
+template <int ROWS, int N>
+__device__ __forceinline__ float row_max(const float (&sc)[N]) {
+  float mx = sc[0];
+#pragma unroll
+  for (int r = 1; r < N; ++r) mx = fmaxf(mx, sc[r]);
+  if constexpr (ROWS == 16) mx = cross_quarter_max(mx);
+  return cross_half_max(mx);
+}
+
+__device__ __forceinline__ float add_pair(uint32_t two, float sum) {  // of two probabilities as they were rounded
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, sum, false);
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, f16x2));
+}
+
+// Writes a wave's 32 rows of outputs times `factor`: column d * 32 + r / 4 * 8 + part * 4 + r % 4 is element r of block d.  The two
+// halves of a wave exchange four columns each, so that a lane writes eight in a row.
+template <typename Pack>
+__device__ __forceinline__ void write_row(const f32x16 (&o)[16], uint16_t* to, float factor, int part, bool in_range, Pack pack) {
+#pragma unroll
+  for (int d = 0; d < 16; ++d)
+#pragma unroll
+    for (int r8 = 0; r8 < 2; ++r8) {
+      u32x2 x[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) x[h][k] = pack(o[d][r8 * 8 + h * 4 + 2 * k] * factor, o[d][r8 * 8 + h * 4 + 2 * k + 1] * factor);
+      u32x4 words;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const auto both = __builtin_amdgcn_permlane32_swap(x[0][k], x[1][k], false, false);
+        words[k] = both[0];
+        words[2 + k] = both[1];
       }
-      const float inv = 1.f / l_run;
-#pragma unroll
-      for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-        for (int r4 = 0; r4 < kAcc / 4; ++r4)
-          write4(tile_row, column(d, r4), f32x4{o[d][4 * r4], o[d][4 * r4 + 1], o[d][4 * r4 + 2], o[d][4 * r4 + 3]}, inv);
+      if (in_range) *reinterpret_cast<u32x4*>(to + d * 32 + r8 * 16 + part * 8) = words;
     }
-  } else {
-    // join of the four waves, 128 columns at a time: [wave][row][128 + 4]
+}
+
+// Items of more than 32 query rows: a wave takes 32 of 128 rows and the four share the tiles, three ahead.  Around a tile's
+// barrier a wave
+//   * adds the value product of tile h - 1 and turns the scores of tile h into probabilities under its products,
+//   * behind the barrier, which frees the buffer of h - 1 and publishes tile h + 1, forms the scores of h + 1 with the
+//     loads of tile h + 3 among the products.
+// One wave runs on a SIMD (256 registers of outputs, 144 of queries), so nothing else hides the softmax.  No maximum is
+// formed on the way: the reference is the row's maximum over the item's first tile, and moves where a tile's sum of
+// probabilities tells that one of them passed 2^kSlack.
+__global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
+                                                                     const uint16_t* __restrict__ cache,
+                                                                     const int32_t* __restrict__ block_table,
+                                                                     uint16_t* __restrict__ out) {
+  using Op = Operands<32>;
+  constexpr int TILE = 32 * kWaves;
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int heads = args.table.heads, page_shift = args.table.page_shift;
+  *reinterpret_cast<u32x4*>(lds + kZeros + lane * 16) = u32x4{0, 0, 0, 0};  // (by every wave: it reads behind its own writes)
+  Op op(lane);
+
+  for (Share<TILE> it(args.table, lane); !it.done(); it.advance()) {
+    const int32_t* pages = block_table + (int64_t)it.rq.req * args.table.max_pages;
+    const int ntiles = (it.k1 - it.k0 + kTileKeys - 1) / kTileKeys;
+    // the wave's queries as operands; rows behind the tile's last are copies of it
+    const int i = lane & 31, part = lane >> 5;
+    const int row = min(wave * 32 + i, it.rows - 1);
+    const uint16_t* q_row = q + (it.packed + row) * kLatentRow + part * 8;
+    bf16x8 qb[Op::kSteps];
+#pragma unroll
+    for (int s = 0; s < Op::kSteps; ++s) qb[s] = *reinterpret_cast<const bf16x8*>(q_row + s * 16);
+    // the wave gathers a quarter of each tile; lane t holds the page of its rows in tile held_from + t
+    const Gather gather(cache, it.k1, page_shift, lane);
+    auto key_of = [&](int tile) { return it.k0 + tile * kTileKeys + wave * kGroupKeys; };
+    auto pages_from = [&](int tile) { return pages[min(key_of(tile + lane), it.k1 - 1) >> page_shift]; };
+    int held_from = 0;
+    int32_t held = pages_from(0);
+    auto page_of = [&](int tile) { return __builtin_amdgcn_readlane(held, tile - held_from); };
+    auto buffer = [&](int tile) { return lds0 + (tile & (kWaves - 1)) * kTileBytes; };
+    gather.group(key_of(0), wave, page_of(0), buffer(0) + wave * kGroupBytes);
+    // (the loop below counts the gathers in flight itself: everything the compiler knows of is waited for here)
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int a = 1; a < kWaves - 1; ++a)
+      if (a < ntiles) gather.group(key_of(a), wave, page_of(a), buffer(a) + wave * kGroupBytes);
+    __syncthreads();
+
+    const int visible = it.rq.cached + (it.row0 + row) / heads + 1;
+    const int least = it.rq.cached + (it.row0 + min(wave * 32, it.rows - 1)) / heads + 1;  // of the wave's first row
+    f32x16 o[Op::kBlocks];
+#pragma unroll
+    for (int d = 0; d < Op::kBlocks; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    constexpr int kAhead = 6;  // operands read in front of their products
+    float sc[16];
+    uint32_t unfit = 0;
+
+    // scores of a tile; the gather of tile `next` goes out in front of the products
+    auto scores = [&](int tile, int next) __attribute__((always_inline)) {
+      if (next < ntiles) {
+        if (next - held_from >= 64) {
+          held_from = next;
+          held = pages_from(next);
+          __builtin_amdgcn_s_waitcnt(0x0F70);
+        }
+        gather.group(key_of(next), wave, page_of(next), buffer(next) + wave * kGroupBytes);
+      }
+      op.forget();
+      const Keys<32> keys(op, buffer(tile));
+      const f32x16 acc = score_products<kAhead, Op::kSteps>([&](int n) { return keys.read(n); }, [&](int n) { return qb[n]; });
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = acc[r];
+      unfit = 0;
+      const int key0 = it.k0 + tile * kTileKeys;
+      if (key0 + kTileKeys > least) unfit = mask_scores<32>(sc, key0, visible, part);
+    };
+
+    float m_run = kNoReference, l_run = 0.f;
+    u32x4 pb[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, pn[2];  // probabilities of the tile in front and of the one at hand, as operands
+    uint32_t pb_unfit = ~0u;                             // (in front of the first there is none)
+    auto probability = [&](int e) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(sc[e] * args.scale_log2 - m_run); };
+
+    // One copy of each product: a second one for the first or the last tile makes the compiler move the outputs between
+    // registers.  So the last round forms the value product of the last tile beside probabilities that nobody takes.
+    for (int tile = 0;; ++tile) {
+      if (tile < ntiles) {
+        if (tile > 0) {
+          // wait for the tile, of which a later one's gather may be in flight; then every wave is done with tile - 2
+          if (tile + 1 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kGroupLoads) : "memory");
+          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          __syncthreads();
+        }
+        scores(tile, tile > 0 ? tile + kWaves - 2 : ntiles);
+        if (tile == 0) m_run = fmaxf(row_max<32>(sc) * args.scale_log2, kNoReference);
+      }
+      // the value product of the tile in front and the probabilities of the scores at hand: an element to two products
+      const Values<32> v(op, buffer(tile + kWaves - 1), pb_unfit, lds0 + kZeros);
+      bf16x8 va[kAhead];
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) va[n] = v.read(n);
+      __builtin_amdgcn_sched_barrier(0);
+      float sum = 0.f, pair[2];
+#pragma unroll
+      for (int n = 0; n < Op::kValueProducts; ++n) {
+        o[n % Op::kBlocks] = Op::product(va[n % kAhead], __builtin_bit_cast(bf16x8, pb[n / Op::kBlocks]), o[n % Op::kBlocks]);
+        if (n + kAhead < Op::kValueProducts) va[n % kAhead] = v.read(n + kAhead);
+        if (n % 2 == 0) {
+          const int e = n / 2;
+          pair[e & 1] = probability(e);
+          if (e & 1) {
+            const uint32_t two = pack_bf16(pair[0], pair[1]);
+            pn[e >> 3][(e & 7) >> 1] = two;
+            sum = add_pair(two, sum);
+            asm volatile("" : "+v"(sum));  // (keeps the step in its place)
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (tile == ntiles) break;
+      // where a probability passed the slack its row's reference moves to its maximum and they are formed again
+      if (__any(sum >= kOver)) {
+        const float mx = row_max<32>(sc) * args.scale_log2;
+        const float m_new = mx > m_run + kSlack ? mx : m_run;
+        const float f = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= f;
+        after_products();
+#pragma unroll
+        for (int d = 0; d < Op::kBlocks; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] = scale_accumulator(o[d][r], f);
+        before_products();
+        m_run = m_new;
+        sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const uint32_t two = pack_bf16(probability(e), probability(e + 1));
+          pn[e >> 3][(e & 7) >> 1] = two;
+          sum = add_pair(two, sum);
+        }
+      }
+      l_run += sum;
+      pb[0] = pn[0];
+      pb[1] = pn[1];
+      pb_unfit = unfit;
+    }
+    l_run = cross_half_sum(l_run);
+
+    const int tile_row = wave * 32 + i;
+    if (it.slot >= 0) {
+      float top = 0.f;
+#pragma unroll
+      for (int d = 0; d < Op::kBlocks; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(o[d][r]));
+      top = cross_half_max(top);
+      const int64_t at = (int64_t)it.slot * TILE + tile_row;
+      if (tile_row < it.rows && part == 0) *reinterpret_cast<f32x4*>(args.part_ml + at * 4) = f32x4{m_run, l_run, top * kPartScale, 0.f};
+      write_row(o, args.part_o + at * kLatentRank, top > 0.f ? 1.f / (top * kPartScale) : 0.f, part, tile_row < it.rows,
+                [](float a, float b) { return pack_f16(a, b); });
+    } else {
+      write_row(o, out + (it.packed + tile_row) * kLatentRank, 1.f / l_run, part, tile_row < it.rows,
+                [](float a, float b) { return pack_bf16(a, b); });
+    }
+    __syncthreads();  // every wave is done with the part's tiles
+  }
+}
+
+// Items of at most ROWS (16 or 32) query rows: all waves take the same rows, every fourth key tile each, in LDS of their own,
+// and join their results at the end.  Such a step is bound by reading the cache; the waves wait for nothing but their
+// own gathers, so that some load while others compute.
+template <int ROWS>
+__global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
+                                                                     const uint16_t* __restrict__ cache,
+                                                                     const int32_t* __restrict__ block_table,
+                                                                     uint16_t* __restrict__ out) {
+  using Op = Operands<ROWS>;
+  using Acc = typename Op::Acc;
+  constexpr int kAcc = Op::kAcc;
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int heads = args.table.heads, page_shift = args.table.page_shift;
+  *reinterpret_cast<u32x4*>(lds + kZeros + lane * 16) = u32x4{0, 0, 0, 0};  // (by every wave: it reads behind its own writes)
+  Op op(lane);
+
+  for (Share<ROWS> it(args.table, lane); !it.done(); it.advance()) {
+    const int32_t* pages = block_table + (int64_t)it.rq.req * args.table.max_pages;
+    const int ntiles = (it.k1 - it.k0 + kTileKeys - 1) / kTileKeys;
+    // (the units are dealt to the waves in turn from one part to the next)
+    const int turn = (wave - (int)(it.next & (kWaves - 1))) & (kWaves - 1);
+    // the n-th tile of the wave; lane 4 n + g holds the page of group g of its tile held_from + n
+    const Gather gather(cache, it.k1, page_shift, lane);
+    const uint32_t buf = lds0 + wave * kTileBytes;
+    auto key_of = [&](int n, int g) { return it.k0 + (turn + n * kWaves) * kTileKeys + g * kGroupKeys; };
+    auto pages_from = [&](int n) { return pages[min(key_of(n + (lane >> 2), lane & 3), it.k1 - 1) >> page_shift]; };
+    int held_from = 0;
+    int32_t held = pages_from(0);
+    auto fetch = [&](int n) __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+        gather.group(key_of(n, g), g, __builtin_amdgcn_readlane(held, (n - held_from) * 4 + g), buf + g * kGroupBytes);
+    };
+    const int mine = (ntiles - turn + kWaves - 1) / kWaves;
+    if (mine > 0) fetch(0);
+
+    const int i = lane % ROWS, part = lane / ROWS;
+    const int row = min(i, it.rows - 1);
+    const uint16_t* q_row = q + (it.packed + row) * kLatentRow + part * 8;
+    bf16x8 qb[Op::kSteps];
+#pragma unroll
+    for (int s = 0; s < Op::kSteps; ++s) qb[s] = *reinterpret_cast<const bf16x8*>(q_row + s * (Op::R32 ? 16 : 32));
+    const int visible = it.rq.cached + (it.row0 + row) / heads + 1;
+    const int least = it.rq.cached + it.row0 / heads + 1;  // of the first row
+    Acc o[Op::kBlocks];
+#pragma unroll
+    for (int d = 0; d < Op::kBlocks; ++d)
+#pragma unroll
+      for (int r = 0; r < kAcc; ++r) o[d][r] = 0.f;
+    float m_run = kNoReference, l_run = 0.f;
+    constexpr int kAhead = 6;
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+
+    for (int n = 0; n < mine; ++n) {
+      if (n + 1 - held_from >= 16 && n + 1 < mine) {
+        held_from = n + 1;
+        held = pages_from(n + 1);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      op.forget();
+      const Keys<ROWS> keys(op, buf);
+      float sc[Op::kScores];
+      if constexpr (Op::R32) {
+        const f32x16 acc = score_products<kAhead, Op::kSteps>([&](int p) { return keys.read(p); }, [&](int p) { return qb[p]; });
+#pragma unroll
+        for (int r = 0; r < Op::kScores; ++r) sc[r] = acc[r];
+      } else {
+        bf16x8 ka[kAhead];
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) ka[p] = keys.read(p);
+        Acc acc[Op::kKeyBlocks];
+#pragma unroll
+        for (int b = 0; b < Op::kKeyBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < kAcc; ++r) acc[b][r] = 0.f;
+#pragma unroll
+        for (int p = 0; p < Op::kKeyProducts; ++p) {
+          acc[p % Op::kKeyBlocks] = Op::product(ka[p % kAhead], qb[p / Op::kKeyBlocks], acc[p % Op::kKeyBlocks]);
+          if (p + kAhead < Op::kKeyProducts) ka[p % kAhead] = keys.read(p + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int r = 0; r < Op::kScores; ++r) sc[r] = acc[r / kAcc][r % kAcc];
+      }
+      uint32_t unfit = 0;
+      const int key0 = key_of(n, 0);
+      if (key0 + kTileKeys > least) unfit = mask_scores<ROWS>(sc, key0, visible, part);
+      const float mx = row_max<ROWS>(sc) * args.scale_log2;
+      if (__any(mx > m_run + kSlack)) {
+        const float m_new = mx > m_run + kSlack ? mx : m_run;
+        const float f = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= f;
+        after_products();
+#pragma unroll
+        for (int d = 0; d < Op::kBlocks; ++d)
+#pragma unroll
+          for (int r = 0; r < kAcc; ++r) o[d][r] = scale_accumulator(o[d][r], f);
+        before_products();
+        m_run = m_new;
+      }
+      const Values<ROWS> v(op, buf, unfit, lds0 + kZeros);
+      bf16x8 va[kAhead];
+#pragma unroll
+      for (int p = 0; p < kAhead; ++p) va[p] = v.read(p);
+      u32x4 pb[Op::kScores / 8];
+#pragma unroll
+      for (int e = 0; e < Op::kScores; e += 2) {
+        const uint32_t two = pack_bf16(__builtin_amdgcn_exp2f(sc[e] * args.scale_log2 - m_run),
+                                       __builtin_amdgcn_exp2f(sc[e + 1] * args.scale_log2 - m_run));
+        pb[e >> 3][(e & 7) >> 1] = two;
+        l_run = add_pair(two, l_run);
+      }
+#pragma unroll
+      for (int p = 0; p < Op::kValueProducts; ++p) {
+        o[p % Op::kBlocks] = Op::product(va[p % kAhead], __builtin_bit_cast(bf16x8, pb[p / Op::kBlocks]), o[p % Op::kBlocks]);
+        if (p + kAhead < Op::kValueProducts) va[p % kAhead] = v.read(p + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
+      if (n + 1 < mine) fetch(n + 1);
+    }
+    if constexpr (!Op::R32) l_run = cross_quarter_sum(l_run);
+    l_run = cross_half_sum(l_run);
+
+    // join of the four waves, kCols columns at a time: [wave][row][kCols + 4], and behind them [wave][row] (reference, sum,
+    // largest magnitude, -)
     constexpr int kCols = 128, kPitch = kCols + 4;
-    static_assert(kWaves * ROWS * (kPitch + 2) * 4 <= kWaves * kTileBytes, "the join fits the tiles' place");
+    static_assert(kWaves * ROWS * (kPitch + 4) * 4 <= kZeros, "the join fits the tiles' place");
     float* const joined = reinterpret_cast<float*>(lds);
-    float* const s_ml = joined + kWaves * ROWS * kPitch;  // [wave][row][2]
-    __syncthreads();  // the tiles are read
-    if (part == 0) {
-      s_ml[(wave * ROWS + i) * 2] = m_run;
-      s_ml[(wave * ROWS + i) * 2 + 1] = l_run;
+    f32x4* const s_ml = reinterpret_cast<f32x4*>(joined + kWaves * ROWS * kPitch);
+    float top = 0.f;
+    if (it.slot >= 0) {
+#pragma unroll
+      for (int d = 0; d < Op::kBlocks; ++d)
+#pragma unroll
+        for (int r = 0; r < kAcc; ++r) top = fmaxf(top, fabsf(o[d][r]));
+      if constexpr (!Op::R32) top = cross_quarter_max(top);
+      top = cross_half_max(top);
     }
+    __syncthreads();  // the tiles are read
+    if (part == 0) s_ml[wave * ROWS + i] = f32x4{m_run, l_run, top, 0.f};
     __syncthreads();
     float m = kNoReference;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_ml[(w * ROWS + i) * 2]);
+    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, s_ml[k * ROWS + i][0]);
     const float f = __builtin_amdgcn_exp2f(m_run - m);
-    constexpr int kThreadsPerRow = 64 * kWaves / ROWS, kPer = kCols / kThreadsPerRow;
+    constexpr int kThreadsPerRow = 64 * kWaves / ROWS, kPer = kCols / kThreadsPerRow;  // 8 columns, or 16
     const int my_row = tid / kThreadsPerRow, my_col = tid % kThreadsPerRow * kPer;
-    float my_m = kNoReference, my_l = 0.f;
+    float my_m = kNoReference, my_l = 0.f, my_top = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) my_m = fmaxf(my_m, s_ml[(w * ROWS + my_row) * 2]);
+    for (int k = 0; k < kWaves; ++k) my_m = fmaxf(my_m, s_ml[k * ROWS + my_row][0]);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      my_l += s_ml[(w * ROWS + my_row) * 2 + 1] * __builtin_amdgcn_exp2f(s_ml[(w * ROWS + my_row) * 2] - my_m);
-    if (it.slot >= 0 && my_col == 0) {
-      float* ml = args.part_ml + ((int64_t)it.slot * TILE + my_row) * 2;
-      ml[0] = my_m;
-      ml[1] = my_l;
+    for (int k = 0; k < kWaves; ++k) {
+      const f32x4 ml = s_ml[k * ROWS + my_row];
+      const float weight = __builtin_amdgcn_exp2f(ml[0] - my_m);
+      my_l += ml[1] * weight;
+      my_top += ml[2] * weight;  // (no sum of the four is larger)
     }
-    const float inv = 1.f / my_l;
+    const int64_t at = (int64_t)it.slot * ROWS + my_row;
+    if (it.slot >= 0 && my_col == 0 && my_row < it.rows) *reinterpret_cast<f32x4*>(args.part_ml + at * 4) = f32x4{my_m, my_l, my_top * kPartScale, 0.f};
+    const float inv = it.slot < 0 ? 1.f / my_l : my_top > 0.f ? 1.f / (my_top * kPartScale) : 0.f;
+    uint16_t* const dst = (it.slot < 0 ? out + (it.packed + my_row) * kLatentRank : args.part_o + at * kLatentRank) + my_col;
     constexpr int kBlocksPerRound = kCols / ROWS;
 #pragma unroll
     for (int round = 0; round < kLatentRank / kCols; ++round) {
@@ -396,48 +720,93 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_attention_kernel(
 #pragma unroll
         for (int r4 = 0; r4 < kAcc / 4; ++r4) {
           const int d = round * kBlocksPerRound + b;
-          const f32x4 v = {o[d][4 * r4] * f, o[d][4 * r4 + 1] * f, o[d][4 * r4 + 2] * f, o[d][4 * r4 + 3] * f};
-          *reinterpret_cast<f32x4*>(joined + (wave * ROWS + i) * kPitch + column(b, r4)) = v;
+          const f32x4 x = {o[d][4 * r4] * f, o[d][4 * r4 + 1] * f, o[d][4 * r4 + 2] * f, o[d][4 * r4 + 3] * f};
+          *reinterpret_cast<f32x4*>(joined + (wave * ROWS + i) * kPitch + b * ROWS + r4 * 8 + part * 4) = x;
         }
       __syncthreads();
       if (my_row < it.rows) {
 #pragma unroll
-        for (int c = 0; c < kPer; c += 4) {
-          f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < kPer; c += 8) {
+          f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(joined + (w * ROWS + my_row) * kPitch + my_col + c);
-          write4(my_row, round * kCols + my_col + c, v, inv);
+          for (int k = 0; k < kWaves; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              x[h] += *reinterpret_cast<const f32x4*>(joined + (k * ROWS + my_row) * kPitch + my_col + c + 4 * h);
+          u32x4 words;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float a = x[k >> 1][2 * (k & 1)] * inv, b = x[k >> 1][2 * (k & 1) + 1] * inv;
+            words[k] = it.slot < 0 ? pack_bf16(a, b) : pack_f16(a, b);
+          }
+          *reinterpret_cast<u32x4*>(dst + round * kCols + c) = words;
         }
       }
     }
+    __syncthreads();  // what was joined has been read
   }
 }
 
-// Joins the ranges of split tiles: with M = max m, out = sum 2^(m - M) O / sum 2^(m - M) l, in the ranges' order.  Two rows to a
-// workgroup, 128 threads each; blockIdx.y is the request.
-__global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args, int row_tile, uint16_t* __restrict__ out) {
+// Joins the parts of a tile that several workgroups share: with M = max m, out = sum 2^(m - M) O / sum 2^(m - M) l, in the parts'
+// order.  blockIdx.y stands for the first workgroup whose share begins inside the tile; a wave takes every
+// 4 gridDim.x-th row, eight columns to a lane, eight parts' loads at a time.
+template <int TILE>
+__global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args, uint16_t* __restrict__ out) {
   const LatentTable& t = args.table;
-  const LatentReq q = t.req[blockIdx.y];
-  const int splits = latent_splits(q.cached + q.new_len, t.range);
-  const int row = blockIdx.x * 2 + (threadIdx.x >> 7), col = (threadIdx.x & 127) * 4;
-  if (splits < 2 || row >= q.new_len * t.heads) return;
-  const int tile = row / row_tile, in_tile = row - tile * row_tile;
-  const int64_t first = ((int64_t)q.slot_start + (int64_t)tile * splits) * row_tile + in_tile;
-  float m = kNoReference;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, args.part_ml[(first + (int64_t)s * row_tile) * 2]);
-  float l = 0.f;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const int64_t at = first + (int64_t)s * row_tile;
-    const float part = args.part_ml[at * 2 + 1];
-    if (part == 0.f) continue;  // (its output may never have been written)
-    const float w = __builtin_amdgcn_exp2f(args.part_ml[at * 2] - m);
-    l += w * part;
-    v += *reinterpret_cast<const f32x4*>(args.part_o + at * kLatentRank + col) * w;
+  const int lane = threadIdx.x & 63;
+  const int group = blockIdx.y + 1;
+  const int64_t cut = t.first_unit(group);
+  const Place at = find_tile<TILE>(t, cut, lane);
+  if (cut == at.first || t.first_unit(group - 1) > at.first) return;
+  const LatentReq q = t.req[at.r];
+  const int rows = latent_rows_of(q, t.heads, TILE, at.tile);
+  int parts = 2;
+  while (group - 1 + parts < t.groups && t.first_unit(group - 1 + parts) < at.first + at.units) ++parts;
+  // the first part is its workgroup's first too where the two begin together, the others are
+  const bool together = t.first_unit(group - 1) == at.first;
+  auto slot_of = [&](int s) { return latent_slot(group - 1 + s, s > 0 || together); };
+  for (int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); row < rows; row += 4 * gridDim.x) {
+    float m = kNoReference, l = 0.f, v[8] = {};
+    constexpr int kGroup = 8;
+    for (int s0 = 0; s0 < parts; s0 += kGroup) {
+      f32x4 ml[kGroup];
+      u32x4 h[kGroup];
+#pragma unroll
+      for (int s = 0; s < kGroup; ++s) {
+        const int64_t from = (int64_t)slot_of(min(s0 + s, parts - 1)) * TILE + row;
+        ml[s] = *reinterpret_cast<const f32x4*>(args.part_ml + from * 4);
+        h[s] = *reinterpret_cast<const u32x4*>(args.part_o + from * kLatentRank + lane * 8);
+      }
+      float m_new = m;
+#pragma unroll
+      for (int s = 0; s < kGroup; ++s)
+        if (s0 + s < parts) m_new = fmaxf(m_new, ml[s][0]);
+      const float f = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[c] *= f;
+#pragma unroll
+      for (int s = 0; s < kGroup; ++s) {
+        if (s0 + s >= parts) continue;
+        const float w = __builtin_amdgcn_exp2f(ml[s][0] - m), scale = w * ml[s][2];
+        l += w * ml[s][1];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+          const uint32_t word = h[s][c];
+          const f16x2 two = __builtin_bit_cast(f16x2, word);
+          v[2 * c] += (float)two[0] * scale;
+          v[2 * c + 1] += (float)two[1] * scale;
+        }
+      }
+    }
+    const float inv = 1.f / l;
+    u32x4 words;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) words[c] = pack_bf16(v[2 * c] * inv, v[2 * c + 1] * inv);
+    *reinterpret_cast<u32x4*>(out + ((int64_t)q.row_start * t.heads + at.tile * TILE + row) * kLatentRank + lane * 8) = words;
   }
-  const float inv = 1.f / l;
-  const u32x2 w = {pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
-  *reinterpret_cast<u32x2*>(out + ((int64_t)q.row_start * t.heads + row) * kLatentRank + col) = w;
 }
 
 int latent_attention(const efim_batch_t* b, const void* q, const void* cache, void* out, float sm_scale,
@@ -454,17 +823,20 @@ int latent_attention(const efim_batch_t* b, const void* q, const void* cache, vo
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < bytes.total) return EFIM_ERR_WORKSPACE;
   LatentArgs args;
   args.scale_log2 = sm_scale * 1.44269504088896340736f;
-  args.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + bytes.off_o);
+  args.part_o = static_cast<uint16_t*>(workspace);
   args.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + bytes.off_ml);
   LatentCursor at;
   while (latent_next(b, plan, &at, &args.table)) {
-    auto* kernel = plan.row_tile == 16 ? latent_attention_kernel<16, true>
-                   : plan.row_tile == 32 ? latent_attention_kernel<32, true> : latent_attention_kernel<32, false>;
-    kernel<<<args.table.items, 64 * kWaves, 0, stream>>>(args, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(cache),
-                                                        b->block_table, static_cast<uint16_t*>(out));
-    if (args.table.split_rows > 0)
-      latent_join_kernel<<<dim3((unsigned)((args.table.split_rows + 1) / 2), args.table.nreq), 256, 0, stream>>>(
-          args, plan.row_tile, static_cast<uint16_t*>(out));
+    const unsigned groups = (unsigned)(args.table.groups + kXcds - 1) / kXcds * kXcds;
+    auto launch = [&](auto* kernel, auto* join, int join_groups) {
+      kernel<<<groups, 64 * kWaves, 0, stream>>>(args, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(cache),
+                                                 b->block_table, static_cast<uint16_t*>(out));
+      if (args.table.groups > 1)
+        join<<<dim3(join_groups, args.table.groups - 1), 256, 0, stream>>>(args, static_cast<uint16_t*>(out));
+    };
+    if (plan.row_tile == 16) launch(latent_keys_kernel<16>, latent_join_kernel<16>, 4);
+    else if (plan.row_tile == 32) launch(latent_keys_kernel<32>, latent_join_kernel<32>, 8);
+    else launch(latent_rows_kernel, latent_join_kernel<128>, 16);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }
   }
@@ -479,6 +851,7 @@ extern "C" {
 size_t efim_latent_workspace_bytes(const efim_batch_t* batch) {
   int64_t total = 0;
   if (efim::validate_latent_batch(batch, &total) != EFIM_OK) return 0;
+  if (total == 0) return 256;
   const size_t bytes = efim::latent_bytes(efim::plan_latent(batch, efim::compute_units())).total;
   return bytes < 256 ? 256 : bytes;
 }

@@ -55,14 +55,16 @@ __device__ __forceinline__ bf16x8 without_keys(bf16x8 x, uint32_t unfit) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
-__device__ __forceinline__ LatentReq find_request(const LatentTable& t, int at, int lane, int LatentReq::*start) {
+// The request that a tile of keys, or of query rows, lies in.
+template <bool KEYS>
+__device__ __forceinline__ int find_request(const ExpandedTable& t, int tile, int lane) {
   int r = -1;
 #pragma unroll
   for (int i = 0; i < kLatentTableReqs / 64; ++i) {
-    const int k = i * 64 + lane;
-    r += __popcll(__ballot(k < t.nreq && t.req[min(k, t.nreq - 1)].*start <= at));
+    const int k = min(i * 64 + lane, t.nreq - 1);
+    r += __popcll(__ballot(i * 64 + lane < t.nreq && (KEYS ? (int)t.req[k].unit_start : t.row_tile_start[k]) <= tile));
   }
-  return t.req[__builtin_amdgcn_readfirstlane(r)];
+  return __builtin_amdgcn_readfirstlane(r);
 }
 
 // --- expansion -----------------------------------------------------------------------------------------------------------
@@ -74,7 +76,7 @@ constexpr int kExpandWaves = 8;
 
 // blockIdx.x: head (fastest, so that an XCD meets few heads' weights) and pair of tiles.  A wave forms 64 tokens x 64
 // outputs as W C^T: a lane's results are four neighbouring outputs of one token.
-__global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const LatentTable t, const uint16_t* __restrict__ cache,
+__global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const ExpandedTable t, const uint16_t* __restrict__ cache,
                                                                       const uint16_t* __restrict__ w_kv,
                                                                       const int32_t* __restrict__ block_table,
                                                                       char* __restrict__ tiles) {
@@ -84,9 +86,9 @@ __global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const Late
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int pair = blockIdx.x / t.heads, head = blockIdx.x - pair * t.heads;
-  const LatentReq rq = find_request(t, 2 * pair, lane, &LatentReq::slot_start);
+  const LatentReq rq = t.req[find_request<true>(t, 2 * pair, lane)];
   const int keys = rq.cached + rq.new_len;
-  const int key0 = (2 * pair - rq.slot_start) * kTileKeys;  // first token of the pair
+  const int key0 = (2 * pair - (int)rq.unit_start) * kTileKeys;  // first token of the pair
   const int32_t* pages = block_table + (int64_t)rq.req * t.max_pages;
   const int page_shift = t.page_shift, page_mask = (1 << page_shift) - 1;
   const char* w = reinterpret_cast<const char*>(w_kv) + (int64_t)head * kHeadOut * kLatentRank * 2;
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const Late
     *reinterpret_cast<u32x4*>(lds + (token / kTileKeys) * kTileBytes + row * kKeyBytes + ((16 + (chunk ^ key_swizzle(row))) << 4)) = v;
   }
   __syncthreads();
-  char* dst = tiles + ((int64_t)head * t.items + 2 * pair) * kTileBytes;
+  char* dst = tiles + ((int64_t)head * t.key_tiles + 2 * pair) * kTileBytes;
 #pragma unroll
   for (int j = 0; j < 2 * kTileBytes / (64 * kExpandWaves * 16); ++j) {
     const int n = (j * 64 * kExpandWaves + tid) * 16;
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const Late
 // --- attention -----------------------------------------------------------------------------------------------------------
 
 struct ExpandedArgs {
-  LatentTable table;   // item_start: tiles of query rows, slot_start: key tiles; items: key tiles of a head
+  ExpandedTable table;
   float scale_log2;
 };
 
@@ -205,16 +207,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const LatentTable& t = args.table;
+  const ExpandedTable& t = args.table;
   const int heads = t.heads;
   const int at = blockIdx.x / heads, head = blockIdx.x - at * heads;
-  const LatentReq rq = find_request(t, at, lane, &LatentReq::item_start);
+  const int r = find_request<false>(t, at, lane);
+  const LatentReq rq = t.req[r];
   const int row_tiles = (rq.new_len + TILE - 1) / TILE;
-  const int row0 = (row_tiles - 1 - (at - rq.item_start)) * TILE;
+  const int row0 = (row_tiles - 1 - (at - t.row_tile_start[r])) * TILE;
   const int rows = min(TILE, rq.new_len - row0);
   const int keys = rq.cached + row0 + rows;
   const int ntiles = (keys + kTileKeys - 1) / kTileKeys;
-  const char* src = tiles + ((int64_t)head * t.items + rq.slot_start) * kTileBytes + wave * (kLoads * 1024);
+  const char* src = tiles + ((int64_t)head * t.key_tiles + rq.unit_start) * kTileBytes + wave * (kLoads * 1024);
   auto fetch = [&](int tile) __attribute__((always_inline)) {
     const char* from = src + (int64_t)tile * kTileBytes;
     const uint32_t to = lds0 + (tile % kStages) * kTileBytes + wave * (kLoads * 1024);
@@ -349,16 +352,15 @@ int latent_attention_expanded(const efim_batch_t* b, const void* q, const void* 
   args.scale_log2 = sm_scale * 1.44269504088896340736f;
   char* tiles = static_cast<char*>(workspace);
   LatentCursor at;
-  int row_items = 0;
-  while (expanded_next(b, plan, &at, &args.table, &row_items)) {
+  while (expanded_next(b, plan, &at, &args.table)) {
     const unsigned heads = (unsigned)b->num_q_heads;
-    expand_kernel<<<(unsigned)args.table.items / 2 * heads, 64 * kExpandWaves, 0, stream>>>(
+    expand_kernel<<<(unsigned)args.table.key_tiles / 2 * heads, 64 * kExpandWaves, 0, stream>>>(
         args.table, static_cast<const uint16_t*>(cache), static_cast<const uint16_t*>(w_kv), b->block_table, tiles);
     if (plan.row_tile == 256)
-      expanded_attention_kernel<8><<<(unsigned)row_items * heads, 512, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
+      expanded_attention_kernel<8><<<(unsigned)args.table.row_tiles * heads, 512, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
                                                                                     static_cast<uint16_t*>(out));
     else
-      expanded_attention_kernel<4><<<(unsigned)row_items * heads, 256, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
+      expanded_attention_kernel<4><<<(unsigned)args.table.row_tiles * heads, 256, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
                                                                                     static_cast<uint16_t*>(out));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }

@@ -1,6 +1,7 @@
-// Plans of the latent attention on random batches: every query row of every request lies in one tile, the ranges of a tile
-// cover the keys that it sees once each, partial results have places of their own within the workspace, and no launch is
-// beyond what a grid takes.  Of the expanded form: every request has its key tiles and row tiles.
+// Plans of the latent attention on random batches: the shares of the workgroups are the units of all tiles once each, every
+// query row of every request lies in one tile and the tile's units hold the keys that it sees, no workgroup has more than
+// two parts of tiles that it does not have whole, and their places are its own and within the workspace.  Of the expanded
+// form: every request has its key tiles and row tiles.
 #include <cstdio>
 #include <cstdlib>
 #include <random>
@@ -15,8 +16,8 @@ using namespace efim;
 
 int main() {
   std::mt19937_64 rng(11);
-  long split = 0, launches = 0, tiles128 = 0, tiles256 = 0;
-  for (int iter = 0; iter < 6000; ++iter) {
+  long parts = 0, launches = 0, tiles128 = 0, tiles256 = 0;
+  for (int iter = 0; iter < 4000; ++iter) {
     const int B = (int)(rng() % 8 == 0 ? rng() % 400 : rng() % 24);
     std::vector<int32_t> cached(B), fresh(B);
     const int long_keys = 1 + (int)(rng() % 20000), most_new = 1 + (int)(rng() % (rng() % 3 ? 4 : 300));
@@ -38,59 +39,54 @@ int main() {
     b.block_table = reinterpret_cast<const int32_t*>(0x1000);
     int64_t total = 0;
     CHECK(validate_latent_batch(&b, &total) == EFIM_OK);
-    const LatentPlan plan = plan_latent(&b, 256);
+    const LatentPlan plan = plan_latent(&b, rng() % 2 ? 256 : 1 + (int)(rng() % 300));
     const LatentBytes bytes = latent_bytes(plan);
-    CHECK(plan.range > 0 && plan.range % kLatentRangeStep == 0);
     LatentCursor at;
     LatentTable t;
     int expect = 0;
     int64_t row = 0;
     while (latent_next(&b, plan, &at, &t)) {
       ++launches;
-      CHECK(t.nreq <= kLatentTableReqs && t.items > 0 && (int64_t)t.items * 256 <= INT32_MAX);
-      std::vector<char> used(plan.slots, 0);
-      int item = 0;
+      CHECK(t.nreq > 0 && t.nreq <= kLatentTableReqs && t.groups > 0 && t.groups <= plan.units);
+      CHECK(t.first_unit(0) == 0 && t.first_unit(t.groups) == t.units);
+      int group = 0, of_group = 0;       // the workgroup at hand, and how many parts of it are done
+      std::vector<int> used(plan.slots, 0);
+      int64_t unit = 0;
       for (int k = 0; k < t.nreq; ++k) {
         const LatentReq& q = t.req[k];
         while (fresh[expect] == 0) ++expect;
-        CHECK(q.req == expect && q.cached == cached[expect] && q.new_len == fresh[expect] && q.row_start == row && q.item_start == item);
-        const int end = k + 1 < t.nreq ? t.req[k + 1].item_start : t.items;
-        int rows = 0, keys = 0, whole = 0;  // of the tile at hand
-        for (; item < end; ++item) {
-          const LatentItem it = latent_item(t, q, item, plan.row_tile);
-          if (it.row0 != rows - whole) {  // the next tile
-            CHECK(it.row0 == rows);
+        CHECK(q.req == expect && q.cached == cached[expect] && q.new_len == fresh[expect] && q.row_start == row && q.unit_start == unit);
+        int rows = 0;
+        const int tiles = latent_tiles(q, t.heads, plan.row_tile);
+        for (int tile = 0; tile < tiles; ++tile) {
+          const int mine = latent_rows_of(q, t.heads, plan.row_tile, tile), units = latent_units_of(q, t.heads, plan.row_tile, tile);
+          CHECK(mine > 0 && mine <= plan.row_tile);
+          rows += mine;
+          const int seen = q.cached + (rows - 1) / t.heads + 1;  // of the last row
+          CHECK(latent_keys_of(q, t.heads, plan.row_tile, tile) == seen && units * kLatentTileKeys >= seen && (units - 1) * kLatentTileKeys < seen);
+          for (int64_t u = unit; u < unit + units;) {
+            while (t.first_unit(group + 1) <= u) {
+              ++group;
+              of_group = 0;
+            }
+            CHECK(group < t.groups && t.first_unit(group) <= u);
+            const int64_t end = t.first_unit(group + 1) < unit + units ? t.first_unit(group + 1) : unit + units;
+            if (u > unit || end < unit + units) {
+              ++parts;
+              const int slot = latent_slot(group, of_group == 0);
+              CHECK(slot < plan.slots && !used[slot]++);
+              CHECK(((size_t)slot + 1) * plan.row_tile * kLatentRank * 2 <= bytes.off_ml && bytes.off_ml + ((size_t)slot + 1) * plan.row_tile * 16 <= bytes.total);
+            }
+            ++of_group;
+            u = end;
           }
-          if (it.k0 == 0) {
-            CHECK(it.row0 == rows);
-            whole = it.rows;
-            rows += it.rows;
-            keys = 0;
-          }
-          CHECK(it.rows > 0 && it.rows <= plan.row_tile && it.row0 + it.rows == rows);
-          const int key_end = q.cached + (rows - 1) / b.num_q_heads + 1;
-          if (it.k0 < it.k1) {
-            CHECK(it.k0 == keys && it.k1 <= key_end);
-            keys = it.k1;
-          } else {
-            CHECK(keys == key_end);
-          }
-          if (it.slot >= 0) {
-            ++split;
-            CHECK(it.slot < plan.slots && !used[it.slot]);
-            used[it.slot] = 1;
-            CHECK(((size_t)it.slot + 1) * plan.row_tile * kLatentRank * 4 <= bytes.off_ml);
-            CHECK(bytes.off_ml + ((size_t)it.slot + 1) * plan.row_tile * 8 <= bytes.total);
-            CHECK(t.split_rows >= q.new_len * b.num_q_heads);
-          }
-          const LatentItem next = item + 1 < end ? latent_item(t, q, item + 1, plan.row_tile) : LatentItem{-1, 0, 0, 0, 0};
-          if (next.row0 != it.row0) CHECK(keys == key_end);
+          unit += units;
         }
-        CHECK(rows == q.new_len * b.num_q_heads);
+        CHECK(rows == q.new_len * t.heads);
         row += q.new_len;
         ++expect;
       }
-      CHECK(item == t.items);
+      CHECK(unit == t.units && group == t.groups - 1);
     }
     CHECK(row == total);
 
@@ -98,17 +94,17 @@ int main() {
     CHECK(ep.ok);
     (ep.row_tile == 256 ? tiles256 : tiles128) += 1;
     LatentCursor ea;
-    int row_items = 0;
+    ExpandedTable e;
     expect = 0;
     row = 0;
-    while (expanded_next(&b, ep, &ea, &t, &row_items)) {
-      CHECK(t.items % 2 == 0 && (size_t)t.items * b.num_q_heads * kExpandedTileBytes <= ep.bytes);
-      for (int k = 0; k < t.nreq; ++k) {
-        const LatentReq& q = t.req[k];
+    while (expanded_next(&b, ep, &ea, &e)) {
+      CHECK(e.key_tiles % 2 == 0 && (size_t)e.key_tiles * b.num_q_heads * kExpandedTileBytes <= ep.bytes);
+      for (int k = 0; k < e.nreq; ++k) {
+        const LatentReq& q = e.req[k];
         while (fresh[expect] == 0) ++expect;
         CHECK(q.req == expect && q.row_start == row);
-        const int key_tiles = (k + 1 < t.nreq ? t.req[k + 1].slot_start : t.items) - q.slot_start;
-        const int row_tiles = (k + 1 < t.nreq ? t.req[k + 1].item_start : row_items) - q.item_start;
+        const int64_t key_tiles = (k + 1 < e.nreq ? e.req[k + 1].unit_start : e.key_tiles) - q.unit_start;
+        const int row_tiles = (k + 1 < e.nreq ? e.row_tile_start[k + 1] : e.row_tiles) - e.row_tile_start[k];
         CHECK(key_tiles % 2 == 0 && key_tiles * kExpandedTileKeys >= q.cached + q.new_len && (key_tiles - 2) * kExpandedTileKeys < q.cached + q.new_len);
         CHECK(row_tiles == (q.new_len + ep.row_tile - 1) / ep.row_tile);
         row += q.new_len;
@@ -117,7 +113,7 @@ int main() {
     }
     CHECK(row == total);
   }
-  CHECK(split > 0 && tiles128 > 0 && tiles256 > 0);
-  printf("latent plan ok, %ld launches, %ld parts\n", launches, split);
+  CHECK(parts > 0 && tiles128 > 0 && tiles256 > 0);
+  printf("latent plan ok, %ld launches, %ld parts\n", launches, parts);
   return 0;
 }
