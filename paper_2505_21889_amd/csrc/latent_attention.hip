@@ -195,6 +195,10 @@ struct Gather {
     return cache + (((int64_t)page << page_shift) + (key & page_mask)) * kRowBytes;
   }
   __device__ __forceinline__ bool whole(int key) const { return key + kGroupKeys <= k1; }
+  // load j of a whole group whose first row is at `base`
+  __device__ __forceinline__ void piece(const char* base, int j, int odd, uint32_t to) const {
+    load_to_lds_16(base + j * 1024, offset(j, odd), to + j * 1024);
+  }
   // group `key` .. key + 7, which is group g of its tile, to LDS at `to`; rows at or behind k1 become copies of the last one's
   __device__ __forceinline__ void group(int key, int g, int32_t page, uint32_t to) const {
     if (whole(key)) {
@@ -275,13 +279,15 @@ template <int ROWS>
 struct Values {
   using Op = Operands<ROWS>;
   uint32_t at[Op::kKeyGroups][Op::kValueAddrs];
-  __device__ __forceinline__ Values(const Op& op, uint32_t buf, uint32_t unfit, uint32_t zeros) {
+  // addresses of one of the key groups
+  __device__ __forceinline__ void set(const Op& op, uint32_t buf, int g) {
     // (the swizzle of a row eight further on differs in its lowest bit, sixteen further on it is the same)
 #pragma unroll
-    for (int g = 0; g < Op::kKeyGroups; ++g)
-#pragma unroll
-      for (int d = 0; d < Op::kValueAddrs; ++d)
-        at[g][d] = buf + ((op.value_at ^ (d * (Op::R32 ? 64 : 32)) ^ (Op::R32 ? (g & 1) * 16 : 0)) + g * Op::kGroupRows * kRowBytes);
+    for (int d = 0; d < Op::kValueAddrs; ++d)
+      at[g][d] = buf + ((op.value_at ^ (d * (Op::R32 ? 64 : 32)) ^ (Op::R32 ? (g & 1) * 16 : 0)) + g * Op::kGroupRows * kRowBytes);
+  }
+  // zeros in place of the keys named in `unfit`
+  __device__ __forceinline__ void drop(const Op& op, uint32_t unfit, uint32_t zeros) {
     if (unfit) {
 #pragma unroll
       for (int g = 0; g < Op::kKeyGroups; ++g)
@@ -289,6 +295,11 @@ struct Values {
         for (int d = 0; d < Op::kValueAddrs; ++d)
           if (unfit >> (op.value_key + g * Op::kGroupRows) & 1) at[g][d] = zeros;
     }
+  }
+  __device__ __forceinline__ void set(const Op& op, uint32_t buf, uint32_t unfit, uint32_t zeros) {
+#pragma unroll
+    for (int g = 0; g < Op::kKeyGroups; ++g) set(op, buf, g);
+    drop(op, unfit, zeros);
   }
   // operand of value product n
   __device__ __forceinline__ bf16x8 read(int n) const {
@@ -299,26 +310,26 @@ struct Values {
   }
 };
 
-// Scores of 32 keys for 32 rows: the sum of the products over n steps, `key(n)` and `query(n)` their operands.  Written out,
-// because the compiler gives every product accumulation registers once some have them, and the outputs take all of those.
-// It does not count wait states for it: a product's sum goes straight into the next, and whoever reads the last waits.
-template <int AHEAD, int STEPS, typename Key, typename Query>
-__device__ __forceinline__ f32x16 score_products(Key key, Query query) {
-  bf16x8 ka[AHEAD];
-#pragma unroll
-  for (int n = 0; n < AHEAD; ++n) ka[n] = key(n);
-  __builtin_amdgcn_sched_barrier(0);
+// Scores of 32 keys for 32 rows: the sum of the products over the steps; `ahead` holds the first operands of the keys,
+// `key(n)` is the n-th, `query(n)` the other one, `beside(n)` what goes along with a product.  Written out, because the
+// compiler gives every product accumulation registers once some have them, and the outputs take all of those.  It counts no
+// wait states for it: a product's sum goes straight into the next, and the last one may be read kScoreStates behind it.
+constexpr int kScoreStates = 12;
+template <int AHEAD, int STEPS, typename Key, typename Query, typename Beside>
+__device__ __forceinline__ f32x16 score_products(bf16x8 (&ahead)[AHEAD], Key key, Query query, Beside beside) {
   f32x16 acc;
 #pragma unroll
   for (int n = 0; n < STEPS; ++n) {
-    if (n == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(ka[0]), "v"(query(0)));
-    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(ka[n % AHEAD]), "v"(query(n)));
-    if (n + AHEAD < STEPS) ka[n % AHEAD] = key(n + AHEAD);
+    if (n == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(ahead[0]), "v"(query(0)));
+    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(ahead[n % AHEAD]), "v"(query(n)));
+    if (n + AHEAD < STEPS) ahead[n % AHEAD] = key(n + AHEAD);
+    beside(n);
     __builtin_amdgcn_sched_barrier(0);
   }
-  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(acc));
   return acc;
 }
+// Lets the scores be read.
+__device__ __forceinline__ void await_scores(f32x16& acc) { asm volatile("s_nop %1" : "+v"(acc) : "n"(kScoreStates)); }
 
 // Masks the scores of the tile whose first key is key0 for a row that sees keys in front of `visible`; returns its unfit keys.
 // R32: element r of lane i, half `part` is key (r / 4) * 8 + part * 4 + r % 4; R16: (r / 4) * 16 + part * 4 + r % 4.
@@ -375,20 +386,22 @@ __device__ __forceinline__ void write_row(const f32x16 (&o)[16], uint16_t* to, f
     }
 }
 
-// Items of more than 32 query rows: a wave takes 32 of 128 rows and the four share the tiles, three ahead.  Around a tile's
-// barrier a wave
-//   * adds the value product of tile h - 1 and turns the scores of tile h into probabilities under its products,
-//   * behind the barrier, which frees the buffer of h - 1 and publishes tile h + 1, forms the scores of h + 1 with the
-//     loads of tile h + 3 among the products.
-// One wave runs on a SIMD (256 registers of outputs, 144 of queries), so nothing else hides the softmax.  No maximum is
-// formed on the way: the reference is the row's maximum over the item's first tile, and moves where a tile's sum of
-// probabilities tells that one of them passed 2^kSlack.
+// Tiles of 128 query rows: a wave takes 32 of them and the four share the key tiles, three ahead.  One wave runs on a SIMD (256
+// registers of outputs, 144 of queries), so whatever is not a product has to go out beside one.  Of key tile h a wave
+//   * forms the scores; beside the products go the gather of tile h + 2, a quarter each wave, and the first reads of the
+//     values of h - 1,
+//   * adds the value product of h - 1 and beside it turns the scores of h into probabilities; behind the last read of
+//     values, six products before the end, the waves meet: the buffer of h - 1 is free and tile h + 1 is there for all, and
+//     beside the six go the first reads of its keys.
+// No maximum is formed on the way: the reference is the row's maximum over the part's first key tile, and moves where a tile's
+// sum of probabilities tells that one of them passed 2^kSlack.
 __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
                                                                      const uint16_t* __restrict__ cache,
                                                                      const int32_t* __restrict__ block_table,
                                                                      uint16_t* __restrict__ out) {
   using Op = Operands<32>;
   constexpr int TILE = 32 * kWaves;
+  constexpr int kAhead = 6;  // operands read in front of their products
   __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -431,61 +444,85 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
     for (int d = 0; d < Op::kBlocks; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    constexpr int kAhead = 6;  // operands read in front of their products
-    float sc[16];
-    uint32_t unfit = 0;
-
-    // scores of a tile; the gather of tile `next` goes out in front of the products
-    auto scores = [&](int tile, int next) __attribute__((always_inline)) {
-      if (next < ntiles) {
-        if (next - held_from >= 64) {
-          held_from = next;
-          held = pages_from(next);
-          __builtin_amdgcn_s_waitcnt(0x0F70);
-        }
-        gather.group(key_of(next), wave, page_of(next), buffer(next) + wave * kGroupBytes);
-      }
-      op.forget();
-      const Keys<32> keys(op, buffer(tile));
-      const f32x16 acc = score_products<kAhead, Op::kSteps>([&](int n) { return keys.read(n); }, [&](int n) { return qb[n]; });
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = acc[r];
-      unfit = 0;
-      const int key0 = it.k0 + tile * kTileKeys;
-      if (key0 + kTileKeys > least) unfit = mask_scores<32>(sc, key0, visible, part);
-    };
-
     float m_run = kNoReference, l_run = 0.f;
     u32x4 pb[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, pn[2];  // probabilities of the tile in front and of the one at hand, as operands
-    uint32_t pb_unfit = ~0u;                             // (in front of the first there is none)
+    uint32_t unfit = 0, pb_unfit = ~0u;                  // (in front of the first there is none)
+    f32x16 sc;
     auto probability = [&](int e) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(sc[e] * args.scale_log2 - m_run); };
+    bf16x8 ka[kAhead], va[kAhead];
+    {
+      const Keys<32> keys(op, buffer(0));
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) ka[n] = keys.read(n);
+    }
 
     // One copy of each product: a second one for the first or the last tile makes the compiler move the outputs between
     // registers.  So the last round forms the value product of the last tile beside probabilities that nobody takes.
     for (int tile = 0;; ++tile) {
+      Values<32> v;
+      const uint32_t values_at = buffer(tile + kWaves - 1);
       if (tile < ntiles) {
-        if (tile > 0) {
-          // wait for the tile, of which a later one's gather may be in flight; then every wave is done with tile - 2
-          if (tile + 1 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kGroupLoads) : "memory");
-          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-          __syncthreads();
+        const int next = tile + kWaves - 2;
+        bool fetch = tile > 0 && next < ntiles;
+        const char* from = nullptr;
+        const uint32_t to = buffer(next) + wave * kGroupBytes;
+        if (fetch) {
+          if (next - held_from >= 64) {
+            held_from = next;
+            held = pages_from(next);
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+          }
+          const int key = key_of(next);
+          fetch = gather.whole(key);
+          if (fetch) from = gather.row_at(page_of(next), key);
+          else gather.group(key, wave, page_of(next), to);
         }
-        scores(tile, tile > 0 ? tile + kWaves - 2 : ntiles);
-        if (tile == 0) m_run = fmaxf(row_max<32>(sc) * args.scale_log2, kNoReference);
-      }
-      // the value product of the tile in front and the probabilities of the scores at hand: an element to two products
-      const Values<32> v(op, buffer(tile + kWaves - 1), pb_unfit, lds0 + kZeros);
-      bf16x8 va[kAhead];
+        op.forget();
+        const Keys<32> keys(op, buffer(tile));
+        constexpr int kLast = Op::kKeyProducts;
+        sc = score_products<kAhead, kLast>(
+            ka, [&](int n) { return keys.read(n); }, [&](int n) { return qb[n]; },
+            [&](int n) __attribute__((always_inline)) {
+              if (n % 2 == 1 && n / 2 < kGroupLoads && fetch) gather.piece(from, n / 2, wave & 1, to);
+              if (n >= kLast - kAhead - 4 && n < kLast - kAhead) v.set(op, values_at, n - (kLast - kAhead - 4));
+              if (n == kLast - kAhead - 1) v.drop(op, pb_unfit, lds0 + kZeros);
+              if (n >= kLast - kAhead) va[n - (kLast - kAhead)] = v.read(n - (kLast - kAhead));
+            });
+        unfit = 0;
+        const int key0 = it.k0 + tile * kTileKeys;
+        if (tile == 0 || key0 + kTileKeys > least) {
+          await_scores(sc);
+          float x[16];
 #pragma unroll
-      for (int n = 0; n < kAhead; ++n) va[n] = v.read(n);
+          for (int r = 0; r < 16; ++r) x[r] = sc[r];
+          unfit = mask_scores<32>(x, key0, visible, part);
+          if (tile == 0) m_run = fmaxf(row_max<32>(x) * args.scale_log2, kNoReference);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[r] = x[r];
+        }
+      } else {
+        v.set(op, values_at, pb_unfit, lds0 + kZeros);
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) va[n] = v.read(n);
+      }
       __builtin_amdgcn_sched_barrier(0);
+      constexpr int kMeet = Op::kValueProducts - kAhead;
       float sum = 0.f, pair[2];
+      const Keys<32> next_keys(op, buffer(tile + 1));
 #pragma unroll
       for (int n = 0; n < Op::kValueProducts; ++n) {
         o[n % Op::kBlocks] = Op::product(va[n % kAhead], __builtin_bit_cast(bf16x8, pb[n / Op::kBlocks]), o[n % Op::kBlocks]);
-        if (n + kAhead < Op::kValueProducts) va[n % kAhead] = v.read(n + kAhead);
-        if (n % 2 == 0) {
-          const int e = n / 2;
+        if (n < kMeet) va[n % kAhead] = v.read(n + kAhead);
+        if (n == kMeet - 1 && tile + 1 < ntiles) {
+          if (tile + 2 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kGroupLoads) : "memory");
+          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          __syncthreads();
+        }
+        if (n >= kMeet) ka[n - kMeet] = next_keys.read(n - kMeet);  // (behind the last tile: whatever is there, for nobody)
+        // the scores are read two products and some states behind the last of theirs, then an element to two products
+        if (n == 1) await_scores(sc);
+        const int e = n < 2 ? -1 : n == 31 ? 15 : n % 2 == 0 ? n / 2 - 1 : -1;
+        if (e >= 0) {
           pair[e & 1] = probability(e);
           if (e & 1) {
             const uint32_t two = pack_bf16(pair[0], pair[1]);
@@ -499,7 +536,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
       if (tile == ntiles) break;
       // where a probability passed the slack its row's reference moves to its maximum and they are formed again
       if (__any(sum >= kOver)) {
-        const float mx = row_max<32>(sc) * args.scale_log2;
+        float x[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = sc[r];
+        const float mx = row_max<32>(x) * args.scale_log2;
         const float m_new = mx > m_run + kSlack ? mx : m_run;
         const float f = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
         l_run *= f;
@@ -612,7 +652,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
       const Keys<ROWS> keys(op, buf);
       float sc[Op::kScores];
       if constexpr (Op::R32) {
-        const f32x16 acc = score_products<kAhead, Op::kSteps>([&](int p) { return keys.read(p); }, [&](int p) { return qb[p]; });
+        bf16x8 ka[kAhead];
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) ka[p] = keys.read(p);
+        f32x16 acc = score_products<kAhead, Op::kSteps>(ka, [&](int p) { return keys.read(p); }, [&](int p) { return qb[p]; }, [](int) {});
+        await_scores(acc);
 #pragma unroll
         for (int r = 0; r < Op::kScores; ++r) sc[r] = acc[r];
       } else {
@@ -649,7 +693,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
         before_products();
         m_run = m_new;
       }
-      const Values<ROWS> v(op, buf, unfit, lds0 + kZeros);
+      Values<ROWS> v;
+      v.set(op, buf, unfit, lds0 + kZeros);
       bf16x8 va[kAhead];
 #pragma unroll
       for (int p = 0; p < kAhead; ++p) va[p] = v.read(p);
