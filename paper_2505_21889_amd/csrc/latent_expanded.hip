@@ -35,7 +35,8 @@ constexpr int kValueBytes = kLatentValue * 2;
 constexpr int kKeysBytes = kTileKeys * kKeyBytes;
 constexpr int kTileBytes = kExpandedTileBytes;
 static_assert(kTileBytes == kTileKeys * (kKeyBytes + kValueBytes), "keys, then values");
-constexpr float kSlack = 8.f;
+constexpr float kSlack = 8.f;    // log2 units by which a row's maximum may outgrow its reference
+constexpr float kOver = 256.f;   // 2^kSlack: a sum of rounded probabilities is never below its largest one
 constexpr float kNoReference = -3.0e38f;
 
 // Swizzles of a tile row's 16-byte chunks.  Keys: 24 chunks, so neighbouring rows start half of the 256-byte bank line
@@ -43,17 +44,6 @@ constexpr float kNoReference = -3.0e38f;
 // the four chunks that a transposing read takes of each of eight rows.
 __device__ __forceinline__ int key_swizzle(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int value_swizzle(int row) { return (row & 3) << 2; }
-
-// An operand of the value product without the keys named in `unfit`, by the bits of its elements 0..3 and 8 on.
-__device__ __forceinline__ bf16x8 without_keys(bf16x8 x, uint32_t unfit) {
-  u32x4 w = __builtin_bit_cast(u32x4, x);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t two = unfit >> (j < 2 ? 2 * j : 2 * j + 4);
-    w[j] &= (two & 1 ? 0u : 0xFFFFu) | (two & 2 ? 0u : 0xFFFF0000u);
-  }
-  return __builtin_bit_cast(bf16x8, w);
-}
 
 // The request that a tile of keys, or of query rows, lies in.
 template <bool KEYS>
@@ -70,18 +60,26 @@ __device__ __forceinline__ int find_request(const ExpandedTable& t, int tile, in
 // --- expansion -----------------------------------------------------------------------------------------------------------
 
 constexpr int kTokens = 2 * kTileKeys;  // of a workgroup: two tiles
-constexpr int kDepth = 64;              // elements of the latent staged at a time
-constexpr int kStageBytes = (kTokens + kHeadOut) * kDepth * 2;
-constexpr int kExpandWaves = 8;
+constexpr int kDepth = 32;              // elements of the latent staged at a time
+constexpr int kDepthBytes = kDepth * 2;
+constexpr int kStageBytes = (kTokens + kHeadOut) * kDepthBytes;
+constexpr int kStageCount = 3;
+constexpr int kExpandWaves = 4;
 
-// blockIdx.x: head (fastest, so that an XCD meets few heads' weights) and pair of tiles.  A wave forms 64 tokens x 64
-// outputs as W C^T: a lane's results are four neighbouring outputs of one token.
+// Swizzle of a staged row's four 16-byte chunks: sixteen rows' equal chunks take the sixteen places of the bank line.
+__device__ __forceinline__ int stage_swizzle(int row) { return (row >> 2) & 3; }
+
+// blockIdx.x: head (fastest, so that an XCD meets few heads' weights) and pair of tiles.  A wave forms 64 tokens x 128
+// outputs as W C^T: a lane's results are four neighbouring outputs of one token, and an operand of either side serves two or
+// four products.  Two workgroups share a unit, so that one multiplies while the other writes its tiles; the loads are two
+// stages ahead.
 __global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const ExpandedTable t, const uint16_t* __restrict__ cache,
                                                                       const uint16_t* __restrict__ w_kv,
                                                                       const int32_t* __restrict__ block_table,
                                                                       char* __restrict__ tiles) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStageBytes];
-  static_assert(2 * kStageBytes >= 2 * kTileBytes, "the finished tiles take the stages' place");
+  constexpr int kLdsBytes = 2 * kTileBytes;
+  static_assert(kStageCount * kStageBytes <= kLdsBytes, "the finished tiles take the stages' place");
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -92,88 +90,97 @@ __global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const Expa
   const int32_t* pages = block_table + (int64_t)rq.req * t.max_pages;
   const int page_shift = t.page_shift, page_mask = (1 << page_shift) - 1;
   const char* w = reinterpret_cast<const char*>(w_kv) + (int64_t)head * kHeadOut * kLatentRank * 2;
+  // Tokens behind the request's last are copies of it (their scores are masked).
+  auto token_row = [&](int token) {
+    const int key = min(key0 + token, keys - 1);
+    const int64_t page = pages[key >> page_shift];
+    return reinterpret_cast<const char*>(cache) + ((page << page_shift) + (key & page_mask)) * (kLatentRow * 2);
+  };
 
-  // 1 KB loads of eight rows by 128 bytes: 16 of tokens, 32 of weight rows; lane l fetches row l / 8, its chunk l % 8
-  // swizzled.  Tokens behind the request's last are copies of it (their scores are masked).
-  constexpr int kTokenLoads = kTokens / 8, kLoads = kTokenLoads + kHeadOut / 8, kPerWave = kLoads / kExpandWaves;
-  static_assert(kTokenLoads == 2 * kExpandWaves && kPerWave == 6, "two loads of tokens, four of the weight a wave");
-  const char* src[kPerWave];
+  // 1 KB loads of sixteen rows by 64 bytes, eight of tokens and sixteen of weight rows: two and four a wave; lane l fetches row
+  // l / 4, its chunk l % 4 swizzled.
+  constexpr int kLoadRows = 1024 / kDepthBytes;
+  constexpr int kTokenLoads = kTokens / kLoadRows / kExpandWaves, kWeightLoads = kHeadOut / kLoadRows / kExpandWaves;
+  static_assert(kTokenLoads == 2 && kWeightLoads == 4, "loads of a wave and stage");
+  const char* token_src[kTokenLoads];
+  uint32_t weight_src[kWeightLoads];
 #pragma unroll
-  for (int j = 0; j < kPerWave; ++j) {
-    const int row = (j < 2 ? wave * 2 + j : wave * 4 + j - 2) * 8 + (lane >> 3);
-    const int chunk = (lane & 7) ^ key_swizzle(row);
-    if (j < 2) {
-      const int key = min(key0 + row, keys - 1);
-      const int64_t page = pages[key >> page_shift];
-      src[j] = reinterpret_cast<const char*>(cache) + ((page << page_shift) + (key & page_mask)) * (kLatentRow * 2) + chunk * 16;
-    } else {
-      src[j] = w + (int64_t)row * (kLatentRank * 2) + chunk * 16;
-    }
+  for (int j = 0; j < kTokenLoads; ++j) {
+    const int row = (wave * kTokenLoads + j) * kLoadRows + (lane >> 2);
+    token_src[j] = token_row(row) + (((lane & 3) ^ stage_swizzle(row)) << 4);
   }
-  auto fetch = [&](int step) {
-    const uint32_t to = lds0 + (step & 1) * kStageBytes;
 #pragma unroll
-    for (int j = 0; j < kPerWave; ++j)
-      load_to_lds_16(src[j] + step * (kDepth * 2), to + (j < 2 ? wave * 2 + j : kTokenLoads + wave * 4 + j - 2) * 1024);
+  for (int j = 0; j < kWeightLoads; ++j) {
+    const int row = (wave * kWeightLoads + j) * kLoadRows + (lane >> 2);
+    weight_src[j] = (uint32_t)(row * (kLatentRank * 2) + (((lane & 3) ^ stage_swizzle(row)) << 4));
+  }
+  auto stage = [&](int step) { return lds0 + (uint32_t)(step % kStageCount) * kStageBytes; };
+  auto fetch = [&](int step) __attribute__((always_inline)) {
+    const uint32_t to = stage(step);
+#pragma unroll
+    for (int j = 0; j < kTokenLoads; ++j)
+      load_to_lds_16(token_src[j] + step * kDepthBytes, to + (wave * kTokenLoads + j) * 1024);
+#pragma unroll
+    for (int j = 0; j < kWeightLoads; ++j)
+      load_to_lds_16(w + step * kDepthBytes, weight_src[j], to + kTokens * kDepthBytes + (wave * kWeightLoads + j) * 1024);
   };
   fetch(0);
+  fetch(1);
 
   const int i = lane & 31, part = lane >> 5;
-  const int token_half = wave & 1, out_quarter = wave >> 1;
-  f32x16 acc[2][2];  // [token block][output block]
+  const int token_half = wave & 1, out_half = wave >> 1;
+  f32x16 acc[2][4];  // [token block][output block]
 #pragma unroll
   for (int a = 0; a < 2; ++a)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
-  uint32_t at[4];  // of an operand's step in a row of 128 bytes
+  uint32_t at[2];  // of an operand in a staged row
 #pragma unroll
-  for (int s = 0; s < 4; ++s) at[s] = i * (kDepth * 2) + (((2 * s + part) ^ key_swizzle(i)) << 4);
-  constexpr int kStepCount = kLatentRank / kDepth;
-  for (int step = 0; step < kStepCount; ++step) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  for (int s = 0; s < 2; ++s) at[s] = i * kDepthBytes + (((2 * s + part) ^ stage_swizzle(i)) << 4);
+  constexpr int kSteps = kLatentRank / kDepth;
+  for (int step = 0; step < kSteps; ++step) {
+    if (step + 1 < kSteps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kTokenLoads + kWeightLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (step + 1 < kStepCount) fetch(step + 1);
-    const uint32_t tok = lds0 + (step & 1) * kStageBytes + token_half * 64 * (kDepth * 2);
-    const uint32_t wgt = lds0 + (step & 1) * kStageBytes + kTokens * (kDepth * 2) + out_quarter * 64 * (kDepth * 2);
+    if (step + 2 < kSteps) fetch(step + 2);
+    const uint32_t tok = stage(step) + token_half * 64 * kDepthBytes;
+    const uint32_t wgt = stage(step) + kTokens * kDepthBytes + out_half * 128 * kDepthBytes;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      bf16x8 x[2], y[2];
+    for (int s = 0; s < 2; ++s) {
+      bf16x8 x[2], y[4];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        x[b] = *(const LDS_PTR(bf16x8))(uintptr_t)(tok + at[s] + b * 32 * (kDepth * 2));
-        y[b] = *(const LDS_PTR(bf16x8))(uintptr_t)(wgt + at[s] + b * 32 * (kDepth * 2));
-      }
+      for (int a = 0; a < 2; ++a) x[a] = *(const LDS_PTR(bf16x8))(uintptr_t)(tok + at[s] + a * 32 * kDepthBytes);
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
+      for (int b = 0; b < 4; ++b) y[b] = *(const LDS_PTR(bf16x8))(uintptr_t)(wgt + at[s] + b * 32 * kDepthBytes);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[b], x[a], acc[a][b], 0, 0, 0);
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int a = 0; a < 2; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[b], x[a], acc[a][b], 0, 0, 0);
     }
   }
   __syncthreads();
   // the tiles as the attention takes them, in LDS, then out in whole lines
+  char* const tile = lds + token_half * kTileBytes;
 #pragma unroll
   for (int a = 0; a < 2; ++a)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
-        const int row = a * 32 + i;  // of tile `token_half`
-        const int col = out_quarter * 64 + b * 32 + r4 * 8 + part * 4;
+        const int row = a * 32 + i;
+        const int col = b * 32 + r4 * 8 + part * 4;  // of the keys (out_half 0) or of the values
         const u32x2 v = {pack_bf16(acc[a][b][4 * r4], acc[a][b][4 * r4 + 1]), pack_bf16(acc[a][b][4 * r4 + 2], acc[a][b][4 * r4 + 3])};
-        char* tile = lds + token_half * kTileBytes;
-        char* to = col < kLatentNope ? tile + row * kKeyBytes + (((col >> 3) ^ key_swizzle(row)) << 4)
-                                     : tile + kKeysBytes + row * kValueBytes + ((((col - kLatentNope) >> 3) ^ value_swizzle(row)) << 4);
-        *reinterpret_cast<u32x2*>(to + (col & 4) * 2) = v;
+        char* to = out_half == 0 ? tile + row * kKeyBytes + (((col >> 3) ^ key_swizzle(row)) << 4)
+                                 : tile + kKeysBytes + row * kValueBytes + (((col >> 3) ^ value_swizzle(row)) << 4);
+        *reinterpret_cast<u32x2*>(to + part * 8) = v;
       }
   // rotated part of the keys: 8 chunks a token, of the cache
 #pragma unroll
   for (int j = 0; j < kTokens * 8 / (64 * kExpandWaves); ++j) {
     const int n = j * 64 * kExpandWaves + tid, token = n >> 3, chunk = n & 7;
-    const int key = min(key0 + token, keys - 1);
-    const int64_t page = pages[key >> page_shift];
-    const u32x4 v = *reinterpret_cast<const u32x4*>(cache + ((page << page_shift) + (key & page_mask)) * kLatentRow + kLatentRank + chunk * 8);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(token_row(token) + kLatentRank * 2 + chunk * 16);
     const int row = token & (kTileKeys - 1);
     *reinterpret_cast<u32x4*>(lds + (token / kTileKeys) * kTileBytes + row * kKeyBytes + ((16 + (chunk ^ key_swizzle(row))) << 4)) = v;
   }
@@ -194,19 +201,26 @@ struct ExpandedArgs {
 };
 
 // blockIdx.x: head (fastest: an XCD meets few heads, whose tiles its workgroups share) and tile of 32 * WAVES query rows,
-// the request's last rows, which see most keys, first.
+// the request's last rows, which see most keys, first.  A wave takes 32 rows.
+//
+// The keys are worked off in halves of a tile, three at a time: while the scores of half h are turned into probabilities,
+// the products form the scores of h + 1 and add the values of h - 1.  Between the two halves of a tile the waves meet: the
+// tile in front is read then, and the next one is there.  No maximum is formed on the way: the reference is the row's
+// maximum over the first half and moves where a half's sum of probabilities tells that one of them passed 2^kSlack.
 template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const ExpandedArgs args,
                                                                            const uint16_t* __restrict__ q,
                                                                            const char* __restrict__ tiles,
                                                                            uint16_t* __restrict__ out) {
   constexpr int TILE = 32 * WAVES;
-  constexpr int kStages = WAVES == 8 ? 3 : 2;
+  constexpr int kStages = 3;
   constexpr int kLoads = kTileBytes / 1024 / WAVES;  // a wave's, of a tile
-  __shared__ __attribute__((aligned(1024))) char lds[kStages * kTileBytes];
+  constexpr int kZeros = kStages * kTileBytes;       // the values in front of the first half
+  __shared__ __attribute__((aligned(1024))) char lds[kZeros + 32 * kValueBytes];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  for (int n = tid * 16; n < 32 * kValueBytes; n += 64 * WAVES * 16) *reinterpret_cast<u32x4*>(lds + kZeros + n) = u32x4{0, 0, 0, 0};
   const ExpandedTable& t = args.table;
   const int heads = t.heads;
   const int at = blockIdx.x / heads, head = blockIdx.x - at * heads;
@@ -218,26 +232,32 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
   const int keys = rq.cached + row0 + rows;
   const int ntiles = (keys + kTileKeys - 1) / kTileKeys;
   const char* src = tiles + ((int64_t)head * t.key_tiles + rq.unit_start) * kTileBytes + wave * (kLoads * 1024);
+  auto buffer = [&](int tile) { return lds0 + (uint32_t)(tile % kStages) * kTileBytes; };
   auto fetch = [&](int tile) __attribute__((always_inline)) {
     const char* from = src + (int64_t)tile * kTileBytes;
-    const uint32_t to = lds0 + (tile % kStages) * kTileBytes + wave * (kLoads * 1024);
+    const uint32_t to = buffer(tile) + wave * (kLoads * 1024);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) load_to_lds_16(from + j * 1024, (uint32_t)lane * 16, to + j * 1024);
   };
-#pragma unroll
-  for (int a = 0; a < kStages - 1; ++a)
-    if (a < ntiles) fetch(a);
 
   const int i = lane & 31, part = lane >> 5;
   const int row = min(wave * 32 + i, rows - 1);
   const int64_t packed = (int64_t)rq.row_start + row0 + row;
-  constexpr int kSteps = kQueryRow / 16, kBlocks = kLatentValue / 32;
+  constexpr int kSteps = kQueryRow / 16, kBlocks = kLatentValue / 32, kValueProducts = 2 * kBlocks;
   bf16x8 qb[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
     qb[s] = *reinterpret_cast<const bf16x8*>(q + (packed * heads + head) * kQueryRow + s * 16 + part * 8);
+  fetch(0);
+  // (the loop below counts the gathers in flight itself: everything the compiler knows of is waited for here)
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (1 < ntiles) fetch(1);
+  __syncthreads();
   const int visible = rq.cached + row0 + row + 1;
-  const int least = rq.cached + row0 + min(wave * 32, rows - 1) + 1;
+  const int least = rq.cached + row0 + wave * 32 + 1;  // of the wave's first row
+  // halves of which the wave's last row sees a part; none where the wave has no rows
+  const int halves = wave * 32 >= rows ? 0 : (rq.cached + row0 + min(wave * 32 + 31, rows - 1) + 32) / 32;
 
   uint32_t key_at[4], value_at[kBlocks];
 #pragma unroll
@@ -255,83 +275,158 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m_run = kNoReference, l_run = 0.f;
+  f32x16 s0, s1;                  // scores of an even and an odd half
+  u32x4 p0[2], p1[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // and their probabilities, as operands
 
-  auto work_off = [&](int tile, auto masked) __attribute__((always_inline)) {
-    constexpr bool kMasked = decltype(masked)::value;
-    if (kStages == 3 && tile + 1 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tile + kStages - 1 < ntiles) fetch(tile + kStages - 1);
-    const uint32_t buf = lds0 + (tile % kStages) * kTileBytes;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int key0 = tile * kTileKeys + half * 32;
-      f32x16 sc;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = 0.f;
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            *(const LDS_PTR(bf16x8))(uintptr_t)(buf + key_at[s & 3] + (s >> 2) * 128 + half * 32 * kKeyBytes), qb[s], sc, 0, 0, 0);
-      uint32_t unfit = 0;
-      if constexpr (kMasked) {
-        float raw[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) raw[r] = sc[r];
-        unfit = unfit_keys<32>(raw);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key0 + (r >> 2) * 8 + part * 4 + (r & 3) >= visible) sc[r] = -__builtin_inff();
-      }
-      float mx = sc[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-      mx = cross_half_max(mx) * args.scale_log2;
-      if (__any(mx > m_run + kSlack)) {
-        const float m_new = mx > m_run + kSlack ? mx : m_run;
-        const float f = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-        l_run *= f;
-#pragma unroll
-        for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] *= f;
-        m_run = m_new;
-      }
-      u32x4 pb[2];
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const uint32_t two = pack_bf16(__builtin_amdgcn_exp2f(sc[r] * args.scale_log2 - m_run),
-                                       __builtin_amdgcn_exp2f(sc[r + 1] * args.scale_log2 - m_run));
-        pb[r >> 3][(r & 7) >> 1] = two;
-        l_run += __uint_as_float(two << 16) + __uint_as_float(two & 0xFFFF0000u);
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int d = 0; d < kBlocks; ++d) {
-          const uint32_t v = buf + value_at[d] + (half * 32 + k * 16) * kValueBytes;
-          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v));
-          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v + 8 * kValueBytes));
-          bf16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          if constexpr (kMasked)
-            if (unfit) a = without_keys(a, unfit >> (16 * k + 4 * part));
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, pb[k]), o[d], 0, 0, 0);
-        }
-    }
+  // Products of a round: the scores of half `kh` of the tile at `ks` into `sn`, the values of half `vh` of the tile at `vs`
+  // under the probabilities `pv`; beside them the probabilities of the scores `sc` into `pn`, whose sum is returned.
+  constexpr int kProducts = kSteps + kValueProducts, kAhead = 4;
+  auto probability = [&](const f32x16& sc, int e) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(sc[e] * args.scale_log2 - m_run); };
+  auto add_pair = [&](uint32_t two, float sum) __attribute__((always_inline)) {  // of two probabilities as they were rounded
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, sum, false);
   };
-  // Tiles that all rows of the wave see, then those that some see a part of.
-  const int plain = min(ntiles, least / kTileKeys);
-  for (int tile = 0; tile < plain; ++tile) work_off(tile, std::false_type{});
-  for (int tile = plain; tile < ntiles; ++tile) work_off(tile, std::true_type{});
+  auto key_operand = [&](uint32_t ks, int kh, int n) __attribute__((always_inline)) {
+    return *(const LDS_PTR(u32x4))(uintptr_t)(ks + key_at[n & 3] + (n >> 2) * 128 + kh * 32 * kKeyBytes);
+  };
+  auto score_product = [&](u32x4 a, int n, f32x16& sn) __attribute__((always_inline)) {
+    f32x16 from = sn;
+    if (n == 0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) from[r] = 0.f;
+    }
+    sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qb[n], from, 0, 0, 0);
+  };
+  auto round = [&](f32x16& sn, uint32_t ks, int kh, const u32x4 (&pv)[2], uint32_t vs, int vh, const f32x16& sc,
+                   u32x4 (&pn)[2]) __attribute__((always_inline)) -> float {
+    u32x4 staged[kAhead];
+    auto operand = [&](int n) __attribute__((always_inline)) -> u32x4 {
+      if (n < kSteps) return key_operand(ks, kh, n);
+      const int k = (n - kSteps) / kBlocks, d = (n - kSteps) % kBlocks;
+      const uint32_t v = vs + value_at[d] + (vh * 32 + k * 16) * kValueBytes;
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v + 8 * kValueBytes));
+      return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) staged[n] = operand(n);
+    __builtin_amdgcn_sched_barrier(0);
+    float sum = 0.f, pair[2];
+#pragma unroll
+    for (int n = 0; n < kProducts; ++n) {
+      if (n < kSteps) {
+        score_product(staged[n % kAhead], n, sn);
+      } else {
+        const int j = n - kSteps;
+        o[j % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, staged[n % kAhead]),
+                                                                 __builtin_bit_cast(bf16x8, pv[j / kBlocks]), o[j % kBlocks], 0, 0, 0);
+      }
+      if (n + kAhead < kProducts) staged[n % kAhead] = operand(n + kAhead);
+      if (n < 16) {
+        pair[n & 1] = probability(sc, n);
+        if (n & 1) {
+          const uint32_t two = pack_bf16(pair[0], pair[1]);
+          pn[n >> 3][(n & 7) >> 1] = two;
+          sum = add_pair(two, sum);
+          asm volatile("" : "+v"(sum));  // (keeps the step in its place)
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return sum;
+  };
+  auto row_max = [&](const f32x16& sc) __attribute__((always_inline)) {
+    float mx = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    return cross_half_max(mx) * args.scale_log2;
+  };
+  // Half h of the keys, which is half `kh` of the tile at `here`: scores `sc`, probabilities to `pn`.  The round's products
+  // are those of its neighbours, scores of h + 1 and values of h - 1.  Behind the last half there is a round for its values
+  // alone: what it does beside them is for nobody, as are the scores behind the last half.
+  auto half = [&](int h, int kh, uint32_t here, uint32_t ks, uint32_t vs, f32x16& sc, f32x16& sn, u32x4 (&pn)[2],
+                  u32x4 (&po)[2]) __attribute__((always_inline)) {
+    if (h > halves || halves == 0) return;
+    const bool last = h == halves;
+    const int key0 = h * 32;
+    if (!last && key0 + 32 > least) {
+      float raw[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) raw[r] = sc[r];
+      uint32_t unfit = unfit_keys<32>(raw);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (key0 + (r >> 2) * 8 + part * 4 + (r & 3) >= visible) sc[r] = -__builtin_inff();
+      // Their values become zeros where they lie: the weight of a row that sees such a key is no number, so that any wave may
+      // take either.
+      while (unfit) {
+        const int key = kh * 32 + __builtin_ctz(unfit);
+        unfit &= unfit - 1;
+        if (lane < kValueBytes / 16)
+          *(LDS_PTR(u32x4))(uintptr_t)(here + kKeysBytes + key * kValueBytes + lane * 16) = u32x4{0, 0, 0, 0};
+      }
+    }
+    if (h == 0) m_run = fmaxf(row_max(sc), kNoReference);
+    float sum = round(sn, ks, kh ^ 1, po, h == 0 ? lds0 + kZeros - kKeysBytes - (kh ^ 1) * 32 * kValueBytes : vs, kh ^ 1, sc, pn);
+    if (last) return;
+    if (__any(sum >= kOver)) {
+      const float mx = row_max(sc);
+      const float m_new = mx > m_run + kSlack ? mx : m_run;
+      const float f = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= f;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= f;
+      m_run = m_new;
+      sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const uint32_t two = pack_bf16(probability(sc, e), probability(sc, e + 1));
+        pn[e >> 3][(e & 7) >> 1] = two;
+        sum = add_pair(two, sum);
+      }
+    }
+    l_run += sum;
+  };
+
+  if (halves > 0) {
+#pragma unroll
+    for (int n = 0; n < kSteps; ++n) score_product(key_operand(buffer(0), 0, n), n, s0);
+  }
+  for (int tile = 0; tile <= ntiles; ++tile) {
+    const uint32_t here = buffer(tile);
+    // even half: the scores of this tile's other half, the values of the other half of the tile in front
+    half(2 * tile, 0, here, here, buffer(tile + kStages - 1), s0, s1, p0, p1);
+    if (tile == ntiles) break;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tile + 2 < ntiles) fetch(tile + 2);
+    // odd half: the scores of the next tile's first half, the values of this tile's
+    half(2 * tile + 1, 1, here, buffer(tile + 1), here, s1, s0, p1, p0);
+  }
   const float inv = 1.f / cross_half_sum(l_run);
-  if (wave * 32 + i >= rows) return;
   uint16_t* dst = out + (packed * heads + head) * kLatentValue;
+  // the two halves of the wave exchange four columns each, so that a lane writes eight in a row
 #pragma unroll
   for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const u32x2 v = {pack_bf16(o[d][4 * r4] * inv, o[d][4 * r4 + 1] * inv), pack_bf16(o[d][4 * r4 + 2] * inv, o[d][4 * r4 + 3] * inv)};
-      *reinterpret_cast<u32x2*>(dst + d * 32 + r4 * 8 + part * 4) = v;
+    for (int r8 = 0; r8 < 2; ++r8) {
+      u32x2 x[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          x[h][k] = pack_bf16(o[d][r8 * 8 + h * 4 + 2 * k] * inv, o[d][r8 * 8 + h * 4 + 2 * k + 1] * inv);
+      u32x4 words;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const auto both = __builtin_amdgcn_permlane32_swap(x[0][k], x[1][k], false, false);
+        words[k] = both[0];
+        words[2 + k] = both[1];
+      }
+      if (wave * 32 + i < rows) *reinterpret_cast<u32x4*>(dst + d * 32 + r8 * 16 + part * 8) = words;
     }
 }
 
