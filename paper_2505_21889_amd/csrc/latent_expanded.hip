@@ -200,27 +200,35 @@ struct ExpandedArgs {
   float scale_log2;
 };
 
-// blockIdx.x: head (fastest: an XCD meets few heads, whose tiles its workgroups share) and tile of 32 * WAVES query rows,
-// the request's last rows, which see most keys, first.  A wave takes 32 rows.
+// blockIdx.x: head (fastest: an XCD meets few heads, whose tiles its workgroups share) and tile of query rows, the request's
+// last rows, which see most keys, first.  Eight waves of 32 rows each: SETS 8 takes 256 rows; SETS 4 takes 128 and
+// divides the keys, the first halves of the key tiles to four waves and the second ones to the others, which join at the end.
 //
-// The keys are worked off in halves of a tile, three at a time: while the scores of half h are turned into probabilities,
-// the products form the scores of h + 1 and add the values of h - 1.  Between the two halves of a tile the waves meet: the
-// tile in front is read then, and the next one is there.  No maximum is formed on the way: the reference is the row's
-// maximum over the first half and moves where a half's sum of probabilities tells that one of them passed 2^kSlack.
-template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const ExpandedArgs args,
-                                                                           const uint16_t* __restrict__ q,
-                                                                           const char* __restrict__ tiles,
-                                                                           uint16_t* __restrict__ out) {
-  constexpr int TILE = 32 * WAVES;
-  constexpr int kStages = 3;
-  constexpr int kLoads = kTileBytes / 1024 / WAVES;  // a wave's, of a tile
-  constexpr int kZeros = kStages * kTileBytes;       // the values in front of the first half
+// A wave works off its halves three at a time: while the scores of half n are turned into probabilities, the products form the
+// scores of n + 1 and add the values of n - 1.  The waves meet where one of the three enters another tile.  Keys are
+// gathered three tiles ahead and values, which are wanted two halves later, two tiles.  No maximum is formed on the way: the
+// reference is the row's maximum over the first half and moves where a half's sum of probabilities tells that one of
+// them passed 2^kSlack.
+constexpr int kAttendWaves = 8;
+constexpr int kKeyStages = 4, kValueStages = 3;
+constexpr int kValuesAt = kKeyStages * kKeysBytes;                           // in LDS
+constexpr int kZeros = kValuesAt + kValueStages * (kTileBytes - kKeysBytes);  // the values in front of the first half
+
+template <int SETS>
+__global__ __launch_bounds__(64 * kAttendWaves, 2) void expanded_attention_kernel(const ExpandedArgs args,
+                                                                                  const uint16_t* __restrict__ q,
+                                                                                  const char* __restrict__ tiles,
+                                                                                  uint16_t* __restrict__ out) {
+  constexpr int TILE = 32 * SETS;
+  constexpr bool kDivided = SETS < kAttendWaves;
+  constexpr int kKeyLoads = kKeysBytes / 1024 / kAttendWaves, kValueLoads = (kTileBytes - kKeysBytes) / 1024 / kAttendWaves;  // a wave's, of a tile
   __shared__ __attribute__((aligned(1024))) char lds[kZeros + 32 * kValueBytes];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  for (int n = tid * 16; n < 32 * kValueBytes; n += 64 * WAVES * 16) *reinterpret_cast<u32x4*>(lds + kZeros + n) = u32x4{0, 0, 0, 0};
+  const int set = wave % SETS, group = wave / SETS;
+  static_assert(32 * kValueBytes == 64 * kAttendWaves * 16, "a piece of the zeros each");
+  *reinterpret_cast<u32x4*>(lds + kZeros + tid * 16) = u32x4{0, 0, 0, 0};
   const ExpandedTable& t = args.table;
   const int heads = t.heads;
   const int at = blockIdx.x / heads, head = blockIdx.x - at * heads;
@@ -231,33 +239,44 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
   const int rows = min(TILE, rq.new_len - row0);
   const int keys = rq.cached + row0 + rows;
   const int ntiles = (keys + kTileKeys - 1) / kTileKeys;
-  const char* src = tiles + ((int64_t)head * t.key_tiles + rq.unit_start) * kTileBytes + wave * (kLoads * 1024);
-  auto buffer = [&](int tile) { return lds0 + (uint32_t)(tile % kStages) * kTileBytes; };
-  auto fetch = [&](int tile) __attribute__((always_inline)) {
-    const char* from = src + (int64_t)tile * kTileBytes;
-    const uint32_t to = buffer(tile) + wave * (kLoads * 1024);
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) load_to_lds_16(from + j * 1024, (uint32_t)lane * 16, to + j * 1024);
+  const char* src = tiles + ((int64_t)head * t.key_tiles + rq.unit_start) * kTileBytes;
+  // (a tile in front of the first, or behind the last, stands for whatever lies in its place)
+  auto keys_at = [&](int tile) { return lds0 + (uint32_t)(tile & (kKeyStages - 1)) * kKeysBytes; };
+  auto values_of = [&](int tile) {
+    return lds0 + kValuesAt + (uint32_t)((tile + kValueStages) % kValueStages) * (kTileBytes - kKeysBytes);
+  };
+  auto fetch_keys = [&](int tile) __attribute__((always_inline)) {
+    const char* from = src + (int64_t)tile * kTileBytes + wave * (kKeyLoads * 1024);
+    load_to_lds_run<kKeyLoads>(from, (uint32_t)lane * 16, keys_at(tile) + wave * (kKeyLoads * 1024));
+  };
+  auto fetch_values = [&](int tile) __attribute__((always_inline)) {
+    const char* from = src + (int64_t)tile * kTileBytes + kKeysBytes + wave * (kValueLoads * 1024);
+    load_to_lds_run<kValueLoads>(from, (uint32_t)lane * 16, values_of(tile) + wave * (kValueLoads * 1024));
   };
 
   const int i = lane & 31, part = lane >> 5;
-  const int row = min(wave * 32 + i, rows - 1);
+  const int row = min(set * 32 + i, rows - 1);
   const int64_t packed = (int64_t)rq.row_start + row0 + row;
   constexpr int kSteps = kQueryRow / 16, kBlocks = kLatentValue / 32, kValueProducts = 2 * kBlocks;
   bf16x8 qb[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
     qb[s] = *reinterpret_cast<const bf16x8*>(q + (packed * heads + head) * kQueryRow + s * 16 + part * 8);
-  fetch(0);
+  fetch_keys(0);
+  fetch_values(0);
+  if (1 < ntiles) fetch_keys(1);
   // (the loop below counts the gathers in flight itself: everything the compiler knows of is waited for here)
   __builtin_amdgcn_s_waitcnt(0x0F70);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (1 < ntiles) fetch(1);
+  if (!kDivided && 1 < ntiles) fetch_values(1);
+  if (2 < ntiles) fetch_keys(2);
+  if (3 < ntiles) fetch_keys(3);
   __syncthreads();
   const int visible = rq.cached + row0 + row + 1;
-  const int least = rq.cached + row0 + wave * 32 + 1;  // of the wave's first row
-  // halves of which the wave's last row sees a part; none where the wave has no rows
-  const int halves = wave * 32 >= rows ? 0 : (rq.cached + row0 + min(wave * 32 + 31, rows - 1) + 32) / 32;
+  const int least = rq.cached + row0 + set * 32 + 1;  // of the wave's first row
+  // halves of which the wave's last row sees a part, counted in its own; none where the wave has no rows
+  const int seen = set * 32 >= rows ? 0 : (rq.cached + row0 + min(set * 32 + 31, rows - 1) + 32) / 32;
+  const int halves = kDivided ? (seen + 1 - group) / 2 : seen;
 
   uint32_t key_at[4], value_at[kBlocks];
 #pragma unroll
@@ -267,7 +286,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
     const int key = (blk >> 1) * 4 + (w16 >> 2), chunk = 2 * (blk & 1) + ((w16 & 3) >> 1);
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d)
-      value_at[d] = kKeysBytes + key * kValueBytes + (((4 * d + chunk) ^ value_swizzle(key)) << 4) + (w16 & 1) * 8;
+      value_at[d] = key * kValueBytes + (((4 * d + chunk) ^ value_swizzle(key)) << 4) + (w16 & 1) * 8;
   }
   f32x16 o[kBlocks];
 #pragma unroll
@@ -278,8 +297,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
   f32x16 s0, s1;                  // scores of an even and an odd half
   u32x4 p0[2], p1[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // and their probabilities, as operands
 
-  // Products of a round: the scores of half `kh` of the tile at `ks` into `sn`, the values of half `vh` of the tile at `vs`
-  // under the probabilities `pv`; beside them the probabilities of the scores `sc` into `pn`, whose sum is returned.
+  // Products of a round: the scores of the 32 keys at `ks` into `sn`, the values of the 32 keys at `vs` under the
+  // probabilities `pv`; beside them the probabilities of the scores `sc` into `pn`, whose sum is returned.
   constexpr int kProducts = kSteps + kValueProducts, kAhead = 4;
   auto probability = [&](const f32x16& sc, int e) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(sc[e] * args.scale_log2 - m_run); };
   auto add_pair = [&](uint32_t two, float sum) __attribute__((always_inline)) {  // of two probabilities as they were rounded
@@ -287,8 +306,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, sum, false);
   };
-  auto key_operand = [&](uint32_t ks, int kh, int n) __attribute__((always_inline)) {
-    return *(const LDS_PTR(u32x4))(uintptr_t)(ks + key_at[n & 3] + (n >> 2) * 128 + kh * 32 * kKeyBytes);
+  auto key_operand = [&](uint32_t ks, int n) __attribute__((always_inline)) {
+    return *(const LDS_PTR(u32x4))(uintptr_t)(ks + key_at[n & 3] + (n >> 2) * 128);
   };
   auto score_product = [&](u32x4 a, int n, f32x16& sn) __attribute__((always_inline)) {
     f32x16 from = sn;
@@ -298,13 +317,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
     }
     sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qb[n], from, 0, 0, 0);
   };
-  auto round = [&](f32x16& sn, uint32_t ks, int kh, const u32x4 (&pv)[2], uint32_t vs, int vh, const f32x16& sc,
-                   u32x4 (&pn)[2]) __attribute__((always_inline)) -> float {
+  auto round = [&](f32x16& sn, uint32_t ks, const u32x4 (&pv)[2], uint32_t vs, const f32x16& sc, u32x4 (&pn)[2]) __attribute__((always_inline)) -> float {
     u32x4 staged[kAhead];
     auto operand = [&](int n) __attribute__((always_inline)) -> u32x4 {
-      if (n < kSteps) return key_operand(ks, kh, n);
+      if (n < kSteps) return key_operand(ks, n);
       const int k = (n - kSteps) / kBlocks, d = (n - kSteps) % kBlocks;
-      const uint32_t v = vs + value_at[d] + (vh * 32 + k * 16) * kValueBytes;
+      const uint32_t v = vs + value_at[d] + k * 16 * kValueBytes;
       const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v));
       const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v + 8 * kValueBytes));
       return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -342,14 +360,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
     return cross_half_max(mx) * args.scale_log2;
   };
-  // Half h of the keys, which is half `kh` of the tile at `here`: scores `sc`, probabilities to `pn`.  The round's products
-  // are those of its neighbours, scores of h + 1 and values of h - 1.  Behind the last half there is a round for its values
-  // alone: what it does beside them is for nobody, as are the scores behind the last half.
-  auto half = [&](int h, int kh, uint32_t here, uint32_t ks, uint32_t vs, f32x16& sc, f32x16& sn, u32x4 (&pn)[2],
-                  u32x4 (&po)[2]) __attribute__((always_inline)) {
-    if (h > halves || halves == 0) return;
-    const bool last = h == halves;
-    const int key0 = h * 32;
+  // The waves meet in front of the round that enters key tile `next`: it is there then, as are the values of the tile
+  // `kLate` tiles in front of it, and what the rounds so far read is free for those further on.
+  constexpr int kLate = kDivided ? 2 : 1;
+  auto meet = [&](int next) __attribute__((always_inline)) {
+    // (in flight may be what the meeting in front sent for: keys three tiles on, values)
+    if (next + 2 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kKeyLoads + kValueLoads) : "memory");
+    else if (next + 1 - kLate < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kValueLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (next + 3 < ntiles) fetch_keys(next + 3);
+    if (next + 2 - kLate < ntiles) fetch_values(next + 2 - kLate);
+  };
+
+  // The wave's n-th half: scores `sc`, probabilities to `pn`.  The round's products are those of its neighbours.  Behind the
+  // last half there is a round for its values alone: what it does beside them is for nobody, as are the scores behind
+  // the last half.
+  auto tile_of = [&](int n) { return kDivided ? n : n >> 1; };
+  auto half_of = [&](int n) { return kDivided ? group : n & 1; };
+  auto half = [&](int n, f32x16& sc, f32x16& sn, u32x4 (&pn)[2], u32x4 (&po)[2]) __attribute__((always_inline)) {
+    if (n > halves || halves == 0) return;
+    const bool last = n == halves;
+    const int key0 = tile_of(n) * kTileKeys + half_of(n) * 32;
     if (!last && key0 + 32 > least) {
       float raw[16];
 #pragma unroll
@@ -361,14 +393,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
       // Their values become zeros where they lie: the weight of a row that sees such a key is no number, so that any wave may
       // take either.
       while (unfit) {
-        const int key = kh * 32 + __builtin_ctz(unfit);
+        const int key = half_of(n) * 32 + __builtin_ctz(unfit);
         unfit &= unfit - 1;
         if (lane < kValueBytes / 16)
-          *(LDS_PTR(u32x4))(uintptr_t)(here + kKeysBytes + key * kValueBytes + lane * 16) = u32x4{0, 0, 0, 0};
+          *(LDS_PTR(u32x4))(uintptr_t)(values_of(tile_of(n)) + key * kValueBytes + lane * 16) = u32x4{0, 0, 0, 0};
       }
     }
-    if (h == 0) m_run = fmaxf(row_max(sc), kNoReference);
-    float sum = round(sn, ks, kh ^ 1, po, h == 0 ? lds0 + kZeros - kKeysBytes - (kh ^ 1) * 32 * kValueBytes : vs, kh ^ 1, sc, pn);
+    if (n == 0) m_run = fmaxf(row_max(sc), kNoReference);
+    const uint32_t front = n == 0 ? lds0 + kZeros : values_of(tile_of(n - 1)) + half_of(n - 1) * 32 * kValueBytes;
+    float sum = round(sn, keys_at(tile_of(n + 1)) + half_of(n + 1) * 32 * kKeyBytes, po, front, sc, pn);
     if (last) return;
     if (__any(sum >= kOver)) {
       const float mx = row_max(sc);
@@ -390,23 +423,54 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
     }
     l_run += sum;
   };
-
   if (halves > 0) {
 #pragma unroll
-    for (int n = 0; n < kSteps; ++n) score_product(key_operand(buffer(0), 0, n), n, s0);
+    for (int n = 0; n < kSteps; ++n) score_product(key_operand(keys_at(0) + half_of(0) * 32 * kKeyBytes, n), n, s0);
   }
-  for (int tile = 0; tile <= ntiles; ++tile) {
-    const uint32_t here = buffer(tile);
-    // even half: the scores of this tile's other half, the values of the other half of the tile in front
-    half(2 * tile, 0, here, here, buffer(tile + kStages - 1), s0, s1, p0, p1);
-    if (tile == ntiles) break;
+  if constexpr (kDivided) {
+    for (int n = 0; n <= ntiles; n += 2) {
+      meet(n + 1);
+      half(n, s0, s1, p0, p1);
+      if (n + 1 > ntiles) break;
+      meet(n + 2);
+      half(n + 1, s1, s0, p1, p0);
+    }
+  } else {
+    for (int tile = 0; tile <= ntiles; ++tile) {
+      half(2 * tile, s0, s1, p0, p1);
+      if (tile == ntiles) break;
+      meet(tile + 1);
+      half(2 * tile + 1, s1, s0, p1, p0);
+    }
+  }
+  l_run = cross_half_sum(l_run);
+  if constexpr (kDivided) {
+    // join: the second four waves leave their outputs, references and sums, a row to a lane, the first four add them
+    constexpr int kPitch = 33;  // words of a lane's 32 and one, so that the lanes' words take all banks
+    float* const left = reinterpret_cast<float*>(lds) + set * (64 * kPitch * 2 + 2 * 64);
+    static_assert(SETS * (64 * kPitch * 2 + 2 * 64) * 4 <= kZeros, "the join takes the tiles' place");
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tile + 2 < ntiles) fetch(tile + 2);
-    // odd half: the scores of the next tile's first half, the values of this tile's
-    half(2 * tile + 1, 1, here, buffer(tile + 1), here, s1, s0, p1, p0);
+    if (group == 1) {
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) left[(d >> 1) * 64 * kPitch + lane * kPitch + (d & 1) * 16 + r] = o[d][r];
+      left[64 * kPitch * 2 + lane] = m_run;
+      left[64 * kPitch * 2 + 64 + lane] = l_run;
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float m_other = left[64 * kPitch * 2 + lane], l_other = left[64 * kPitch * 2 + 64 + lane];
+    const float m = fmaxf(m_run, m_other);
+    const float f = __builtin_amdgcn_exp2f(m_run - m), f_other = __builtin_amdgcn_exp2f(m_other - m);
+    l_run = l_run * f + l_other * f_other;
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * f + left[(d >> 1) * 64 * kPitch + lane * kPitch + (d & 1) * 16 + r] * f_other;
   }
-  const float inv = 1.f / cross_half_sum(l_run);
+  const float inv = 1.f / l_run;
   uint16_t* dst = out + (packed * heads + head) * kLatentValue;
   // the two halves of the wave exchange four columns each, so that a lane writes eight in a row
 #pragma unroll
@@ -426,7 +490,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void expanded_attention_kernel(const
         words[k] = both[0];
         words[2 + k] = both[1];
       }
-      if (wave * 32 + i < rows) *reinterpret_cast<u32x4*>(dst + d * 32 + r8 * 16 + part * 8) = words;
+      if (set * 32 + i < rows) *reinterpret_cast<u32x4*>(dst + d * 32 + r8 * 16 + part * 8) = words;
     }
 }
 
@@ -455,7 +519,7 @@ int latent_attention_expanded(const efim_batch_t* b, const void* q, const void* 
       expanded_attention_kernel<8><<<(unsigned)args.table.row_tiles * heads, 512, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
                                                                                     static_cast<uint16_t*>(out));
     else
-      expanded_attention_kernel<4><<<(unsigned)args.table.row_tiles * heads, 256, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
+      expanded_attention_kernel<4><<<(unsigned)args.table.row_tiles * heads, 512, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
                                                                                     static_cast<uint16_t*>(out));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }
