@@ -76,16 +76,31 @@ __device__ __forceinline__ float scale_accumulator(float x, float f) {
   return x;
 }
 
-// The request that a unit lies in.
-__device__ __forceinline__ int find_request(const LatentTable& t, int64_t unit, int lane) {
-  int r = -1;
+// The requests of a launch, a lane each (two for each lane), asked for at once: what a unit's request is follows without
+// another load.
+struct Requests {
+  LatentReq held[kLatentTableReqs / 64];
+  int nreq;
+  __device__ __forceinline__ Requests(const LatentTable& t, int lane) : nreq(t.nreq) {
 #pragma unroll
-  for (int i = 0; i < kLatentTableReqs / 64; ++i) {
-    const int at = i * 64 + lane;
-    r += __popcll(__ballot(at < t.nreq && t.req[min(at, t.nreq - 1)].unit_start <= unit));
+    for (int i = 0; i < kLatentTableReqs / 64; ++i) held[i] = t.req[min(i * 64 + lane, t.nreq - 1)];
   }
-  return __builtin_amdgcn_readfirstlane(r);
-}
+  __device__ __forceinline__ int find(int64_t unit, int lane) const {
+    int r = -1;
+#pragma unroll
+    for (int i = 0; i < kLatentTableReqs / 64; ++i) r += __popcll(__ballot(i * 64 + lane < nreq && held[i].unit_start <= unit));
+    return __builtin_amdgcn_readfirstlane(r);
+  }
+  __device__ __forceinline__ LatentReq get(int r) const {
+    static_assert(kLatentTableReqs == 128, "two requests to a lane");
+    const bool upper = r >= 64;
+    auto of = [&](int low, int high) { return __builtin_amdgcn_readlane(upper ? high : low, r & 63); };
+    const uint32_t first = (uint32_t)of((int)held[0].unit_start, (int)held[1].unit_start);
+    const uint32_t rest = (uint32_t)of((int)(held[0].unit_start >> 32), (int)(held[1].unit_start >> 32));
+    return LatentReq{(int64_t)((uint64_t)rest << 32 | first), of(held[0].req, held[1].req), of(held[0].cached, held[1].cached),
+                     of(held[0].new_len, held[1].new_len), of(held[0].row_start, held[1].row_start)};
+  }
+};
 
 // The tile that a unit lies in, by the whole wave: 64 tiles of the request at a time.
 struct Place {
@@ -95,10 +110,10 @@ struct Place {
   int64_t first;   // unit of the launch at which the tile begins
 };
 template <int TILE>
-__device__ __forceinline__ Place find_tile(const LatentTable& t, int64_t unit, int lane) {
+__device__ __forceinline__ Place find_tile(const LatentTable& t, const Requests& requests, int64_t unit, int lane) {
   Place at;
-  at.r = find_request(t, unit, lane);
-  const LatentReq& q = t.req[at.r];
+  at.r = requests.find(unit, lane);
+  const LatentReq q = requests.get(at.r);
   at.first = q.unit_start;
   at.tile = 0;
   at.units = latent_units_of(q, t.heads, TILE, 0);
@@ -141,19 +156,20 @@ struct Share {
   int64_t packed;      // packed query row of the tile's first row
 
   __device__ __forceinline__ Share(const LatentTable& table, int lane) : t(table) {
+    const Requests requests(table, lane);
     // an XCD takes neighbouring shares, which have rows of the cache in common
     group = (int)(blockIdx.x % kXcds) * (int)(gridDim.x / kXcds) + (int)(blockIdx.x / kXcds);
     next = end = 0;
     if (group >= t.groups) return;
     next = t.first_unit(group);
     end = t.first_unit(group + 1);
-    at = find_tile<TILE>(t, next, lane);
+    at = find_tile<TILE>(t, requests, next, lane);
     first = true;
+    rq = requests.get(at.r);
     part();
   }
   __device__ __forceinline__ bool done() const { return next >= end; }
   __device__ __forceinline__ void part() {
-    rq = t.req[at.r];
     row0 = at.tile * TILE;
     rows = latent_rows_of(rq, t.heads, TILE, at.tile);
     const int u0 = (int)(next - at.first), u1 = (int)min((int64_t)at.units, end - at.first);
@@ -169,10 +185,10 @@ struct Share {
     at.first = next;
     ++at.tile;
     if (at.tile == latent_tiles(rq, t.heads, TILE)) {
-      ++at.r;
+      rq = t.req[++at.r];
       at.tile = 0;
     }
-    at.units = latent_units_of(t.req[at.r], t.heads, TILE, at.tile);
+    at.units = latent_units_of(rq, t.heads, TILE, at.tile);
     part();
   }
 };
@@ -186,9 +202,12 @@ struct Gather {
 
   __device__ __forceinline__ Gather(const uint16_t* rows, int end, int shift, int lane)
       : cache(reinterpret_cast<const char*>(rows)), k1(end), page_shift(shift), page_mask((1 << shift) - 1), swizzles(0), lane16(lane * 16) {
+    asm volatile("" : "+v"(lane));  // (formed where it is used: offsets held from part to part were spilled)
 #pragma unroll
     for (int j = 0; j < kGroupLoads; ++j) swizzles |= (uint32_t)(swizzle((j * 64 + lane) / kRowChunks) >> 1) << (2 * j);
   }
+  // (formed again for every tile, as the operands' addresses are)
+  __device__ __forceinline__ void forget() { asm volatile("" : "+v"(swizzles), "+v"(lane16)); }
   // byte offset of load j in a group (its multiple of 1 KB aside) whose tile row divided by eight is even or odd
   __device__ __forceinline__ uint32_t offset(int j, int odd) const { return lane16 ^ (((swizzles >> (2 * j)) & 3) << 5) ^ (odd << 4); }
   __device__ __forceinline__ const char* row_at(int32_t page, int key) const {
@@ -362,28 +381,24 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, f16x2));
 }
 
-// Writes a wave's 32 rows of outputs times `factor`: column d * 32 + r / 4 * 8 + part * 4 + r % 4 is element r of block d.  The two
-// halves of a wave exchange four columns each, so that a lane writes eight in a row.
+// Writes a wave's rows of outputs times `factor`: column d * 32 + r / 4 * 8 + part * 4 + r % 4 is element r of block d.  They go
+// through the wave's LDS at `staged` and out a row at a time; written from where they are, 32 bytes of each of 32 rows
+// at a time, they took 43 cycles a store.
+constexpr int kStagedPitch = kLatentRank * 2 + 16;  // so that sixteen rows' equal chunks take all banks
+static_assert(32 * kStagedPitch <= kTileBytes, "a wave's rows take a tile's place");
 template <typename Pack>
-__device__ __forceinline__ void write_row(const f32x16 (&o)[16], uint16_t* to, float factor, int part, bool in_range, Pack pack) {
+__device__ __forceinline__ void write_rows(const f32x16 (&o)[16], char* staged, uint16_t* to, float factor, int lane, int rows, Pack pack) {
+  const int i = lane & 31, part = lane >> 5;
 #pragma unroll
   for (int d = 0; d < 16; ++d)
 #pragma unroll
-    for (int r8 = 0; r8 < 2; ++r8) {
-      u32x2 x[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) x[h][k] = pack(o[d][r8 * 8 + h * 4 + 2 * k] * factor, o[d][r8 * 8 + h * 4 + 2 * k + 1] * factor);
-      u32x4 words;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const auto both = __builtin_amdgcn_permlane32_swap(x[0][k], x[1][k], false, false);
-        words[k] = both[0];
-        words[2 + k] = both[1];
-      }
-      if (in_range) *reinterpret_cast<u32x4*>(to + d * 32 + r8 * 16 + part * 8) = words;
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const u32x2 words = {pack(o[d][4 * r4] * factor, o[d][4 * r4 + 1] * factor), pack(o[d][4 * r4 + 2] * factor, o[d][4 * r4 + 3] * factor)};
+      *reinterpret_cast<u32x2*>(staged + i * kStagedPitch + (d * 32 + r4 * 8 + part * 4) * 2) = words;
     }
+#pragma unroll 8
+  for (int row = 0; row < rows; ++row)
+    *reinterpret_cast<u32x4*>(to + (int64_t)row * kLatentRank + lane * 8) = *reinterpret_cast<const u32x4*>(staged + row * kStagedPitch + lane * 16);
 }
 
 // Tiles of 128 query rows: a wave takes 32 of them and the four share the key tiles, three ahead.  One wave runs on a SIMD (256
@@ -413,28 +428,38 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
   for (Share<TILE> it(args.table, lane); !it.done(); it.advance()) {
     const int32_t* pages = block_table + (int64_t)it.rq.req * args.table.max_pages;
     const int ntiles = (it.k1 - it.k0 + kTileKeys - 1) / kTileKeys;
-    // the wave's queries as operands; rows behind the tile's last are copies of it
     const int i = lane & 31, part = lane >> 5;
     const int row = min(wave * 32 + i, it.rows - 1);
-    const uint16_t* q_row = q + (it.packed + row) * kLatentRow + part * 8;
-    bf16x8 qb[Op::kSteps];
+    // The wave's queries, through a tile's place: read from memory as operands, 16 bytes of each of 32 rows at a time, they
+    // took 55 cycles a load.  Rows behind the tile's last are copies of it.
+    const Gather queries(q + it.packed * kLatentRow, it.rows, 30, lane);
 #pragma unroll
-    for (int s = 0; s < Op::kSteps; ++s) qb[s] = *reinterpret_cast<const bf16x8*>(q_row + s * 16);
-    // the wave gathers a quarter of each tile; lane t holds the page of its rows in tile held_from + t
-    const Gather gather(cache, it.k1, page_shift, lane);
+    for (int g = 0; g < kGroups; ++g)
+      queries.group(wave * 32 + g * kGroupKeys, g, 0, lds0 + wave * kTileBytes + g * kGroupBytes);
+    // the wave gathers a quarter of each key tile; lane t holds the page of its rows in tile held_from + t
+    Gather gather(cache, it.k1, page_shift, lane);
     auto key_of = [&](int tile) { return it.k0 + tile * kTileKeys + wave * kGroupKeys; };
     auto pages_from = [&](int tile) { return pages[min(key_of(tile + lane), it.k1 - 1) >> page_shift]; };
     int held_from = 0;
     int32_t held = pages_from(0);
     auto page_of = [&](int tile) { return __builtin_amdgcn_readlane(held, tile - held_from); };
     auto buffer = [&](int tile) { return lds0 + (tile & (kWaves - 1)) * kTileBytes; };
-    gather.group(key_of(0), wave, page_of(0), buffer(0) + wave * kGroupBytes);
-    // (the loop below counts the gathers in flight itself: everything the compiler knows of is waited for here)
+    // (the gathers in flight are counted here: everything the compiler knows of is waited for)
     __builtin_amdgcn_s_waitcnt(0x0F70);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bf16x8 qb[Op::kSteps];
+    {
+      const Keys<32> rows(op, lds0 + wave * kTileBytes);
 #pragma unroll
-    for (int a = 1; a < kWaves - 1; ++a)
+      for (int s = 0; s < Op::kSteps; ++s) qb[s] = rows.read(s);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < kWaves - 1; ++a)
       if (a < ntiles) gather.group(key_of(a), wave, page_of(a), buffer(a) + wave * kGroupBytes);
+    if (ntiles > 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kGroupLoads) : "memory");
+    else if (ntiles > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kGroupLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 
     const int visible = it.rq.cached + (it.row0 + row) / heads + 1;
@@ -478,6 +503,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
           else gather.group(key, wave, page_of(next), to);
         }
         op.forget();
+        gather.forget();
         const Keys<32> keys(op, buffer(tile));
         constexpr int kLast = Op::kKeyProducts;
         sc = score_products<kAhead, kLast>(
@@ -565,7 +591,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
     }
     l_run = cross_half_sum(l_run);
 
-    const int tile_row = wave * 32 + i;
+    __syncthreads();  // every wave is done with the part's tiles
+    const int mine = max(0, min(32, it.rows - wave * 32));
+    char* const staged = lds + wave * kTileBytes;
     if (it.slot >= 0) {
       float top = 0.f;
 #pragma unroll
@@ -573,15 +601,16 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(o[d][r]));
       top = cross_half_max(top);
-      const int64_t at = (int64_t)it.slot * TILE + tile_row;
-      if (tile_row < it.rows && part == 0) *reinterpret_cast<f32x4*>(args.part_ml + at * 4) = f32x4{m_run, l_run, top * kPartScale, 0.f};
-      write_row(o, args.part_o + at * kLatentRank, top > 0.f ? 1.f / (top * kPartScale) : 0.f, part, tile_row < it.rows,
-                [](float a, float b) { return pack_f16(a, b); });
+      const int64_t at = (int64_t)it.slot * TILE + wave * 32;
+      if (i < mine && part == 0) *reinterpret_cast<f32x4*>(args.part_ml + (at + i) * 4) = f32x4{m_run, l_run, top * kPartScale, 0.f};
+      write_rows(o, staged, args.part_o + at * kLatentRank, top > 0.f ? 1.f / (top * kPartScale) : 0.f, lane, mine,
+                 [](float a, float b) { return pack_f16(a, b); });
     } else {
-      write_row(o, out + (it.packed + tile_row) * kLatentRank, 1.f / l_run, part, tile_row < it.rows,
-                [](float a, float b) { return pack_bf16(a, b); });
+      write_rows(o, staged, out + (it.packed + wave * 32) * kLatentRank, 1.f / l_run, lane, mine,
+                 [](float a, float b) { return pack_bf16(a, b); });
     }
-    __syncthreads();  // every wave is done with the part's tiles
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's place is read
+    __syncthreads();
   }
 }
 
@@ -801,9 +830,10 @@ __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args,
   const int lane = threadIdx.x & 63;
   const int group = blockIdx.y + 1;
   const int64_t cut = t.first_unit(group);
-  const Place at = find_tile<TILE>(t, cut, lane);
+  const Requests requests(t, lane);
+  const Place at = find_tile<TILE>(t, requests, cut, lane);
   if (cut == at.first || t.first_unit(group - 1) > at.first) return;
-  const LatentReq q = t.req[at.r];
+  const LatentReq q = requests.get(at.r);
   const int rows = latent_rows_of(q, t.heads, TILE, at.tile);
   int parts = 2;
   while (group - 1 + parts < t.groups && t.first_unit(group - 1 + parts) < at.first + at.units) ++parts;
