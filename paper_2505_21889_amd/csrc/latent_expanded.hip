@@ -8,11 +8,14 @@
 // as the second one's LDS tiles: of 64 keys and a head, 24 KB of keys and 16 KB of values, chunks swizzled, so that the
 // second gathers a tile with plain 1 KB loads.  The second is the attention, 32 query rows to a wave: scores and values as in the
 // absorbed form, sums fp32, expanded keys, values and probabilities bf16 (as the weight and the latents are).
+// 12 prompts of 20k new tokens, 26k keys and 32 heads: 225 us (214 GFLOP, 523 MB written) and 600 us (536 GFLOP that count).
 #include <cstddef>
 #include <type_traits>
+#include <utility>
 
 #include "efim_internal.h"
 #include "latent_plan.h"
+#include "latent_device.h"
 #include "rope_math.h"
 #include "wave_ops.h"
 
@@ -45,152 +48,259 @@ constexpr float kNoReference = -3.0e38f;
 __device__ __forceinline__ int key_swizzle(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int value_swizzle(int row) { return (row & 3) << 2; }
 
-// The request that a tile of keys, or of query rows, lies in.
-template <bool KEYS>
-__device__ __forceinline__ int find_request(const ExpandedTable& t, int tile, int lane) {
-  int r = -1;
-#pragma unroll
-  for (int i = 0; i < kLatentTableReqs / 64; ++i) {
-    const int k = min(i * 64 + lane, t.nreq - 1);
-    r += __popcll(__ballot(i * 64 + lane < t.nreq && (KEYS ? (int)t.req[k].unit_start : t.row_tile_start[k]) <= tile));
-  }
-  return __builtin_amdgcn_readfirstlane(r);
-}
-
 // --- expansion -----------------------------------------------------------------------------------------------------------
 
-constexpr int kTokens = 2 * kTileKeys;  // of a workgroup: two tiles
-constexpr int kDepth = 32;              // elements of the latent staged at a time
-constexpr int kDepthBytes = kDepth * 2;
-constexpr int kStageBytes = (kTokens + kHeadOut) * kDepthBytes;
+constexpr int kUnitKeys = 32;                             // half a tile
+constexpr int kLatentBytes = kLatentRank * 2;
+constexpr int kStageBytes = kUnitKeys * kRowBytes;        // rows of the cache, as the absorbed form's tiles have them
 constexpr int kStageCount = 3;
-constexpr int kExpandWaves = 4;
+constexpr int kExpandWaves = 8, kWaveOuts = kHeadOut / kExpandWaves;
+constexpr int kPlacePitch = kWaveOuts * 2 + 16;           // of a wave's outputs on their way out
+constexpr int kPlacesAt = kStageCount * kStageBytes;
+constexpr int kWeightBytes = kWaveOuts * kLatentBytes / 2;  // half of a wave's weight on its way in
+constexpr int kExpandLds = kPlacesAt + kExpandWaves * kUnitKeys * kPlacePitch;
+static_assert(kExpandWaves * kWeightBytes <= kExpandLds && kLatentBytes == 1024 && kWaveOuts == 32, "sizes");
+static_assert(kExpandWaves / 2 * kGroupKeys == kUnitKeys, "two waves gather a group");
 
-// Swizzle of a staged row's four 16-byte chunks: sixteen rows' equal chunks take the sixteen places of the bank line.
-__device__ __forceinline__ int stage_swizzle(int row) { return (row >> 2) & 3; }
+// f(0), f(1), .. with the number as a type: a loop of so long a body is not unrolled.
+template <int... N, typename F>
+__device__ __forceinline__ void each(std::integer_sequence<int, N...>, F f) {
+  (f(std::integral_constant<int, N>()), ...);
+}
+template <int COUNT, typename F>
+__device__ __forceinline__ void each(F f) {
+  each(std::make_integer_sequence<int, COUNT>(), f);
+}
 
-// blockIdx.x: head (fastest, so that an XCD meets few heads' weights) and pair of tiles.  A wave forms 64 tokens x 128
-// outputs as W C^T: a lane's results are four neighbouring outputs of one token, and an operand of either side serves two or
-// four products.  Two workgroups share a unit, so that one multiplies while the other writes its tiles; the loads are two
-// stages ahead.
+// The compiler gives such products accumulation registers, which the weight takes, and counts no states behind written-out ones.
+__device__ __forceinline__ void first_expand_product(f32x16& acc, bf16x8 weight, bf16x8 token) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "a"(weight), "v"(token));
+}
+__device__ __forceinline__ void expand_product(f32x16& acc, bf16x8 weight, bf16x8 token) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "a"(weight), "v"(token));
+}
+
+// blockIdx.x: head and slice of the launch's keys.  A workgroup keeps the head's whole weight in registers, 32 of its 256 rows
+// in each of eight waves, and the slice's latents pass by in LDS, 32 at a time: so a latent is fetched once a head.  A wave's
+// results W C^T are, a lane, four neighbouring outputs of one token; beside the products of a unit those of the unit in front
+// go out through LDS, in runs of 64 bytes, and the gather of the unit two further on.  Without the gathers and the stores the
+// products take 160 us of the 225 above, alone 110.  (Four waves of 64 rows, for which an operand read from LDS serves
+// two products, measured the same; tiles of 128 tokens and 256 outputs with the weight in LDS, 2.5 GB gathered, 290 us.)
 __global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const ExpandedTable t, const uint16_t* __restrict__ cache,
                                                                       const uint16_t* __restrict__ w_kv,
                                                                       const int32_t* __restrict__ block_table,
                                                                       char* __restrict__ tiles) {
-  constexpr int kLdsBytes = 2 * kTileBytes;
-  static_assert(kStageCount * kStageBytes <= kLdsBytes, "the finished tiles take the stages' place");
-  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
+  __shared__ __attribute__((aligned(1024))) char lds[kExpandLds];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int pair = blockIdx.x / t.heads, head = blockIdx.x - pair * t.heads;
-  const LatentReq rq = t.req[find_request<true>(t, 2 * pair, lane)];
-  const int keys = rq.cached + rq.new_len;
-  const int key0 = (2 * pair - (int)rq.unit_start) * kTileKeys;  // first token of the pair
-  const int32_t* pages = block_table + (int64_t)rq.req * t.max_pages;
-  const int page_shift = t.page_shift, page_mask = (1 << page_shift) - 1;
-  const char* w = reinterpret_cast<const char*>(w_kv) + (int64_t)head * kHeadOut * kLatentRank * 2;
-  // Tokens behind the request's last are copies of it (their scores are masked).
-  auto token_row = [&](int token) {
-    const int key = min(key0 + token, keys - 1);
-    const int64_t page = pages[key >> page_shift];
-    return reinterpret_cast<const char*>(cache) + ((page << page_shift) + (key & page_mask)) * (kLatentRow * 2);
-  };
-
-  // 1 KB loads of sixteen rows by 64 bytes, eight of tokens and sixteen of weight rows: two and four a wave; lane l fetches row
-  // l / 4, its chunk l % 4 swizzled.
-  constexpr int kLoadRows = 1024 / kDepthBytes;
-  constexpr int kTokenLoads = kTokens / kLoadRows / kExpandWaves, kWeightLoads = kHeadOut / kLoadRows / kExpandWaves;
-  static_assert(kTokenLoads == 2 && kWeightLoads == 4, "loads of a wave and stage");
-  const char* token_src[kTokenLoads];
-  uint32_t weight_src[kWeightLoads];
-#pragma unroll
-  for (int j = 0; j < kTokenLoads; ++j) {
-    const int row = (wave * kTokenLoads + j) * kLoadRows + (lane >> 2);
-    token_src[j] = token_row(row) + (((lane & 3) ^ stage_swizzle(row)) << 4);
-  }
-#pragma unroll
-  for (int j = 0; j < kWeightLoads; ++j) {
-    const int row = (wave * kWeightLoads + j) * kLoadRows + (lane >> 2);
-    weight_src[j] = (uint32_t)(row * (kLatentRank * 2) + (((lane & 3) ^ stage_swizzle(row)) << 4));
-  }
-  auto stage = [&](int step) { return lds0 + (uint32_t)(step % kStageCount) * kStageBytes; };
-  auto fetch = [&](int step) __attribute__((always_inline)) {
-    const uint32_t to = stage(step);
-#pragma unroll
-    for (int j = 0; j < kTokenLoads; ++j)
-      load_to_lds_16(token_src[j] + step * kDepthBytes, to + (wave * kTokenLoads + j) * 1024);
-#pragma unroll
-    for (int j = 0; j < kWeightLoads; ++j)
-      load_to_lds_16(w + step * kDepthBytes, weight_src[j], to + kTokens * kDepthBytes + (wave * kWeightLoads + j) * 1024);
-  };
-  fetch(0);
-  fetch(1);
-
+  const int head = blockIdx.x / t.slices, slice = blockIdx.x - head * t.slices;
+  const int units = t.key_tiles * (kTileKeys / kUnitKeys);
+  const int begin = (int)((int64_t)units * slice / t.slices), end = (int)((int64_t)units * (slice + 1) / t.slices);
+  if (begin == end) return;
   const int i = lane & 31, part = lane >> 5;
-  const int token_half = wave & 1, out_half = wave >> 1;
-  f32x16 acc[2][4];  // [token block][output block]
+  constexpr int kSteps = kLatentRank / 16;
+  bf16x8 weight[kSteps];
+  {
+    // Through LDS, half of the depth at a time: chunk c of row r lies at c exclusive or the row's low four bits.
+    const char* from = reinterpret_cast<const char*>(w_kv) + ((int64_t)head * kHeadOut + wave * kWaveOuts) * kLatentBytes;
+    const uint32_t place = lds0 + wave * kWeightBytes;
 #pragma unroll
-  for (int a = 0; a < 2; ++a)
+    for (int b = 0; b < 2; ++b) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+      for (int r = 0; r < kWaveOuts; r += 2) {
+        const int row = r + part;
+        load_to_lds_16(from + b * (kLatentBytes / 2), (uint32_t)(row * kLatentBytes + ((i ^ (row & 15)) << 4)), place + r * (kLatentBytes / 2));
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
-  uint32_t at[2];  // of an operand in a staged row
-#pragma unroll
-  for (int s = 0; s < 2; ++s) at[s] = i * kDepthBytes + (((2 * s + part) ^ stage_swizzle(i)) << 4);
-  constexpr int kSteps = kLatentRank / kDepth;
-  for (int step = 0; step < kSteps; ++step) {
-    if (step + 1 < kSteps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kTokenLoads + kWeightLoads) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (step + 2 < kSteps) fetch(step + 2);
-    const uint32_t tok = stage(step) + token_half * 64 * kDepthBytes;
-    const uint32_t wgt = stage(step) + kTokens * kDepthBytes + out_half * 128 * kDepthBytes;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      bf16x8 x[2], y[4];
-#pragma unroll
-      for (int a = 0; a < 2; ++a) x[a] = *(const LDS_PTR(bf16x8))(uintptr_t)(tok + at[s] + a * 32 * kDepthBytes);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) y[b] = *(const LDS_PTR(bf16x8))(uintptr_t)(wgt + at[s] + b * 32 * kDepthBytes);
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int a = 0; a < 2; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[b], x[a], acc[a][b], 0, 0, 0);
+      for (int s = 0; s < kSteps / 2; ++s)
+        weight[b * (kSteps / 2) + s] =
+            *(const LDS_PTR(bf16x8))(uintptr_t)(place + i * (kLatentBytes / 2) + (((2 * (s & 7) + part) ^ (i & 15)) << 4) + (s >> 3) * 256);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
   }
   __syncthreads();
-  // the tiles as the attention takes them, in LDS, then out in whole lines
-  char* const tile = lds + token_half * kTileBytes;
+
+  // Lane l holds where the wave's group of unit held_from + l lies: its row's address, its first key in its request, the request's
+  // keys, the page.  (Keys behind the last become copies of it; their scores are masked.)
+  Gather rows(cache, 0, t.page_shift, lane);
+  // A group's nine loads are shared by two waves: five and four.
+  const int group = wave & 3, first_piece = wave < 4 ? 0 : 5;
+  uint32_t piece_at[5];
 #pragma unroll
-  for (int a = 0; a < 2; ++a)
+  for (int n = 0; n < 5; ++n) piece_at[n] = rows.offset(min(first_piece + n, kGroupLoads - 1), group & 1);
+  int held_from = begin, held_key, held_keys;
+  int32_t held_page;
+  uint64_t held_row;
+  auto look = [&](int from) __attribute__((always_inline)) {
+    const Requests requests(t, lane);  // (seldom wanted: not held meanwhile)
+    const int u = min(from + lane, end - 1);
+    int r = 0;
+    for (int k = 1; k < t.nreq; ++k) r += u >= 2 * (int)requests.get(k).unit_start;
+    auto of = [&](int low, int high) {
+      const int a = __shfl(low, r & 63), b = __shfl(high, r & 63);
+      return r >= 64 ? b : a;
+    };
+    const int start = of((int)requests.held[0].unit_start, (int)requests.held[1].unit_start);
+    const int req = of(requests.held[0].req, requests.held[1].req);
+    held_from = from;
+    held_keys = of(requests.held[0].cached + requests.held[0].new_len, requests.held[1].cached + requests.held[1].new_len);
+    held_key = (u - 2 * start) * kUnitKeys + group * kGroupKeys;
+    held_page = block_table[(int64_t)req * t.max_pages + (min(held_key, held_keys - 1) >> t.page_shift)];
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    held_row = reinterpret_cast<uint64_t>(rows.row_at(held_page, held_key));
+  };
+  // Where unit u's group comes from; one that the request's end cuts off is gathered at once.
+  struct Source {
+    const char* base;
+    bool whole;
+  };
+  auto source = [&](int u, uint32_t to) __attribute__((always_inline)) {
+    Source from = {nullptr, false};
+    if (u < end) {
+      if (u - held_from >= 64) look(u);
+      const int l = u - held_from, key = __builtin_amdgcn_readlane(held_key, l);
+      rows.k1 = __builtin_amdgcn_readlane(held_keys, l);
+      from.whole = rows.whole(key);
+      const uint32_t low = __builtin_amdgcn_readlane((uint32_t)held_row, l), high = __builtin_amdgcn_readlane((uint32_t)(held_row >> 32), l);
+      from.base = reinterpret_cast<const char*>((uint64_t)high << 32 | low) + first_piece * 1024;
+      if (!from.whole && wave < 4) rows.group(key, group, __builtin_amdgcn_readlane(held_page, l), to);
+    }
+    return from;
+  };
+  // the wave's loads of a whole group: two, two and for the first waves one
+  auto gather = [&](const char* base, int n, uint32_t to) __attribute__((always_inline)) {
+    if (n < 4) load_to_lds_2x16(base + n * 1024, piece_at[n], piece_at[n < 4 ? n + 1 : n], to + (first_piece + n) * 1024);
+    else if (wave < 4) load_to_lds_16(base + n * 1024, piece_at[n], to + (first_piece + n) * 1024);
+  };
+  // places of the units u, u + 1 and u + 2, in turn
+  uint32_t now = lds0, next = lds0 + kStageBytes, later = lds0 + 2 * kStageBytes;
+  look(begin);
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+  for (int ahead = 0; ahead < 2; ++ahead) {
+    const uint32_t to = (ahead ? next : now) + group * kGroupBytes;
+    const Source from = source(begin + ahead, to);
+    if (from.whole) {
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const int row = a * 32 + i;
-        const int col = b * 32 + r4 * 8 + part * 4;  // of the keys (out_half 0) or of the values
-        const u32x2 v = {pack_bf16(acc[a][b][4 * r4], acc[a][b][4 * r4 + 1]), pack_bf16(acc[a][b][4 * r4 + 2], acc[a][b][4 * r4 + 3])};
-        char* to = out_half == 0 ? tile + row * kKeyBytes + (((col >> 3) ^ key_swizzle(row)) << 4)
-                                 : tile + kKeysBytes + row * kValueBytes + (((col >> 3) ^ value_swizzle(row)) << 4);
-        *reinterpret_cast<u32x2*>(to + part * 8) = v;
-      }
-  // rotated part of the keys: 8 chunks a token, of the cache
-#pragma unroll
-  for (int j = 0; j < kTokens * 8 / (64 * kExpandWaves); ++j) {
-    const int n = j * 64 * kExpandWaves + tid, token = n >> 3, chunk = n & 7;
-    const u32x4 v = *reinterpret_cast<const u32x4*>(token_row(token) + kLatentRank * 2 + chunk * 16);
-    const int row = token & (kTileKeys - 1);
-    *reinterpret_cast<u32x4*>(lds + (token / kTileKeys) * kTileBytes + row * kKeyBytes + ((16 + (chunk ^ key_swizzle(row))) << 4)) = v;
+      for (int n = 0; n <= 4; n += 2) gather(from.base, n, to);
+    }
   }
+
+  // An operand's address, as the absorbed form's keys have it.
+  uint32_t operand_at[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) operand_at[k] = i * kRowBytes + (((2 * k + part) ^ swizzle(i)) << 4);
+  struct Addresses {
+    uint32_t at[4];
+  };
+  auto addresses = [&](uint32_t from) __attribute__((always_inline)) {
+    Addresses a;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      a.at[k] = from + operand_at[k];
+      asm volatile("" : "+v"(a.at[k]));  // (the steps' offsets then go into the reads)
+    }
+    return a;
+  };
+  auto operand = [&](const Addresses& a, int s) __attribute__((always_inline)) {
+    return *(const LDS_PTR(bf16x8))(uintptr_t)(a.at[s & 3] + (s >> 2) * 128);
+  };
+  // Outputs leave a lane's 16 bytes at a time: row lane / 4 of sixteen, chunk lane % 4 of the wave's, to its place in the tile.
+  // The values' waves bring the rotated parts from a group of rows to the keys too.
+  const uint32_t place = lds0 + kPlacesAt + wave * (kUnitKeys * kPlacePitch);
+  const bool of_keys = wave < 4;
+  const int row16 = lane >> 2, chunk4 = group * 4 + (lane & 3);
+  const uint32_t out_at = of_keys ? row16 * kKeyBytes + ((chunk4 ^ key_swizzle(row16)) << 4)
+                                  : kKeysBytes + row16 * kValueBytes + ((chunk4 ^ value_swizzle(row16)) << 4);
+  // (the row sixteen further on has the same swizzle)
+  const uint32_t store_at[2] = {out_at, out_at + 16u * (of_keys ? kKeyBytes : kValueBytes)};
+  const int rope_row = group * kGroupKeys + (lane >> 3), rope_chunk = lane & 7;
+  const uint32_t rope_from = rope_row * kRowBytes + kLatentBytes + ((rope_chunk ^ swizzle(rope_row)) << 4);
+  const uint32_t rope_at = rope_row * kKeyBytes + ((16 + (rope_chunk ^ key_swizzle(rope_row))) << 4);
+  char* const head_tiles = tiles + (int64_t)head * t.key_tiles * kTileBytes;
+  auto tile_of = [&](int u) { return head_tiles + (int64_t)(u >> 1) * kTileBytes; };
+  const int half_bytes = kUnitKeys * (of_keys ? kKeyBytes : kValueBytes);
+  auto write_place = [&](u32x2 words, int r4) __attribute__((always_inline)) {
+    *(LDS_PTR(u32x2))(uintptr_t)(place + i * kPlacePitch + (r4 * 8 + part * 4) * 2) = words;
+  };
+  auto read_place = [&](int k) __attribute__((always_inline)) {
+    return *(const LDS_PTR(u32x4))(uintptr_t)(place + (k * 16 + row16) * kPlacePitch + (lane & 3) * 16);
+  };
+  auto store = [&](char* half, uint32_t at, u32x4 v) __attribute__((always_inline)) { *reinterpret_cast<u32x4*>(half + at) = v; };
+
+  // Products of unit u; beside them the results of the one in front go out (in front of the first there is none: what
+  // is written for it goes to the first one's place, which is written again) and unit u + 2 comes in.  Some products in front
+  // of the end, with its last operand read, the waves meet: unit u + 1 is there, its first operands are read beside the rest, and
+  // the place of u is free for u + 3.
+  constexpr int kAhead = 8, kMeet = 26;
+  bf16x8 staged[kAhead];
+  Addresses here = addresses(now);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  char* dst = tiles + ((int64_t)head * t.key_tiles + 2 * pair) * kTileBytes;
 #pragma unroll
-  for (int j = 0; j < 2 * kTileBytes / (64 * kExpandWaves * 16); ++j) {
-    const int n = (j * 64 * kExpandWaves + tid) * 16;
-    *reinterpret_cast<u32x4*>(dst + n) = *reinterpret_cast<const u32x4*>(lds + n);
+  for (int s = 0; s < kAhead; ++s) staged[s] = operand(here, s);
+  u32x2 done[4] = {{0, 0}, {0, 0}, {0, 0}, {0, 0}};  // outputs of the unit in front
+  for (int u = begin; u < end; ++u) {
+    const uint32_t to = later + group * kGroupBytes;
+    const Source source2 = source(u + 2, to);
+    const int in_front = max(u - 1, begin);
+    char* const front = tile_of(in_front) + (in_front & 1) * half_bytes;
+    char* const ropes = tile_of(u) + (u & 1) * (kUnitKeys * kKeyBytes);
+    const uint32_t rope = now + rope_from;
+    const Addresses from = here;
+    here = addresses(next);
+    u32x4 leaving[3];
+    f32x16 acc;
+    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_sched_barrier(0);
+    each<kSteps>([&](auto index) __attribute__((always_inline)) {
+      constexpr int p = decltype(index)::value;
+      if constexpr (p == 0) first_expand_product(acc, weight[0], staged[0]);
+      else expand_product(acc, weight[p], staged[p % kAhead]);
+      if constexpr (p + kAhead < kSteps) staged[p % kAhead] = operand(from, p + kAhead);
+      if constexpr (p == 1 || p == 3 || p == 5) {
+        if (source2.whole) gather(source2.base, p - 1, to);
+      }
+      if constexpr (p % 2 == 0 && p >= 4 && p <= 10) write_place(done[(p - 4) / 2], (p - 4) / 2);
+      if constexpr (p == 12 || p == 13) leaving[p - 12] = read_place(p - 12);
+      if constexpr (p == 14) {
+        if (!of_keys) leaving[2] = *(const LDS_PTR(u32x4))(uintptr_t)rope;
+      }
+      if constexpr (p == 18 || p == 20) store(front, store_at[(p - 18) / 2], leaving[(p - 18) / 2]);
+      if constexpr (p == 22) {
+        if (!of_keys) store(ropes, rope_at, leaving[2]);
+      }
+      if constexpr (p == kMeet) {
+        // (in flight may be the stores of the unit in front, at least two, the gather of unit u + 2 and the stores behind it, five
+        // and two or four and three)
+        if (u + 2 < end && source2.whole) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_setprio(0);
+        __syncthreads();
+        __builtin_amdgcn_s_setprio(1);
+      }
+      // the next unit's operand k takes the place of the one of step kSteps - kAhead + k
+      if constexpr (p > kMeet && p <= kMeet + 3) {
+        constexpr int k = 2 * (p - kMeet - 1);
+        staged[k] = operand(here, k), staged[k + 1] = operand(here, k + 1);
+      }
+      if constexpr (p > kMeet + 3) staged[p - (kSteps - kAhead)] = operand(here, p - (kSteps - kAhead));
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    __builtin_amdgcn_s_setprio(0);
+    asm volatile("s_nop 15" : "+v"(acc));  // (the last product's result may be read 12 states behind it)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4)
+      done[r4] = u32x2{pack_bf16(acc[4 * r4], acc[4 * r4 + 1]), pack_bf16(acc[4 * r4 + 2], acc[4 * r4 + 3])};
+    const uint32_t place0 = now;
+    now = next, next = later, later = place0;
   }
+  static_assert(kSteps == 32 && kAhead == 8 && kMeet == 26, "as the places above are counted");
+#pragma unroll
+  for (int r4 = 0; r4 < 4; ++r4) write_place(done[r4], r4);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) store(tile_of(end - 1) + ((end - 1) & 1) * half_bytes, store_at[k], read_place(k));
 }
 
 // --- attention -----------------------------------------------------------------------------------------------------------
@@ -200,102 +310,136 @@ struct ExpandedArgs {
   float scale_log2;
 };
 
-// blockIdx.x: head (fastest: an XCD meets few heads, whose tiles its workgroups share) and tile of query rows, the request's
-// last rows, which see most keys, first.  Eight waves of 32 rows each: SETS 8 takes 256 rows; SETS 4 takes 128 and
-// divides the keys, the first halves of the key tiles to four waves and the second ones to the others, which join at the end.
+// blockIdx.x: head (fastest: an XCD meets few heads, whose tiles its workgroups share) and tile of 128 query rows, the
+// request's last rows, which see most keys, first.  A team of four waves, one on each SIMD, takes the rows, 32 each.  GROUPS 1: a
+// workgroup is one team and a unit holds two workgroups, so that each computes through the other's meetings, first loads
+// and last stores.  GROUPS 2: it is two teams, which divide the keys and join at the end.  Bound by the products and what has to
+// be issued beside them (45 % of the cycles are products), at a clock that their power sets.  One workgroup of eight waves
+// and 256 rows to a unit took 2 % more, four waves of 64 rows, whose operands serve two products, 15 % more.
 //
-// A wave works off its halves three at a time: while the scores of half n are turned into probabilities, the products form the
-// scores of n + 1 and add the values of n - 1.  The waves meet where one of the three enters another tile.  Keys are
-// gathered three tiles ahead and values, which are wanted two halves later, two tiles.  No maximum is formed on the way: the
+// A wave works off its keys in halves of tiles, three at a time: while the scores of half n are turned into probabilities, the
+// products form the scores of n + 1 and add the values of n - 1.  The waves meet in front of every round.  Keys are
+// gathered three halves ahead and values, which are wanted two halves later, two.  No maximum is formed on the way: the
 // reference is the row's maximum over the first half and moves where a half's sum of probabilities tells that one of
 // them passed 2^kSlack.
-constexpr int kAttendWaves = 8;
-constexpr int kKeyStages = 4, kValueStages = 3;
-constexpr int kValuesAt = kKeyStages * kKeysBytes;                           // in LDS
-constexpr int kZeros = kValuesAt + kValueStages * (kTileBytes - kKeysBytes);  // the values in front of the first half
+constexpr int kTeam = 4;                              // waves
+constexpr int kHalfKeys = kKeysBytes / 2, kHalfValues = (kTileBytes - kKeysBytes) / 2;
+constexpr int kKeyStages = 4, kValueStages = 3;       // halves in a team's LDS
+constexpr int kValuesAt = kKeyStages * kHalfKeys;
+constexpr int kTeamBytes = kValuesAt + kValueStages * kHalfValues;
+static_assert(kExpandedRowTile == kTeam * 32 && kTeam * 32 * kKeyBytes == kValuesAt, "the queries are first gathered to the keys' place");
+// The outputs leave through LDS too, in rows of 256 bytes and 16 more, so that sixteen rows' equal chunks take all banks.
+constexpr int kOutPitch = kValueBytes + 16;
+constexpr int kJoinPitch = 33;  // words: 32 outputs of a lane and one, so that the lanes' words take all banks
+constexpr int kJoinWords = 2 * 64 * kJoinPitch + 2 * 64;
+static_assert(32 * kOutPitch <= kHalfKeys && kTeam * kJoinWords * 4 <= kTeamBytes, "place for the outputs and a join");
 
-template <int SETS>
-__global__ __launch_bounds__(64 * kAttendWaves, 2) void expanded_attention_kernel(const ExpandedArgs args,
-                                                                                  const uint16_t* __restrict__ q,
-                                                                                  const char* __restrict__ tiles,
-                                                                                  uint16_t* __restrict__ out) {
-  constexpr int TILE = 32 * SETS;
-  constexpr bool kDivided = SETS < kAttendWaves;
-  constexpr int kKeyLoads = kKeysBytes / 1024 / kAttendWaves, kValueLoads = (kTileBytes - kKeysBytes) / 1024 / kAttendWaves;  // a wave's, of a tile
-  __shared__ __attribute__((aligned(1024))) char lds[kZeros + 32 * kValueBytes];
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
+template <int GROUPS>
+__global__ __launch_bounds__(64 * kTeam * GROUPS, 2) void expanded_attention_kernel(const ExpandedArgs args,
+                                                                                    const uint16_t* __restrict__ q,
+                                                                                    const char* __restrict__ tiles,
+                                                                                    uint16_t* __restrict__ out) {
+  constexpr int kKeyLoads = kHalfKeys / 1024 / kTeam, kValueLoads = kHalfValues / 1024 / kTeam;  // a wave's, of a half
+  constexpr int kZeros = GROUPS * kTeamBytes;  // what a key that is to be left out has for a value
+  __shared__ __attribute__((aligned(1024))) char lds[kZeros + 1024];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int set = wave % SETS, group = wave / SETS;
-  static_assert(32 * kValueBytes == 64 * kAttendWaves * 16, "a piece of the zeros each");
-  *reinterpret_cast<u32x4*>(lds + kZeros + tid * 16) = u32x4{0, 0, 0, 0};
+  const int set = wave % kTeam, group = wave / kTeam;
+  const uint32_t zeros = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + kZeros;
+  const uint32_t base = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + group * kTeamBytes;
+  *reinterpret_cast<u32x4*>(lds + kZeros + lane * 16) = u32x4{0, 0, 0, 0};  // (by every wave: it reads behind its own writes)
   const ExpandedTable& t = args.table;
   const int heads = t.heads;
   const int at = blockIdx.x / heads, head = blockIdx.x - at * heads;
-  const int r = find_request<false>(t, at, lane);
-  const LatentReq rq = t.req[r];
-  const int row_tiles = (rq.new_len + TILE - 1) / TILE;
-  const int row0 = (row_tiles - 1 - (at - t.row_tile_start[r])) * TILE;
-  const int rows = min(TILE, rq.new_len - row0);
-  const int keys = rq.cached + row0 + rows;
-  const int ntiles = (keys + kTileKeys - 1) / kTileKeys;
+  const Requests requests(t, lane);
+  int start;
+  const int r = requests.find_row_tile(t, at, lane, &start);
+  const LatentReq rq = requests.get(r);
+  const int row_tiles = (rq.new_len + kExpandedRowTile - 1) / kExpandedRowTile;
+  const int row0 = (row_tiles - 1 - (at - start)) * kExpandedRowTile;
+  const int rows = min(kExpandedRowTile, rq.new_len - row0);
+  // halves that some row sees: the team's begin at `first`, `count` of them
+  const int whole = (rq.cached + row0 + rows + 31) / 32, middle = (whole + 1) / 2;
+  const int first = GROUPS == 1 || group == 0 ? 0 : middle;
+  const int count = GROUPS == 1 ? whole : group == 0 ? middle : whole - middle;
+  const int rounds = GROUPS == 1 ? whole : middle;  // of the longer team
   const char* src = tiles + ((int64_t)head * t.key_tiles + rq.unit_start) * kTileBytes;
-  // (a tile in front of the first, or behind the last, stands for whatever lies in its place)
-  auto keys_at = [&](int tile) { return lds0 + (uint32_t)(tile & (kKeyStages - 1)) * kKeysBytes; };
-  auto values_of = [&](int tile) {
-    return lds0 + kValuesAt + (uint32_t)((tile + kValueStages) % kValueStages) * (kTileBytes - kKeysBytes);
+  // (halves are counted from the team's first; one in front of it, or behind the last, stands for whatever lies in its place)
+  auto keys_at = [&](int n) { return base + (uint32_t)(n & (kKeyStages - 1)) * kHalfKeys; };
+  auto values_at = [&](int n) { return base + kValuesAt + (uint32_t)((n + kValueStages) % kValueStages) * kHalfValues; };
+  auto tile_of = [&](int n) { return src + (int64_t)((first + n) >> 1) * kTileBytes; };
+  auto fetch_keys = [&](int n) __attribute__((always_inline)) {
+    const int piece = set * (kKeyLoads * 1024);
+    load_to_lds_run<kKeyLoads>(tile_of(n) + ((first + n) & 1) * kHalfKeys + piece, (uint32_t)lane * 16, keys_at(n) + piece);
   };
-  auto fetch_keys = [&](int tile) __attribute__((always_inline)) {
-    const char* from = src + (int64_t)tile * kTileBytes + wave * (kKeyLoads * 1024);
-    load_to_lds_run<kKeyLoads>(from, (uint32_t)lane * 16, keys_at(tile) + wave * (kKeyLoads * 1024));
-  };
-  auto fetch_values = [&](int tile) __attribute__((always_inline)) {
-    const char* from = src + (int64_t)tile * kTileBytes + kKeysBytes + wave * (kValueLoads * 1024);
-    load_to_lds_run<kValueLoads>(from, (uint32_t)lane * 16, values_of(tile) + wave * (kValueLoads * 1024));
+  auto fetch_values = [&](int n) __attribute__((always_inline)) {
+    const int piece = set * (kValueLoads * 1024);
+    load_to_lds_run<kValueLoads>(tile_of(n) + kKeysBytes + ((first + n) & 1) * kHalfValues + piece, (uint32_t)lane * 16, values_at(n) + piece);
   };
 
   const int i = lane & 31, part = lane >> 5;
-  const int row = min(set * 32 + i, rows - 1);
-  const int64_t packed = (int64_t)rq.row_start + row0 + row;
+  const int64_t packed = (int64_t)rq.row_start + row0;  // the workgroup's first row
   constexpr int kSteps = kQueryRow / 16, kBlocks = kLatentValue / 32, kValueProducts = 2 * kBlocks;
-  bf16x8 qb[kSteps];
+  // The wave's queries, swizzled as keys are: eight rows are three loads.  Rows behind the last are copies of it.
+  const uint32_t own_place = base + set * kHalfKeys;
+  {
+    const char* from = reinterpret_cast<const char*>(q + (packed * heads + head) * kQueryRow);
+    const uint32_t pitch = (uint32_t)heads * kKeyBytes;
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s)
-    qb[s] = *reinterpret_cast<const bf16x8*>(q + (packed * heads + head) * kQueryRow + s * 16 + part * 8);
-  fetch_keys(0);
-  fetch_values(0);
-  if (1 < ntiles) fetch_keys(1);
-  // (the loop below counts the gathers in flight itself: everything the compiler knows of is waited for here)
-  __builtin_amdgcn_s_waitcnt(0x0F70);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (!kDivided && 1 < ntiles) fetch_values(1);
-  if (2 < ntiles) fetch_keys(2);
-  if (3 < ntiles) fetch_keys(3);
-  __syncthreads();
-  const int visible = rq.cached + row0 + row + 1;
-  const int least = rq.cached + row0 + set * 32 + 1;  // of the wave's first row
-  // halves of which the wave's last row sees a part, counted in its own; none where the wave has no rows
-  const int seen = set * 32 >= rows ? 0 : (rq.cached + row0 + min(set * 32 + 31, rows - 1) + 32) / 32;
-  const int halves = kDivided ? (seen + 1 - group) / 2 : seen;
-
+    for (int j = 0; j < 3; ++j) {
+      const int n = j * 64 + lane, of8 = n / 24, chunk = n - of8 * 24;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int row = g * 8 + of8;
+        const int64_t off = (int64_t)(uint32_t)min(set * 32 + row, rows - 1) * pitch + ((chunk ^ key_swizzle(row)) << 4);
+        load_to_lds_16(from + off, own_place + (g * 3 + j) * 1024);
+      }
+    }
+  }
+  if (0 < count) {
+    fetch_values(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kValueLoads) : "memory");
+  } else {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
   uint32_t key_at[4], value_at[kBlocks];
 #pragma unroll
   for (int s = 0; s < 4; ++s) key_at[s] = i * kKeyBytes + (((2 * s + part) ^ key_swizzle(i)) << 4);
+  const int value_key = part * 4 + ((lane & 15) >> 2);  // and 8, 16, 24 further on
   {
-    const int w16 = lane & 15, blk = lane >> 4;
-    const int key = (blk >> 1) * 4 + (w16 >> 2), chunk = 2 * (blk & 1) + ((w16 & 3) >> 1);
+    const int w16 = lane & 15, chunk = 2 * ((lane >> 4) & 1) + ((w16 & 3) >> 1);
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d)
-      value_at[d] = key * kValueBytes + (((4 * d + chunk) ^ value_swizzle(key)) << 4) + (w16 & 1) * 8;
+      value_at[d] = value_key * kValueBytes + (((4 * d + chunk) ^ value_swizzle(value_key)) << 4) + (w16 & 1) * 8;
   }
+  auto key_operand = [&](uint32_t ks, int n) __attribute__((always_inline)) {
+    return *(const LDS_PTR(u32x4))(uintptr_t)(ks + key_at[n & 3] + (n >> 2) * 128);
+  };
+  bf16x8 qb[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) qb[s] = __builtin_bit_cast(bf16x8, key_operand(own_place, s));
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < kKeyStages; ++n)
+    if (n < count) fetch_keys(n);
+  if (kKeyStages <= count) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kKeyLoads) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  const int visible = rq.cached + row0 + min(set * 32 + i, rows - 1) + 1;
+  const int least = rq.cached + row0 + set * 32 + 1;  // of the wave's first row
+  // of the team's halves those of which the wave's last row sees a part; none where the wave has no rows
+  const int seen = set * 32 >= rows ? 0 : (rq.cached + row0 + min(set * 32 + 31, rows - 1) + 32) / 32;
+  const int halves = max(0, min(seen - first, count));
+
   f32x16 o[kBlocks];
 #pragma unroll
   for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float m_run = kNoReference, l_run = 0.f;
-  f32x16 s0, s1;                  // scores of an even and an odd half
+  f32x16 s0, s1;                                      // scores of an even and an odd half
   u32x4 p0[2], p1[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // and their probabilities, as operands
+  uint32_t dropped = ~0u;  // keys of the half in front that count for nothing (in front of the first: all)
 
   // Products of a round: the scores of the 32 keys at `ks` into `sn`, the values of the 32 keys at `vs` under the
   // probabilities `pv`; beside them the probabilities of the scores `sc` into `pn`, whose sum is returned.
@@ -306,29 +450,39 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void expanded_attention_kerne
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, sum, false);
   };
-  auto key_operand = [&](uint32_t ks, int n) __attribute__((always_inline)) {
-    return *(const LDS_PTR(u32x4))(uintptr_t)(ks + key_at[n & 3] + (n >> 2) * 128);
-  };
   auto score_product = [&](u32x4 a, int n, f32x16& sn) __attribute__((always_inline)) {
     f32x16 from = sn;
     if (n == 0) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) from[r] = 0.f;
+      for (int e = 0; e < 16; ++e) from[e] = 0.f;
     }
     sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qb[n], from, 0, 0, 0);
   };
   auto round = [&](f32x16& sn, uint32_t ks, const u32x4 (&pv)[2], uint32_t vs, const f32x16& sc, u32x4 (&pn)[2]) __attribute__((always_inline)) -> float {
     u32x4 staged[kAhead];
+    uint32_t va[4][kBlocks];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) va[g][d] = vs + value_at[d] + g * 8 * kValueBytes;
+    if (dropped) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+          if (dropped >> (value_key + g * 8) & 1) va[g][d] = zeros;
+    }
     auto operand = [&](int n) __attribute__((always_inline)) -> u32x4 {
       if (n < kSteps) return key_operand(ks, n);
       const int k = (n - kSteps) / kBlocks, d = (n - kSteps) % kBlocks;
-      const uint32_t v = vs + value_at[d] + k * 16 * kValueBytes;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(v + 8 * kValueBytes));
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(va[2 * k][d]));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(va[2 * k + 1][d]));
       return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 #pragma unroll
     for (int n = 0; n < kAhead; ++n) staged[n] = operand(n);
+    // (a wave with operands goes in front of one that looks after meetings and gathers: 10 % fewer cycles)
+    __builtin_amdgcn_s_setprio(1);
     __builtin_amdgcn_sched_barrier(0);
     float sum = 0.f, pair[2];
 #pragma unroll
@@ -352,56 +506,48 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void expanded_attention_kerne
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     return sum;
   };
   auto row_max = [&](const f32x16& sc) __attribute__((always_inline)) {
     float mx = sc[0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e]);
     return cross_half_max(mx) * args.scale_log2;
   };
-  // The waves meet in front of the round that enters key tile `next`: it is there then, as are the values of the tile
-  // `kLate` tiles in front of it, and what the rounds so far read is free for those further on.
-  constexpr int kLate = kDivided ? 2 : 1;
-  auto meet = [&](int next) __attribute__((always_inline)) {
-    // (in flight may be what the meeting in front sent for: keys three tiles on, values)
-    if (next + 2 < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kKeyLoads + kValueLoads) : "memory");
-    else if (next + 1 - kLate < ntiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kValueLoads) : "memory");
+  // In front of round n: the keys of half n + 1 and the values of n - 1 are there, and the places of the keys of n and of the
+  // values of n - 2 are free.
+  auto meet = [&](int n) __attribute__((always_inline)) {
+    // (in flight may be, in this order: keys n + 2, values n, keys n + 3)
+    if (n + 3 < count) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kKeyLoads + kValueLoads) : "memory");
+    else if (n + 2 < count) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kKeyLoads + kValueLoads) : "memory");
+    else if (n < count) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kValueLoads) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (next + 3 < ntiles) fetch_keys(next + 3);
-    if (next + 2 - kLate < ntiles) fetch_values(next + 2 - kLate);
+    if (n + 1 < count) fetch_values(n + 1);
+    if (n + 4 < count) fetch_keys(n + 4);
   };
 
   // The wave's n-th half: scores `sc`, probabilities to `pn`.  The round's products are those of its neighbours.  Behind the
   // last half there is a round for its values alone: what it does beside them is for nobody, as are the scores behind
   // the last half.
-  auto tile_of = [&](int n) { return kDivided ? n : n >> 1; };
-  auto half_of = [&](int n) { return kDivided ? group : n & 1; };
   auto half = [&](int n, f32x16& sc, f32x16& sn, u32x4 (&pn)[2], u32x4 (&po)[2]) __attribute__((always_inline)) {
     if (n > halves || halves == 0) return;
     const bool last = n == halves;
-    const int key0 = tile_of(n) * kTileKeys + half_of(n) * 32;
+    const int key0 = (first + n) * 32;
+    uint32_t unfit = 0;
     if (!last && key0 + 32 > least) {
       float raw[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) raw[r] = sc[r];
-      uint32_t unfit = unfit_keys<32>(raw);
+      for (int e = 0; e < 16; ++e) raw[e] = sc[e];
+      unfit = unfit_keys<32>(raw);
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (key0 + (r >> 2) * 8 + part * 4 + (r & 3) >= visible) sc[r] = -__builtin_inff();
-      // Their values become zeros where they lie: the weight of a row that sees such a key is no number, so that any wave may
-      // take either.
-      while (unfit) {
-        const int key = half_of(n) * 32 + __builtin_ctz(unfit);
-        unfit &= unfit - 1;
-        if (lane < kValueBytes / 16)
-          *(LDS_PTR(u32x4))(uintptr_t)(values_of(tile_of(n)) + key * kValueBytes + lane * 16) = u32x4{0, 0, 0, 0};
-      }
+      for (int e = 0; e < 16; ++e)
+        if (key0 + (e >> 2) * 8 + part * 4 + (e & 3) >= visible) sc[e] = -__builtin_inff();
     }
     if (n == 0) m_run = fmaxf(row_max(sc), kNoReference);
-    const uint32_t front = n == 0 ? lds0 + kZeros : values_of(tile_of(n - 1)) + half_of(n - 1) * 32 * kValueBytes;
-    float sum = round(sn, keys_at(tile_of(n + 1)) + half_of(n + 1) * 32 * kKeyBytes, po, front, sc, pn);
+    float sum = round(sn, keys_at(n + 1), po, values_at(n - 1), sc, pn);
+    dropped = unfit;
     if (last) return;
     if (__any(sum >= kOver)) {
       const float mx = row_max(sc);
@@ -411,7 +557,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void expanded_attention_kerne
 #pragma unroll
       for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] *= f;
+        for (int e = 0; e < 16; ++e) o[d][e] *= f;
       m_run = m_new;
       sum = 0.f;
 #pragma unroll
@@ -425,73 +571,59 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void expanded_attention_kerne
   };
   if (halves > 0) {
 #pragma unroll
-    for (int n = 0; n < kSteps; ++n) score_product(key_operand(keys_at(0) + half_of(0) * 32 * kKeyBytes, n), n, s0);
+    for (int n = 0; n < kSteps; ++n) score_product(key_operand(keys_at(0), n), n, s0);
   }
-  if constexpr (kDivided) {
-    for (int n = 0; n <= ntiles; n += 2) {
-      meet(n + 1);
-      half(n, s0, s1, p0, p1);
-      if (n + 1 > ntiles) break;
-      meet(n + 2);
-      half(n + 1, s1, s0, p1, p0);
-    }
-  } else {
-    for (int tile = 0; tile <= ntiles; ++tile) {
-      half(2 * tile, s0, s1, p0, p1);
-      if (tile == ntiles) break;
-      meet(tile + 1);
-      half(2 * tile + 1, s1, s0, p1, p0);
-    }
+  for (int n = 0; n <= rounds; n += 2) {
+    meet(n);
+    half(n, s0, s1, p0, p1);
+    meet(n + 1);
+    half(n + 1, s1, s0, p1, p0);
   }
+  __syncthreads();  // the tiles' place is free
   l_run = cross_half_sum(l_run);
-  if constexpr (kDivided) {
-    // join: the second four waves leave their outputs, references and sums, a row to a lane, the first four add them
-    constexpr int kPitch = 33;  // words of a lane's 32 and one, so that the lanes' words take all banks
-    float* const left = reinterpret_cast<float*>(lds) + set * (64 * kPitch * 2 + 2 * 64);
-    static_assert(SETS * (64 * kPitch * 2 + 2 * 64) * 4 <= kZeros, "the join takes the tiles' place");
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+  float own = 1.f / l_run, other = 0.f;
+  // Two teams: the second one leaves its outputs, references and sums, the first one adds them.
+  float* const left = reinterpret_cast<float*>(lds + kTeamBytes) + set * kJoinWords;
+  float* const stats = left + 2 * 64 * kJoinPitch;
+  auto place = [&](int d, int e) { return ((d >> 1) * 64 + lane) * kJoinPitch + (d & 1) * 16 + e; };
+  if constexpr (GROUPS == 2) {
     if (group == 1) {
 #pragma unroll
       for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) left[(d >> 1) * 64 * kPitch + lane * kPitch + (d & 1) * 16 + r] = o[d][r];
-      left[64 * kPitch * 2 + lane] = m_run;
-      left[64 * kPitch * 2 + 64 + lane] = l_run;
+        for (int e = 0; e < 16; ++e) left[place(d, e)] = o[d][e];
+      stats[lane] = m_run;
+      stats[64 + lane] = l_run;
     }
     __syncthreads();
     if (group == 1) return;
-    const float m_other = left[64 * kPitch * 2 + lane], l_other = left[64 * kPitch * 2 + 64 + lane];
-    const float m = fmaxf(m_run, m_other);
-    const float f = __builtin_amdgcn_exp2f(m_run - m), f_other = __builtin_amdgcn_exp2f(m_other - m);
-    l_run = l_run * f + l_other * f_other;
-#pragma unroll
-    for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * f + left[(d >> 1) * 64 * kPitch + lane * kPitch + (d & 1) * 16 + r] * f_other;
+    const float m_other = stats[lane], l_other = stats[64 + lane], m = fmaxf(m_run, m_other);
+    own = __builtin_amdgcn_exp2f(m_run - m), other = __builtin_amdgcn_exp2f(m_other - m);
+    const float inv = 1.f / (l_run * own + l_other * other);
+    own *= inv, other *= inv;
   }
-  const float inv = 1.f / l_run;
-  uint16_t* dst = out + (packed * heads + head) * kLatentValue;
-  // the two halves of the wave exchange four columns each, so that a lane writes eight in a row
+  // out through LDS, sixteen lanes to a row
+  char* const staged = lds + set * kHalfKeys;
 #pragma unroll
   for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-    for (int r8 = 0; r8 < 2; ++r8) {
-      u32x2 x[2];
+    for (int e4 = 0; e4 < 4; ++e4) {
+      float v[4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          x[h][k] = pack_bf16(o[d][r8 * 8 + h * 4 + 2 * k] * inv, o[d][r8 * 8 + h * 4 + 2 * k + 1] * inv);
-      u32x4 words;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const auto both = __builtin_amdgcn_permlane32_swap(x[0][k], x[1][k], false, false);
-        words[k] = both[0];
-        words[2 + k] = both[1];
+      for (int k = 0; k < 4; ++k) {
+        v[k] = o[d][4 * e4 + k] * own;
+        if constexpr (GROUPS == 2) v[k] = __builtin_fmaf(left[place(d, 4 * e4 + k)], other, v[k]);
       }
-      if (set * 32 + i < rows) *reinterpret_cast<u32x4*>(dst + d * 32 + r8 * 16 + part * 8) = words;
+      *reinterpret_cast<u32x2*>(staged + i * kOutPitch + (d * 32 + e4 * 8 + part * 4) * 2) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     }
+  uint16_t* dst = out + ((packed + set * 32) * heads + head) * kLatentValue;
+#pragma unroll
+  for (int row4 = 0; row4 < 32; row4 += 4) {
+    const int row = row4 + (lane >> 4);
+    if (set * 32 + row < rows)
+      *reinterpret_cast<u32x4*>(dst + (int64_t)row * heads * kLatentValue + (lane & 15) * 8) =
+          *reinterpret_cast<const u32x4*>(staged + row * kOutPitch + (lane & 15) * 16);
+  }
 }
 
 int latent_attention_expanded(const efim_batch_t* b, const void* q, const void* cache, const void* w_kv, void* out,
@@ -513,14 +645,13 @@ int latent_attention_expanded(const efim_batch_t* b, const void* q, const void* 
   LatentCursor at;
   while (expanded_next(b, plan, &at, &args.table)) {
     const unsigned heads = (unsigned)b->num_q_heads;
-    expand_kernel<<<(unsigned)args.table.key_tiles / 2 * heads, 64 * kExpandWaves, 0, stream>>>(
+    expand_kernel<<<(unsigned)args.table.slices * heads, 64 * kExpandWaves, 0, stream>>>(
         args.table, static_cast<const uint16_t*>(cache), static_cast<const uint16_t*>(w_kv), b->block_table, tiles);
-    if (plan.row_tile == 256)
-      expanded_attention_kernel<8><<<(unsigned)args.table.row_tiles * heads, 512, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
-                                                                                    static_cast<uint16_t*>(out));
+    const unsigned groups = (unsigned)args.table.row_tiles * heads;
+    if (plan.teams == 1)
+      expanded_attention_kernel<1><<<groups, 64 * kTeam, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles, static_cast<uint16_t*>(out));
     else
-      expanded_attention_kernel<4><<<(unsigned)args.table.row_tiles * heads, 512, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles,
-                                                                                    static_cast<uint16_t*>(out));
+      expanded_attention_kernel<2><<<groups, 128 * kTeam, 0, stream>>>(args, static_cast<const uint16_t*>(q), tiles, static_cast<uint16_t*>(out));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }
   }

@@ -65,13 +65,28 @@ bool latent_next(const efim_batch_t* b, const LatentPlan& plan, LatentCursor* at
   return true;
 }
 
+// Slices of a head's `keys` units of 32 keys, a workgroup each: the number by which the device's rounds of workgroups take
+// least, where a workgroup spends about as long on its weight as on kWeightUnits units.
+static int expanded_slices(int64_t keys, int64_t heads, int units) {
+  constexpr int64_t kWeightUnits = 4;
+  int64_t best = 1, best_cost = INT64_MAX;
+  const int64_t most = 4 * (int64_t)units / heads + 1;
+  for (int64_t s = 1; s <= most && s <= keys; ++s) {
+    const int64_t cost = (heads * s + units - 1) / units * ((keys + s - 1) / s + kWeightUnits);
+    if (cost < best_cost) best = s, best_cost = cost;
+  }
+  return (int)best;
+}
+
 ExpandedPlan plan_expanded(const efim_batch_t* b, int units) {
   ExpandedPlan plan;
-  // 256 rows share a gathered tile once more than 128 do, 128 leave more workgroups and less of a short last tile empty:
-  // the larger one where it still leaves every unit two of them.
-  int64_t large = 0;
-  for (int r = 0; r < b->batch; ++r) large += ((int64_t)b->new_len[r] + 255) / 256 * b->num_q_heads;
-  plan.row_tile = large >= 2 * (int64_t)units ? 256 : 128;
+  plan.units = units;
+  // Two teams to a workgroup, which halve its keys, while there are no more than two workgroups for each unit: then the longest
+  // workgroup or the second round of them sets the time.  Beyond, one team, two workgroups to a unit.  us with two and one
+  // (256 units): 64 workgroups of 3400 keys 87 / 104, 304 of up to 2355 70 / 80, 512 122 / 138, 608 168 / 167, 928 201 / 174.
+  int64_t groups = 0;
+  for (int r = 0; r < b->batch; ++r) groups += ((int64_t)b->new_len[r] + kExpandedRowTile - 1) / kExpandedRowTile * b->num_q_heads;
+  plan.teams = groups > 2 * (int64_t)units ? 1 : 2;
   plan.ok = true;
   ExpandedTable table;
   LatentCursor at;
@@ -95,7 +110,7 @@ bool expanded_next(const efim_batch_t* b, const ExpandedPlan& plan, LatentCursor
     const int n = b->new_len[at->req];
     if (n == 0) continue;
     const int64_t more_keys = ((int64_t)b->cached_len[at->req] + n + 2 * kExpandedTileKeys - 1) / (2 * kExpandedTileKeys) * 2;
-    const int64_t more_rows = ((int64_t)n + plan.row_tile - 1) / plan.row_tile;
+    const int64_t more_rows = ((int64_t)n + kExpandedRowTile - 1) / kExpandedRowTile;
     if (t->nreq > 0 && ((key_tiles + more_keys) * b->num_q_heads > INT32_MAX / 512 ||
                         (row_tiles + more_rows) * b->num_q_heads > INT32_MAX / 512))
       break;
@@ -106,6 +121,7 @@ bool expanded_next(const efim_batch_t* b, const ExpandedPlan& plan, LatentCursor
     at->row += n;
   }
   t->key_tiles = (int32_t)key_tiles;
+  t->slices = t->nreq > 0 ? expanded_slices(key_tiles * 2, b->num_q_heads, plan.units) : 0;
   t->row_tiles = (int32_t)row_tiles;
   return t->nreq > 0;
 }

@@ -89,6 +89,7 @@ bool latent_next(const efim_batch_t* b, const LatentPlan& plan, LatentCursor* at
 // Key tiles (unit_start) are made in pairs, so a request has an even number of them.
 constexpr int kExpandedTileKeys = 64;
 constexpr int kExpandedTileBytes = 64 * (192 + 128) * 2;
+constexpr int kExpandedRowTile = 128;
 
 struct ExpandedTable {
   LatentReq req[kLatentTableReqs];
@@ -98,12 +99,14 @@ struct ExpandedTable {
   int32_t max_pages;
   int32_t page_shift;
   int32_t key_tiles;                         // of one head
+  int32_t slices;                            // of its keys, each expanded by a workgroup
   int32_t row_tiles;
 };
 
 struct ExpandedPlan {
   bool ok = false;       // every launch's numbers of workgroups are within a launch's reach
-  int row_tile = 0;      // query rows of a workgroup: 128 or 256
+  int teams = 0;         // of a workgroup of the attention: 1 or 2
+  int units = 0;         // compute units
   size_t bytes = 0;      // workspace: the expanded tiles of the largest launch
 };
 ExpandedPlan plan_expanded(const efim_batch_t* b, int units);

@@ -16,7 +16,7 @@ using namespace efim;
 
 int main() {
   std::mt19937_64 rng(11);
-  long parts = 0, launches = 0, tiles128 = 0, tiles256 = 0;
+  long parts = 0, launches = 0, one_team = 0, two_teams = 0;
   for (int iter = 0; iter < 4000; ++iter) {
     const int B = (int)(rng() % 8 == 0 ? rng() % 400 : rng() % 24);
     std::vector<int32_t> cached(B), fresh(B);
@@ -92,12 +92,13 @@ int main() {
 
     const ExpandedPlan ep = plan_expanded(&b, 256);
     CHECK(ep.ok);
-    (ep.row_tile == 256 ? tiles256 : tiles128) += 1;
+    (ep.teams == 2 ? two_teams : one_team) += 1;
     LatentCursor ea;
     ExpandedTable e;
     expect = 0;
     row = 0;
     while (expanded_next(&b, ep, &ea, &e)) {
+      CHECK(e.slices >= 1 && e.slices <= e.key_tiles * kExpandedTileKeys / 32 && e.slices * (int64_t)e.heads <= 4 * 256 + e.heads);
       CHECK(e.key_tiles % 2 == 0 && (size_t)e.key_tiles * b.num_q_heads * kExpandedTileBytes <= ep.bytes);
       for (int k = 0; k < e.nreq; ++k) {
         const LatentReq& q = e.req[k];
@@ -106,14 +107,14 @@ int main() {
         const int64_t key_tiles = (k + 1 < e.nreq ? e.req[k + 1].unit_start : e.key_tiles) - q.unit_start;
         const int row_tiles = (k + 1 < e.nreq ? e.row_tile_start[k + 1] : e.row_tiles) - e.row_tile_start[k];
         CHECK(key_tiles % 2 == 0 && key_tiles * kExpandedTileKeys >= q.cached + q.new_len && (key_tiles - 2) * kExpandedTileKeys < q.cached + q.new_len);
-        CHECK(row_tiles == (q.new_len + ep.row_tile - 1) / ep.row_tile);
+        CHECK(row_tiles == (q.new_len + kExpandedRowTile - 1) / kExpandedRowTile);
         row += q.new_len;
         ++expect;
       }
     }
     CHECK(row == total);
   }
-  CHECK(parts > 0 && tiles128 > 0 && tiles256 > 0);
+  CHECK(parts > 0 && one_team > 0 && two_teams > 0);
   printf("latent plan ok, %ld launches, %ld parts\n", launches, parts);
   return 0;
 }

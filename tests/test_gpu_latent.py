@@ -278,6 +278,24 @@ def test_infinities_and_nan_behind_the_causal_limit(E):
         assert np.array_equal(_expanded(E, b, qe, w)[:11], clean_e[:11])
 
 
+def test_query_rows_that_are_no_numbers_keep_to_themselves(E):
+    """Whole runs of a wave's query rows, and runs that cross tiles, in requests whose other rows see the same keys."""
+    cached, new, heads = [5, 700, 40], [400, 300, 150], 4
+    b = Batch(cached, new, heads, 16, 47)
+    q, w = b.gaussian(b.total, heads, ROW), b.gaussian(heads, 256, 512, sigma=512 ** -0.5)
+    short = np.ascontiguousarray(q[:, :, :192])
+    clean = _absorbed(E, b, q), _expanded(E, b, short, w)
+    bad = np.zeros(b.total, bool)
+    for lo, hi in ((0, 70), (128, 256), (310, 401), (500, 564), (700, 849)):
+        bad[lo:hi] = True
+    for value in (0x7FC0, 0x7F80):
+        q2, short2 = q.copy(), short.copy()
+        q2[bad], short2[bad] = value, value
+        for got, want in zip((_absorbed(E, b, q2), _expanded(E, b, short2, w)), clean):
+            assert np.array_equal(got[~bad], want[~bad])
+            assert not np.any(np.isfinite(bf16_to_f64(got[bad])))
+
+
 def test_streams_and_graph_replays(E):
     """A side stream, and a captured graph replayed between eager work: append, both attentions."""
     b = Batch([900, 33], [3, 4], 16, 16, 13)
