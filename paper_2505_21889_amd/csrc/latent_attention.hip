@@ -108,10 +108,22 @@ struct Share {
     group = (int)(blockIdx.x % kXcds) * (int)(gridDim.x / kXcds) + (int)(blockIdx.x / kXcds);
     next = end = 0;
     if (group >= t.groups) return;
+    first = true;
+    if (t.by_tile) {
+      at.r = requests.find_group(group, lane);
+      rq = requests.get(at.r);
+      const int n = (int)(rq.unit_start >> 32), k = group - (int)(uint32_t)rq.unit_start;
+      at.tile = k / n;
+      at.units = latent_units_of(rq, t.heads, TILE, at.tile);
+      at.first = 0;
+      next = LatentTable::first_of(at.units, n, k - at.tile * n);
+      end = LatentTable::first_of(at.units, n, k - at.tile * n + 1);
+      part();
+      return;
+    }
     next = t.first_unit(group);
     end = t.first_unit(group + 1);
     at = find_tile<TILE>(t, requests, next, lane);
-    first = true;
     rq = requests.get(at.r);
     part();
   }
@@ -731,16 +743,27 @@ __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args,
   const LatentTable& t = args.table;
   const int lane = threadIdx.x & 63;
   const int group = blockIdx.y + 1;
-  const int64_t cut = t.first_unit(group);
   const Requests requests(t, lane);
-  const Place at = find_tile<TILE>(t, requests, cut, lane);
-  if (cut == at.first || t.first_unit(group - 1) > at.first) return;
-  const LatentReq q = requests.get(at.r);
-  const int rows = latent_rows_of(q, t.heads, TILE, at.tile);
+  Place at;
+  LatentReq q;
   int parts = 2;
-  while (group - 1 + parts < t.groups && t.first_unit(group - 1 + parts) < at.first + at.units) ++parts;
-  // the first part is its workgroup's first too where the two begin together, the others are
-  const bool together = t.first_unit(group - 1) == at.first;
+  bool together = true;
+  if (t.by_tile) {
+    q = requests.get(requests.find_group(group, lane));
+    const int k = group - (int)(uint32_t)q.unit_start;
+    parts = (int)(q.unit_start >> 32);
+    at.tile = k / parts;
+    if (k - at.tile * parts != 1) return;
+  } else {
+    const int64_t cut = t.first_unit(group);
+    at = find_tile<TILE>(t, requests, cut, lane);
+    if (cut == at.first || t.first_unit(group - 1) > at.first) return;
+    q = requests.get(at.r);
+    while (group - 1 + parts < t.groups && t.first_unit(group - 1 + parts) < at.first + at.units) ++parts;
+    // the first part is its workgroup's first too where the two begin together, the others are
+    together = t.first_unit(group - 1) == at.first;
+  }
+  const int rows = latent_rows_of(q, t.heads, TILE, at.tile);
   auto slot_of = [&](int s) { return latent_slot(group - 1 + s, s > 0 || together); };
   for (int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); row < rows; row += 4 * gridDim.x) {
     float m = kNoReference, l = 0.f, v[8] = {};
@@ -813,7 +836,7 @@ int latent_attention(const efim_batch_t* b, const void* q, const void* cache, vo
     };
     if (plan.row_tile == 16) launch(latent_keys_kernel<16>, latent_join_kernel<16>, 4);
     else if (plan.row_tile == 32) launch(latent_keys_kernel<32>, latent_join_kernel<32>, 8);
-    else launch(latent_rows_kernel, latent_join_kernel<128>, 16);
+    else launch(latent_rows_kernel, latent_join_kernel<128>, args.table.by_tile ? 32 : 16);  // (many parts of few tiles, or two of each)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }
   }

@@ -41,6 +41,13 @@ struct Requests {
     for (int i = 0; i < kLatentTableReqs / 64; ++i) r += __popcll(__ballot(i * 64 + lane < nreq && held[i].unit_start <= unit));
     return __builtin_amdgcn_readfirstlane(r);
   }
+  // the request of a workgroup, dealt by tile
+  __device__ __forceinline__ int find_group(int group, int lane) const {
+    int r = -1;
+#pragma unroll
+    for (int i = 0; i < kLatentTableReqs / 64; ++i) r += __popcll(__ballot(i * 64 + lane < nreq && (int)(uint32_t)held[i].unit_start <= group));
+    return __builtin_amdgcn_readfirstlane(r);
+  }
   // the request of a tile of query rows, and its first tile
   __device__ __forceinline__ int find_row_tile(const ExpandedTable& t, int tile, int lane, int* first) const {
     int starts[kLatentTableReqs / 64], r = -1;

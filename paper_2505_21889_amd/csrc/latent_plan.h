@@ -19,13 +19,16 @@ constexpr int kLatentTableReqs = 128;   // requests of a launch (kernel argument
 
 // --- absorbed form ---------------------------------------------------------------------------------------------------------
 // A tile is `row_tile` query rows (token x head) of a request.  Its work is a unit for each 32 keys in front of and at the
-// last one that its rows see.  The units of all tiles, one tile behind the other, are dealt out evenly to as many
-// workgroups as the device has compute units, whatever the requests' lengths: a workgroup's share is a run of them, which
-// may begin and end inside a tile.  The parts of a tile that several workgroups share are joined by a second kernel.
+// last one that its rows see.  They are dealt out to as many workgroups as the device has compute units.
+//   * Evenly: the units of all tiles one behind the other, whatever the requests' lengths.  A workgroup's share is a run of them,
+//     which may begin and end inside a tile.
+//   * By tile, where there are few: each tile of a request has the same number of workgroups, which have a part of it each.
+// The parts of a tile that several workgroups share are joined by a second kernel.
 constexpr int kLatentTileKeys = 32;
 
 struct LatentReq {
-  int64_t unit_start;  // units in front of the request in the launch (expanded form: key tiles, of one head)
+  int64_t unit_start;  // units in front of the request in the launch (expanded form: key tiles, of one head; dealt by tile:
+                       // workgroups in front, and from bit 32 on the workgroups of each of its tiles)
   int32_t req;         // block table row
   int32_t cached;      // C_r
   int32_t new_len;     // N_r > 0
@@ -38,12 +41,15 @@ struct LatentTable {
   int64_t share;       // units of a workgroup; the first `longer` have one more
   int32_t longer;
   int32_t groups;      // workgroups with a share
+  int32_t by_tile;     // how they are dealt
   int32_t nreq;
   int32_t heads;
   int32_t max_pages;
   int32_t page_shift;
 
   EFIM_HOST_DEVICE int64_t first_unit(int group) const { return group * share + (group < longer ? group : longer); }
+  // by tile: the first of a tile's units that part j of n has
+  EFIM_HOST_DEVICE static int first_of(int units, int n, int j) { return units / n * j + (j < units % n ? j : units % n); }
 };
 
 // Tiles of a request, the rows of one and its units.

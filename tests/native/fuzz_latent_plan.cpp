@@ -16,7 +16,7 @@ using namespace efim;
 
 int main() {
   std::mt19937_64 rng(11);
-  long parts = 0, launches = 0, one_team = 0, two_teams = 0;
+  long parts = 0, launches = 0, by_tile = 0, one_team = 0, two_teams = 0;
   for (int iter = 0; iter < 4000; ++iter) {
     const int B = (int)(rng() % 8 == 0 ? rng() % 400 : rng() % 24);
     std::vector<int32_t> cached(B), fresh(B);
@@ -48,14 +48,17 @@ int main() {
     while (latent_next(&b, plan, &at, &t)) {
       ++launches;
       CHECK(t.nreq > 0 && t.nreq <= kLatentTableReqs && t.groups > 0 && t.groups <= plan.units);
-      CHECK(t.first_unit(0) == 0 && t.first_unit(t.groups) == t.units);
+      CHECK(t.by_tile || (t.first_unit(0) == 0 && t.first_unit(t.groups) == t.units));
+      by_tile += t.by_tile;
       int group = 0, of_group = 0;       // the workgroup at hand, and how many parts of it are done
       std::vector<int> used(plan.slots, 0);
       int64_t unit = 0;
       for (int k = 0; k < t.nreq; ++k) {
         const LatentReq& q = t.req[k];
         while (fresh[expect] == 0) ++expect;
-        CHECK(q.req == expect && q.cached == cached[expect] && q.new_len == fresh[expect] && q.row_start == row && q.unit_start == unit);
+        CHECK(q.req == expect && q.cached == cached[expect] && q.new_len == fresh[expect] && q.row_start == row && (t.by_tile || q.unit_start == unit));
+        const int n = t.by_tile ? (int)(q.unit_start >> 32) : 0;
+        CHECK(!t.by_tile || (n > 0 && (int)(uint32_t)q.unit_start == group));
         int rows = 0;
         const int tiles = latent_tiles(q, t.heads, plan.row_tile);
         for (int tile = 0; tile < tiles; ++tile) {
@@ -64,7 +67,16 @@ int main() {
           rows += mine;
           const int seen = q.cached + (rows - 1) / t.heads + 1;  // of the last row
           CHECK(latent_keys_of(q, t.heads, plan.row_tile, tile) == seen && units * kLatentTileKeys >= seen && (units - 1) * kLatentTileKeys < seen);
-          for (int64_t u = unit; u < unit + units;) {
+          for (int j = 0; j < n; ++j, ++group) {
+            const int from = LatentTable::first_of(units, n, j), to = LatentTable::first_of(units, n, j + 1);
+            CHECK(from < to && (j > 0 || from == 0) && (j < n - 1 || to == units));
+            if (n > 1) {
+              ++parts;
+              const int slot = latent_slot(group, true);
+              CHECK(slot < plan.slots && !used[slot]++);
+            }
+          }
+          for (int64_t u = unit; !t.by_tile && u < unit + units;) {
             while (t.first_unit(group + 1) <= u) {
               ++group;
               of_group = 0;
@@ -86,7 +98,7 @@ int main() {
         row += q.new_len;
         ++expect;
       }
-      CHECK(unit == t.units && group == t.groups - 1);
+      CHECK(unit == t.units && group == (t.by_tile ? t.groups : t.groups - 1));
     }
     CHECK(row == total);
 
@@ -114,7 +126,7 @@ int main() {
     }
     CHECK(row == total);
   }
-  CHECK(parts > 0 && one_team > 0 && two_teams > 0);
+  CHECK(parts > 0 && by_tile > 0 && by_tile < launches && one_team > 0 && two_teams > 0);
   printf("latent plan ok, %ld launches, %ld parts\n", launches, parts);
   return 0;
 }
