@@ -132,11 +132,11 @@ def _load():
     lib.efim_decode_step_fp8_table.argtypes = [bp, vp, vp, vp, vp, vp, vp, f64p, i32, i32, f32, f32, f32, vp,
                                                ctypes.c_size_t, vp]
     lib.efim_decode_step_fp8_table.restype = i32
-    lib.efim_norm_rope_append.argtypes = [bp, vp, vp, vp, vp, vp, vp, f32, vp, vp, f64p, i32, i32, vp]
+    lib.efim_norm_rope_append.argtypes = [bp, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, i32, i32, vp]
     lib.efim_norm_rope_append.restype = i32
-    lib.efim_norm_rope_append_fp8.argtypes = [bp, vp, vp, vp, vp, vp, vp, f32, vp, vp, f64p, i32, i32, f32, f32, vp]
+    lib.efim_norm_rope_append_fp8.argtypes = [bp, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, i32, i32, f32, f32, vp]
     lib.efim_norm_rope_append_fp8.restype = i32
-    lib.efim_latent_append.argtypes = [bp, vp, i64, vp, i64, vp, i64, vp, f32, vp, f64p, i32, vp]
+    lib.efim_latent_append.argtypes = [bp, vp, i64, vp, i64, vp, i64, vp, f32, vp, vp, i32, vp]
     lib.efim_latent_append.restype = i32
     lib.efim_latent_workspace_bytes.argtypes = [bp]
     lib.efim_latent_workspace_bytes.restype = ctypes.c_size_t
@@ -416,7 +416,7 @@ def efim_norm_rope_append(batch, q, q_out, k_new, v_new, q_weight, k_weight, nor
     table = _freq_table(inv_freq, rotary_dim)
     _check(_lib.efim_norm_rope_append(ctypes.byref(batch.c), _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new),
                                       _ptr(q_weight), _ptr(k_weight), float(norm_eps), _ptr(k_cache), _ptr(v_cache),
-                                      table.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), int(rotary_dim),
+                                      table.ctypes.data, int(rotary_dim),
                                       int(rope_interleaved), _stream_ptr(stream)),
            "efim_norm_rope_append")
 
@@ -426,7 +426,7 @@ def efim_norm_rope_append_fp8(batch, q, q_out, k_new, v_new, q_weight, k_weight,
     table = _freq_table(inv_freq, rotary_dim)
     _check(_lib.efim_norm_rope_append_fp8(ctypes.byref(batch.c), _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new),
                                           _ptr(q_weight), _ptr(k_weight), float(norm_eps), _ptr(k_cache),
-                                          _ptr(v_cache), table.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                          _ptr(v_cache), table.ctypes.data,
                                           int(rotary_dim), int(rope_interleaved), float(k_scale), float(v_scale),
                                           _stream_ptr(stream)),
            "efim_norm_rope_append_fp8")
@@ -440,7 +440,7 @@ def efim_latent_append(batch, q_rope, q_stride, q_out, q_out_stride, kv_new, kv_
     table = _freq_table(inv_freq, EFIM_LATENT_ROPE)
     _check(_lib.efim_latent_append(ctypes.byref(batch.c), _ptr(q_rope), int(q_stride), _ptr(q_out), int(q_out_stride),
                                    _ptr(kv_new), int(kv_stride), _ptr(norm_weight), float(norm_eps),
-                                   _ptr(latent_cache), table.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                                   _ptr(latent_cache), table.ctypes.data,
                                    int(rope_interleaved), _stream_ptr(stream)),
            "efim_latent_append")
 
