@@ -664,9 +664,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
     if constexpr (!Op::R32) l_run = cross_quarter_sum(l_run);
     l_run = cross_half_sum(l_run);
 
-    // join of the four waves, kCols columns at a time: [wave][row][kCols + 4], and behind them [wave][row] (reference, sum,
-    // largest magnitude, -)
-    constexpr int kCols = 128, kPitch = kCols + 4;
+    // join of the four waves, kStage columns at a time (more of 32 rows cost registers): [wave][row][kStage + 4], and behind them
+    // [wave][row] (reference, sum, largest magnitude, -)
+    constexpr int kCols = 128, kStage = ROWS == 16 ? 512 : 128, kPitch = kStage + 4;
     static_assert(kWaves * ROWS * (kPitch + 4) * 4 <= kZeros, "the join fits the tiles' place");
     float* const joined = reinterpret_cast<float*>(lds);
     f32x4* const s_ml = reinterpret_cast<f32x4*>(joined + kWaves * ROWS * kPitch);
@@ -702,9 +702,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
     if (it.slot >= 0 && my_col == 0 && my_row < it.rows) *reinterpret_cast<f32x4*>(args.part_ml + at * 4) = f32x4{my_m, my_l, my_top * kPartScale, 0.f};
     const float inv = it.slot < 0 ? 1.f / my_l : my_top > 0.f ? 1.f / (my_top * kPartScale) : 0.f;
     uint16_t* const dst = (it.slot < 0 ? out + (it.packed + my_row) * kLatentRank : args.part_o + at * kLatentRank) + my_col;
-    constexpr int kBlocksPerRound = kCols / ROWS;
+    constexpr int kBlocksPerRound = kStage / ROWS;
 #pragma unroll
-    for (int round = 0; round < kLatentRank / kCols; ++round) {
+    for (int round = 0; round < kLatentRank / kStage; ++round) {
       if (round) __syncthreads();
 #pragma unroll
       for (int b = 0; b < kBlocksPerRound; ++b)
@@ -717,7 +717,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
       __syncthreads();
       if (my_row < it.rows) {
 #pragma unroll
-        for (int c = 0; c < kPer; c += 8) {
+        for (int n = 0; n < kStage / kCols * kPer; n += 8) {
+          const int c = n / kPer * kCols + n % kPer;
           f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
           for (int k = 0; k < kWaves; ++k)
@@ -730,7 +731,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
             const float a = x[k >> 1][2 * (k & 1)] * inv, b = x[k >> 1][2 * (k & 1) + 1] * inv;
             words[k] = it.slot < 0 ? pack_bf16(a, b) : pack_f16(a, b);
           }
-          *reinterpret_cast<u32x4*>(dst + round * kCols + c) = words;
+          *reinterpret_cast<u32x4*>(dst + round * kStage + c) = words;
         }
       }
     }
@@ -741,7 +742,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
 // Joins the parts of a tile that several workgroups share: with M = max m, out = sum 2^(m - M) O / sum 2^(m - M) l, in the parts'
 // order.  blockIdx.y stands for the first workgroup whose share begins inside the tile; a wave takes every
 // 4 gridDim.x-th row, eight columns to a lane, eight parts' loads at a time.  A launch and 33 MB of parts 9.6 us, 67 MB and as many
-// outputs 20 us, 4 MB 5 us.
+// outputs 18.5 us, 4 MB 5 us.
 template <int TILE>
 __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args, uint16_t* __restrict__ out) {
   const LatentTable& t = args.table;
@@ -771,8 +772,8 @@ __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args,
   auto slot_of = [&](int s) { return latent_slot(group - 1 + s, s > 0 || together); };
   for (int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); row < rows; row += 4 * gridDim.x) {
     float m = kNoReference, l = 0.f, v[8] = {};
-    constexpr int kGroup = 8;
-    for (int s0 = 0; s0 < parts; s0 += kGroup) {
+    auto add = [&](int s0, auto count) __attribute__((always_inline)) {
+      constexpr int kGroup = decltype(count)::value;  // parts, asked for at once
       f32x4 ml[kGroup];
       u32x4 h[kGroup];
 #pragma unroll
@@ -804,7 +805,10 @@ __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args,
           v[2 * c + 1] += (float)two[1] * scale;
         }
       }
-    }
+    };
+    if (parts == 2) add(0, std::integral_constant<int, 2>());
+    else
+      for (int s0 = 0; s0 < parts; s0 += 8) add(s0, std::integral_constant<int, 8>());
     const float inv = 1.f / l;
     u32x4 words;
 #pragma unroll

@@ -36,7 +36,7 @@ void deal_by_tile(LatentTable* t, int row_tile) {
     all += tiles[r];
   }
   t->by_tile = 0;
-  if (all < 2 || all > t->groups) return;
+  if (all > t->groups) return;
   // the least number of units, at least four, by which the parts are no more than the workgroups
   auto parts_of = [&](int r, int units) {
     const int n = (most[r] + units - 1) / units;
