@@ -425,7 +425,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
         sc = score_products<kAhead, kLast>(
             ka, [&](int n) { return keys.read(n); }, [&](int n) { return qb[n]; },
             [&](int n) __attribute__((always_inline)) {
-              if (n % 2 == 1 && n / 2 < kGroupLoads && fetch) gather.piece(from, n / 2, wave & 1, to);
+              if (n % 4 == 1 && n / 2 < kGroupLoads && fetch) gather.pair(from, n / 2, wave & 1, to);
               if (n >= kLast - kAhead - 4 && n < kLast - kAhead) v.set(op, values_at, n - (kLast - kAhead - 4));
               if (n == kLast - kAhead - 1) v.drop(op, pb_unfit, lds0 + kZeros);
               if (n >= kLast - kAhead) va[n - (kLast - kAhead)] = v.read(n - (kLast - kAhead));

@@ -87,26 +87,27 @@ __device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 1) << 2 |
 struct Gather {
   const char* cache;
   int k1, page_shift, page_mask;
-  uint32_t swizzles;  // two bits for each of the nine loads: the swizzle of the row that this lane's chunk lies in, halved
+  uint32_t swizzles;  // two bits from bit 5 on for each of the nine loads: the swizzle of the row that this lane's chunk lies in, halved
   uint32_t lane16;
 
   __device__ __forceinline__ Gather(const uint16_t* rows, int end, int shift, int lane)
       : cache(reinterpret_cast<const char*>(rows)), k1(end), page_shift(shift), page_mask((1 << shift) - 1), swizzles(0), lane16(lane * 16) {
     asm volatile("" : "+v"(lane));  // (formed where it is used: offsets held from part to part were spilled)
 #pragma unroll
-    for (int j = 0; j < kGroupLoads; ++j) swizzles |= (uint32_t)(swizzle((j * 64 + lane) / kRowChunks) >> 1) << (2 * j);
+    for (int j = 0; j < kGroupLoads; ++j) swizzles |= (uint32_t)(swizzle((j * 64 + lane) / kRowChunks) >> 1) << (5 + 2 * j);
   }
   // (formed again for every tile, as the operands' addresses are)
   __device__ __forceinline__ void forget() { asm volatile("" : "+v"(swizzles), "+v"(lane16)); }
   // byte offset of load j in a group (its multiple of 1 KB aside) whose tile row divided by eight is even or odd
-  __device__ __forceinline__ uint32_t offset(int j, int odd) const { return lane16 ^ (((swizzles >> (2 * j)) & 3) << 5) ^ (odd << 4); }
+  __device__ __forceinline__ uint32_t offset(int j, int odd) const { return ((swizzles >> (2 * j)) & 0x60) ^ (lane16 ^ (odd << 4)); }
   __device__ __forceinline__ const char* row_at(int32_t page, int key) const {
     return cache + (((int64_t)page << page_shift) + (key & page_mask)) * kRowBytes;
   }
   __device__ __forceinline__ bool whole(int key) const { return key + kGroupKeys <= k1; }
-  // load j of a whole group whose first row is at `base`
-  __device__ __forceinline__ void piece(const char* base, int j, int odd, uint32_t to) const {
-    load_to_lds_16(base + j * 1024, offset(j, odd), to + j * 1024);
+  // loads j and j + 1 of a whole group whose first row is at `base`, or the last one
+  __device__ __forceinline__ void pair(const char* base, int j, int odd, uint32_t to) const {
+    if (j + 1 < kGroupLoads) load_to_lds_2x16(base + j * 1024, offset(j, odd), offset(j + 1, odd), to + j * 1024);
+    else load_to_lds_16(base + j * 1024, offset(j, odd), to + j * 1024);
   }
   // group `key` .. key + 7, which is group g of its tile, to LDS at `to`; rows at or behind k1 become copies of the last one's
   __device__ __forceinline__ void group(int key, int g, int32_t page, uint32_t to) const {
