@@ -170,6 +170,23 @@ def test_absorbed_split_over_long_contexts(E, heads, new):
     _close(_absorbed(E, b, q), want, size)
 
 
+@pytest.mark.parametrize("cached,new", [
+    ([9000, 5, 700, 64], [1, 1, 1, 1]),            # parts of one tile each, from one key tile to many
+    ([9000, 0, 700, 64, 2000], [2, 9, 3, 16, 7]),  # several tiles of a request
+    ([3000] * 30, [1] * 30),                       # as many parts for each
+    ([100 * r for r in range(60)], [1 + r % 3 for r in range(60)]),
+    ([0, 0, 4000], [40, 1, 1]),                    # first tiles of fewer key tiles than others have parts
+])
+@pytest.mark.parametrize("heads", [4, 16, 48])
+def test_absorbed_dealt_over_tiles_of_different_lengths(E, cached, new, heads):
+    b = Batch(cached, new, heads, 32, 170 + heads)
+    q = b.gaussian(b.total, heads, ROW)
+    got = _absorbed(E, b, q)
+    want, size = S.latent_attention(b.cached, b.new, b.table, 32, bf16_to_f64(q), b.cache, SCALE)
+    _close(got, want, size)
+    assert np.array_equal(got, _absorbed(E, b, q)), "the same call gives the same bits"
+
+
 @pytest.mark.parametrize("heads", [16, 32, 64])
 def test_absorbed_scores_that_grow_and_sharp_weights(E, heads):
     """Keys whose scores grow along the context move the running reference in almost every tile; large queries leave one weight."""
