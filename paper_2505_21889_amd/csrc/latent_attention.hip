@@ -530,18 +530,18 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
   }
 }
 
-// Items of at most ROWS (16 or 32) query rows: all waves take the same rows, every fourth key tile each, in LDS of their own,
-// and join their results at the end.  Such a step is bound by reading the cache; the waves wait for nothing but their
-// own gathers, so that some load while others compute.  32 requests, 176k keys, 16 heads: 38 us = 5.3 TB/s (45 where the cache
+// Items of at most ROWS (16 or 32) query rows: all waves take the same rows, the key tiles in turn, in LDS of their own, and join
+// their results at the end.  Such a step is bound by reading the cache; the waves wait for nothing but their own gathers, so
+// that some load while others compute; two waves have a second place each and load while they compute.  32 requests, 176k keys, 16 heads: 38 us = 5.3 TB/s (45 where the cache
 // comes from HBM); one request of 2345 keys 11 us.
-template <int ROWS>
-__global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
+template <int ROWS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
                                                                      const uint16_t* __restrict__ cache,
                                                                      const int32_t* __restrict__ block_table,
                                                                      uint16_t* __restrict__ out) {
   using Op = Operands<ROWS>;
   using Acc = typename Op::Acc;
-  constexpr int kAcc = Op::kAcc;
+  constexpr int kAcc = Op::kAcc, kBuffers = kWaves / WAVES;  // of a wave
   __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -554,20 +554,20 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
     const int32_t* pages = block_table + (int64_t)it.rq.req * args.table.max_pages;
     const int ntiles = (it.k1 - it.k0 + kTileKeys - 1) / kTileKeys;
     // (the units are dealt to the waves in turn from one part to the next)
-    const int turn = (wave - (int)(it.next & (kWaves - 1))) & (kWaves - 1);
+    const int turn = (wave - (int)(it.next & (WAVES - 1))) & (WAVES - 1);
     // the n-th tile of the wave; lane 4 n + g holds the page of group g of its tile held_from + n
     const Gather gather(cache, it.k1, page_shift, lane);
-    const uint32_t buf = lds0 + wave * kTileBytes;
-    auto key_of = [&](int n, int g) { return it.k0 + (turn + n * kWaves) * kTileKeys + g * kGroupKeys; };
+    auto buffer = [&](int n) { return lds0 + (wave * kBuffers + n % kBuffers) * kTileBytes; };
+    auto key_of = [&](int n, int g) { return it.k0 + (turn + n * WAVES) * kTileKeys + g * kGroupKeys; };
     auto pages_from = [&](int n) { return pages[min(key_of(n + (lane >> 2), lane & 3), it.k1 - 1) >> page_shift]; };
     int held_from = 0;
     int32_t held = pages_from(0);
     auto fetch = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g)
-        gather.group(key_of(n, g), g, __builtin_amdgcn_readlane(held, (n - held_from) * 4 + g), buf + g * kGroupBytes);
+        gather.group(key_of(n, g), g, __builtin_amdgcn_readlane(held, (n - held_from) * 4 + g), buffer(n) + g * kGroupBytes);
     };
-    const int mine = (ntiles - turn + kWaves - 1) / kWaves;
+    const int mine = (ntiles - turn + WAVES - 1) / WAVES;
     if (mine > 0) fetch(0);
 
     const int i = lane % ROWS, part = lane / ROWS;
@@ -594,7 +594,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
         __builtin_amdgcn_s_waitcnt(0x0F70);
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (kBuffers > 1 && n + 1 < mine) fetch(n + 1);
       op.forget();
+      const uint32_t buf = buffer(n);
       const Keys<ROWS> keys(op, buf);
       float sc[Op::kScores];
       if constexpr (Op::R32) {
@@ -659,7 +661,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
         __builtin_amdgcn_sched_barrier(0);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
-      if (n + 1 < mine) fetch(n + 1);
+      if (kBuffers == 1 && n + 1 < mine) fetch(n + 1);
     }
     if constexpr (!Op::R32) l_run = cross_quarter_sum(l_run);
     l_run = cross_half_sum(l_run);
@@ -667,9 +669,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
     // join of the four waves, kStage columns at a time (more of 32 rows cost registers): [wave][row][kStage + 4], and behind them
     // [wave][row] (reference, sum, largest magnitude, -)
     constexpr int kCols = 128, kStage = ROWS == 16 ? 512 : 128, kPitch = kStage + 4;
-    static_assert(kWaves * ROWS * (kPitch + 4) * 4 <= kZeros, "the join fits the tiles' place");
+    static_assert(WAVES * ROWS * (kPitch + 4) * 4 <= kZeros, "the join fits the tiles' place");
     float* const joined = reinterpret_cast<float*>(lds);
-    f32x4* const s_ml = reinterpret_cast<f32x4*>(joined + kWaves * ROWS * kPitch);
+    f32x4* const s_ml = reinterpret_cast<f32x4*>(joined + WAVES * ROWS * kPitch);
     float top = 0.f;
     if (it.slot >= 0) {
 #pragma unroll
@@ -684,15 +686,15 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
     __syncthreads();
     float m = kNoReference;
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, s_ml[k * ROWS + i][0]);
+    for (int k = 0; k < WAVES; ++k) m = fmaxf(m, s_ml[k * ROWS + i][0]);
     const float f = __builtin_amdgcn_exp2f(m_run - m);
-    constexpr int kThreadsPerRow = 64 * kWaves / ROWS, kPer = kCols / kThreadsPerRow;  // 8 columns, or 16
+    constexpr int kThreadsPerRow = 64 * WAVES / ROWS, kPer = kCols / kThreadsPerRow;  // 8 columns, or 16
     const int my_row = tid / kThreadsPerRow, my_col = tid % kThreadsPerRow * kPer;
     float my_m = kNoReference, my_l = 0.f, my_top = 0.f;
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) my_m = fmaxf(my_m, s_ml[k * ROWS + my_row][0]);
+    for (int k = 0; k < WAVES; ++k) my_m = fmaxf(my_m, s_ml[k * ROWS + my_row][0]);
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
+    for (int k = 0; k < WAVES; ++k) {
       const f32x4 ml = s_ml[k * ROWS + my_row];
       const float weight = __builtin_amdgcn_exp2f(ml[0] - my_m);
       my_l += ml[1] * weight;
@@ -721,7 +723,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_keys_kernel(const Laten
           const int c = n / kPer * kCols + n % kPer;
           f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-          for (int k = 0; k < kWaves; ++k)
+          for (int k = 0; k < WAVES; ++k)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
               x[h] += *reinterpret_cast<const f32x4*>(joined + (k * ROWS + my_row) * kPitch + my_col + c + 4 * h);
@@ -836,15 +838,20 @@ int latent_attention(const efim_batch_t* b, const void* q, const void* cache, vo
   LatentCursor at;
   while (latent_next(b, plan, &at, &args.table)) {
     const unsigned groups = (unsigned)(args.table.groups + kXcds - 1) / kXcds * kXcds;
-    auto launch = [&](auto* kernel, auto* join, int join_groups) {
-      kernel<<<groups, 64 * kWaves, 0, stream>>>(args, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(cache),
+    auto launch = [&](auto* kernel, int waves, auto* join, int join_groups) {
+      kernel<<<groups, 64 * waves, 0, stream>>>(args, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(cache),
                                                  b->block_table, static_cast<uint16_t*>(out));
       if (args.table.groups > 1)
         join<<<dim3(join_groups, args.table.groups - 1), 256, 0, stream>>>(args, static_cast<uint16_t*>(out));
     };
-    if (plan.row_tile == 16) launch(latent_keys_kernel<16>, latent_join_kernel<16>, 4);
-    else if (plan.row_tile == 32) launch(latent_keys_kernel<32>, latent_join_kernel<32>, 8);
-    else launch(latent_rows_kernel, latent_join_kernel<128>, args.table.by_tile ? 32 : 16);  // (many parts of few tiles, or two of each)
+    // 32 rows: four waves where a workgroup has few units, else two that gather a tile while they compute another.  us with four
+    // and two: 32 requests of 1k to 8k keys 58.7 / 56.4, 8 of 4k to 16k 47.7 / 45.1, 200 of 100 to 600 (7 units) 67.9 / 64.4; with
+    // four units one of 2344 keys 23.4 / 24.2, one of 300 20.3 / 21.7.  16 rows compute so little that four are ahead there too (45.8 / 47.7).
+    constexpr int kUnitsForTwo = 6;
+    if (plan.row_tile == 16) launch(latent_keys_kernel<16, 4>, 4, latent_join_kernel<16>, 4);
+    else if (plan.row_tile == 32 && args.table.share < kUnitsForTwo) launch(latent_keys_kernel<32, 4>, 4, latent_join_kernel<32>, 8);
+    else if (plan.row_tile == 32) launch(latent_keys_kernel<32, 2>, 2, latent_join_kernel<32>, 8);
+    else launch(latent_rows_kernel, kWaves, latent_join_kernel<128>, args.table.by_tile ? 32 : 16);  // (many parts of few tiles, or two of each)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }
   }
