@@ -844,12 +844,12 @@ int latent_attention(const efim_batch_t* b, const void* q, const void* cache, vo
       if (args.table.groups > 1)
         join<<<dim3(join_groups, args.table.groups - 1), 256, 0, stream>>>(args, static_cast<uint16_t*>(out));
     };
-    // 32 rows: four waves where a workgroup has few units, else two that gather a tile while they compute another.  us with four
-    // and two: 32 requests of 1k to 8k keys 58.7 / 56.4, 8 of 4k to 16k 47.7 / 45.1, 200 of 100 to 600 (7 units) 67.9 / 64.4; with
+    // 32 rows: four waves where no workgroup has many units, else two that gather a tile while they compute another.  us with four
+    // and two: 32 requests of 1k to 8k keys 58.7 / 56.4, 8 of 4k to 16k 47.7 / 45.1, 200 of 100 to 600 67.9 / 64.4; with
     // four units one of 2344 keys 23.4 / 24.2, one of 300 20.3 / 21.7.  16 rows compute so little that four are ahead there too (45.8 / 47.7).
     constexpr int kUnitsForTwo = 6;
     if (plan.row_tile == 16) launch(latent_keys_kernel<16, 4>, 4, latent_join_kernel<16>, 4);
-    else if (plan.row_tile == 32 && args.table.share < kUnitsForTwo) launch(latent_keys_kernel<32, 4>, 4, latent_join_kernel<32>, 8);
+    else if (plan.row_tile == 32 && args.table.longest < kUnitsForTwo) launch(latent_keys_kernel<32, 4>, 4, latent_join_kernel<32>, 8);
     else if (plan.row_tile == 32) launch(latent_keys_kernel<32, 2>, 2, latent_join_kernel<32>, 8);
     else launch(latent_rows_kernel, kWaves, latent_join_kernel<128>, args.table.by_tile ? 32 : 16);  // (many parts of few tiles, or two of each)
     const hipError_t e = hipGetLastError();

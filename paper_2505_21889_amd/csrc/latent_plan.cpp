@@ -59,6 +59,7 @@ void deal_by_tile(LatentTable* t, int row_tile) {
   }
   if (groups > t->groups || worst >= t->share + (t->longer > 0) + kPartUnits) return;
   t->by_tile = 1;
+  t->longest = worst;
   groups = 0;
   for (int r = 0; r < t->nreq; ++r) {
     const int64_t n = parts_of(r, low);
@@ -112,6 +113,7 @@ bool latent_next(const efim_batch_t* b, const LatentPlan& plan, LatentCursor* at
   if (t->nreq == 0) return false;
   t->share = t->units / t->groups;
   t->longer = (int32_t)(t->units - t->share * t->groups);
+  t->longest = t->share + (t->longer > 0);
   deal_by_tile(t, plan.row_tile);
   return true;
 }

@@ -42,6 +42,7 @@ struct LatentTable {
   int32_t longer;
   int32_t groups;      // workgroups with a share
   int32_t by_tile;     // how they are dealt
+  int64_t longest;     // units of the longest share
   int32_t nreq;
   int32_t heads;
   int32_t max_pages;

@@ -52,7 +52,7 @@ int main() {
       by_tile += t.by_tile;
       int group = 0, of_group = 0;       // the workgroup at hand, and how many parts of it are done
       std::vector<int> used(plan.slots, 0);
-      int64_t unit = 0;
+      int64_t unit = 0, longest = t.by_tile ? 0 : t.share + (t.longer > 0);
       for (int k = 0; k < t.nreq; ++k) {
         const LatentReq& q = t.req[k];
         while (fresh[expect] == 0) ++expect;
@@ -70,6 +70,7 @@ int main() {
           for (int j = 0; j < n; ++j, ++group) {
             const int from = LatentTable::first_of(units, n, j), to = LatentTable::first_of(units, n, j + 1);
             CHECK(from < to && (j > 0 || from == 0) && (j < n - 1 || to == units));
+            if (to - from > longest) longest = to - from;
             if (n > 1) {
               ++parts;
               const int slot = latent_slot(group, true);
@@ -98,7 +99,7 @@ int main() {
         row += q.new_len;
         ++expect;
       }
-      CHECK(unit == t.units && group == (t.by_tile ? t.groups : t.groups - 1));
+      CHECK(unit == t.units && longest == t.longest && group == (t.by_tile ? t.groups : t.groups - 1));
     }
     CHECK(row == total);
 
