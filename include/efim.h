@@ -287,7 +287,7 @@ int efim_norm_rope_append_fp8(const efim_batch_t* batch, const void* q, void* q_
  * The cache holds the rows:  latent_cache  DEVICE bf16 [num_pages, P, 576].
  *
  * batch: as for the other calls with num_kv_heads = 1 and head_dim = 576; num_q_heads (H) 1 .. 256,
- * any number.  EFIM_ERR_UNSUPPORTED for other head layouts.
+ * any number.  EFIM_ERR_UNSUPPORTED for other head layouts and for more than 2^30 query rows (T * H).
  * None of these calls keeps host state and all launch only kernels: they may be captured into a HIP graph.
  * ------------------------------------------------------------------------------------- */
 

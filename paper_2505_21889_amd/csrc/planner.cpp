@@ -73,7 +73,11 @@ int validate_latent_batch(const efim_batch_t* b, int64_t* total_new) {
   if (rc != EFIM_OK) return rc;
   if (b->num_kv_heads != 1 || b->head_dim != kLatentRow || b->num_q_heads > kMaxLatentHeads) return EFIM_ERR_UNSUPPORTED;
   if (!page_size_ok(b->page_size)) return EFIM_ERR_UNSUPPORTED;
-  return validate_lengths(b, total_new);
+  int64_t total = 0;
+  const int lengths = validate_lengths(b, &total);
+  if (total_new) *total_new = total;
+  if (lengths != EFIM_OK) return lengths;
+  return total * b->num_q_heads > (int64_t)1 << 30 ? EFIM_ERR_UNSUPPORTED : EFIM_OK;  // (rows are counted in 32 bits)
 }
 
 namespace {

@@ -117,6 +117,17 @@ def test_latent_refusals():
     assert _expand(_desc([1 << 29], [1], 256, page=256, max_pages=1 << 22, num_pages=1 << 22)) == UNSUPPORTED
 
 
+def test_latent_rows_are_counted_in_32_bits():
+    def rows(new, heads):
+        return _desc([0] * len(new), new, heads, page=256, max_pages=1 << 22, num_pages=1 << 22)
+
+    for new, heads in (([1 << 23], 256), ([1 << 22] * 2, 256), ([(1 << 22) + 1], 256)):
+        for call in (_attend, _expand):
+            assert call(rows(new, heads)) == UNSUPPORTED
+        assert E.efim_latent_workspace_bytes(rows(new, heads)) == 0 == E.efim_latent_expanded_workspace_bytes(rows(new, heads))
+    assert E.efim_latent_workspace_bytes(rows([1 << 22], 256)) > 256
+
+
 def _verify(counts=(2, 1), batch=None, vocab=100, t=FAKE, ts=100, d=FAKE, ds=100, tok=FAKE, u=FAKE, out=FAKE, acc=FAKE, ws=FAKE, nbytes=1 << 30, drafts=True):
     arr = np.asarray(counts, np.int32)
     return E.raw_library().efim_verify_drafts(len(counts) if batch is None else batch, arr.ctypes.data if drafts else None, vocab,
