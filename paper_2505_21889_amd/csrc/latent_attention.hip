@@ -87,14 +87,16 @@ __device__ __forceinline__ Place find_tile(const LatentTable& t, const Requests&
   return at;
 }
 
-// A workgroup's share of the units, a tile's part at a time.
+// A workgroup's share of the units, a tile's part at a time, the last one first: where a share is about a tile, its last part
+// begins at its tile's first key and its first part goes on from about the key where that one ends, so that the workgroups of
+// a request are at the same keys at a time and gather them from their XCD's L2.
 template <int TILE>
 struct Share {
   const LatentTable& t;
   Place at;
   int group;
-  int64_t next, end;   // units
-  bool first;
+  int64_t begin, end;  // units that are left
+  int64_t next;        // the part's first
   // the part at hand
   LatentReq rq;
   int row0, rows;      // of the request
@@ -106,9 +108,8 @@ struct Share {
     const Requests requests(table, lane);
     // an XCD takes neighbouring shares, which have rows of the cache in common
     group = (int)(blockIdx.x % kXcds) * (int)(gridDim.x / kXcds) + (int)(blockIdx.x / kXcds);
-    next = end = 0;
+    begin = end = 0;
     if (group >= t.groups) return;
-    first = true;
     if (t.by_tile) {
       at.r = requests.find_group(group, lane);
       rq = requests.get(at.r);
@@ -116,38 +117,38 @@ struct Share {
       at.tile = k / n;
       at.units = latent_units_of(rq, t.heads, TILE, at.tile);
       at.first = 0;
-      next = LatentTable::first_of(at.units, n, k - at.tile * n);
+      begin = LatentTable::first_of(at.units, n, k - at.tile * n);
       end = LatentTable::first_of(at.units, n, k - at.tile * n + 1);
-      part();
-      return;
+    } else {
+      begin = t.first_unit(group);
+      end = t.first_unit(group + 1);
+      at = find_tile<TILE>(t, requests, end - 1, lane);
+      rq = requests.get(at.r);
     }
-    next = t.first_unit(group);
-    end = t.first_unit(group + 1);
-    at = find_tile<TILE>(t, requests, next, lane);
-    rq = requests.get(at.r);
     part();
   }
-  __device__ __forceinline__ bool done() const { return next >= end; }
+  __device__ __forceinline__ bool done() const { return end <= begin; }
   __device__ __forceinline__ void part() {
     row0 = at.tile * TILE;
     rows = latent_rows_of(rq, t.heads, TILE, at.tile);
-    const int u0 = (int)(next - at.first), u1 = (int)min((int64_t)at.units, end - at.first);
+    const bool first = begin >= at.first;
+    const int u0 = first ? (int)(begin - at.first) : 0, u1 = (int)(end - at.first);
+    next = at.first + u0;
     k0 = u0 * kTileKeys;
     k1 = min(u1 * kTileKeys, latent_keys_of(rq, t.heads, TILE, at.tile));
     slot = u0 == 0 && u1 == at.units ? -1 : latent_slot(group, first);
     packed = (int64_t)rq.row_start * t.heads + row0;
   }
   __device__ __forceinline__ void advance() {
-    first = false;
-    next = at.first + at.units;
+    end = at.first;
     if (done()) return;
-    at.first = next;
-    ++at.tile;
-    if (at.tile == latent_tiles(rq, t.heads, TILE)) {
-      rq = t.req[++at.r];
-      at.tile = 0;
+    if (at.tile == 0) {
+      rq = t.req[--at.r];
+      at.tile = latent_tiles(rq, t.heads, TILE);
     }
+    --at.tile;
     at.units = latent_units_of(rq, t.heads, TILE, at.tile);
+    at.first = end - at.units;
     part();
   }
 };
@@ -325,7 +326,7 @@ __device__ __forceinline__ void write_rows(const f32x16 (&o)[16], char* staged, 
 // No maximum is formed on the way: the reference is the row's maximum over the part's first key tile, and moves where a tile's
 // sum of probabilities tells that one of them passed 2^kSlack.
 // A tile takes 3.7k cycles, 2.2k of them products; a part's queries in and outputs out 20 to 25k.  32 requests of 128 rows, 88k keys:
-// 42 us; 1014 tokens of 28 heads over 164k keys: 320 us = 0.99 PFLOP/s, products 48 % of the cycles.
+// 42 us; 1014 tokens of 28 heads over 164k keys: 312 us = 1.01 PFLOP/s, products 49 % of the cycles (371 on a hot card).
 __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
                                                                      const uint16_t* __restrict__ cache,
                                                                      const int32_t* __restrict__ block_table,
