@@ -43,8 +43,8 @@ struct LatentArgs {
   LatentTable table;
   float scale_log2;  // sm_scale * log2(e)
   // Partial results of the ranges of split tiles, [slot][row tile]: the unnormalised output O as binary16 values O / a with
-  // a = 2^-15 max |O| over the row, and (reference in log2 units, sum, a, -).  Half the bytes of fp32; what is within 2^-29 of
-  // the row's largest keeps 11 significant bits, a fraction of what the output's own rounding to bf16 costs.
+  // a = 2^-15 max |O| over the row (2^-126 at least), and (reference in log2 units, sum, a, -).  Half the bytes of fp32; what
+  // is within 2^-29 of the row's largest keeps 11 significant bits, a fraction of what the output's own rounding to bf16 costs.
   uint16_t* part_o;
   float* part_ml;
 };
@@ -153,7 +153,10 @@ struct Share {
   }
 };
 
+// The scale of a partial result whose largest magnitude is `top`: never below fp32's least normal number, so that its
+// reciprocal is finite.  Rows of less than 2^-111 are then stored as less than 2^15; fp32's normal numbers keep their 11 bits.
 constexpr float kPartScale = 0x1p-15f;
+__device__ __forceinline__ float part_scale(float top) { return fmaxf(top * kPartScale, 0x1p-126f); }
 constexpr float kOver = 256.f;  // 2^kSlack: a sum of rounded probabilities is never below its largest one
 constexpr int kZeros = kWaves * kTileBytes;  // 1 KB of zeros behind the tiles, in place of values that are not finite
 constexpr int kLdsBytes = kZeros + 1024;
@@ -519,8 +522,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
         for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(o[d][r]));
       top = cross_half_max(top);
       const int64_t at = (int64_t)it.slot * TILE + wave * 32;
-      if (i < mine && part == 0) *reinterpret_cast<f32x4*>(args.part_ml + (at + i) * 4) = f32x4{m_run, l_run, top * kPartScale, 0.f};
-      write_rows(o, staged, args.part_o + at * kLatentRank, top > 0.f ? 1.f / (top * kPartScale) : 0.f, lane, mine,
+      if (i < mine && part == 0) *reinterpret_cast<f32x4*>(args.part_ml + (at + i) * 4) = f32x4{m_run, l_run, part_scale(top), 0.f};
+      write_rows(o, staged, args.part_o + at * kLatentRank, 1.f / part_scale(top), lane, mine,
                  [](float a, float b) { return pack_f16(a, b); });
     } else {
       write_rows(o, staged, out + (it.packed + wave * 32) * kLatentRank, 1.f / l_run, lane, mine,
@@ -702,8 +705,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
       my_top += ml[2] * weight;  // (no sum of the four is larger)
     }
     const int64_t at = (int64_t)it.slot * ROWS + my_row;
-    if (it.slot >= 0 && my_col == 0 && my_row < it.rows) *reinterpret_cast<f32x4*>(args.part_ml + at * 4) = f32x4{my_m, my_l, my_top * kPartScale, 0.f};
-    const float inv = it.slot < 0 ? 1.f / my_l : my_top > 0.f ? 1.f / (my_top * kPartScale) : 0.f;
+    if (it.slot >= 0 && my_col == 0 && my_row < it.rows) *reinterpret_cast<f32x4*>(args.part_ml + at * 4) = f32x4{my_m, my_l, part_scale(my_top), 0.f};
+    const float inv = 1.f / (it.slot < 0 ? my_l : part_scale(my_top));
     uint16_t* const dst = (it.slot < 0 ? out + (it.packed + my_row) * kLatentRank : args.part_o + at * kLatentRank) + my_col;
     constexpr int kBlocksPerRound = kStage / ROWS;
 #pragma unroll
