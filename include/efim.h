@@ -320,7 +320,8 @@ int efim_latent_append(const efim_batch_t* batch, const void* q_rope, int64_t q_
  *   workspace DEVICE, 256-byte aligned, at least efim_latent_workspace_bytes(batch) bytes, contents irrelevant; not to
  *             be used by an overlapping call
  * Scores and sums are fp32; probabilities enter the second product as bf16.  A row's result does not depend on the run, only
- * on the batch.  Slots at or beyond C_r + N_r may hold anything.
+ * on the batch.  Slots at or beyond C_r + N_r may hold anything.  Infinities and NaN in rows that a query row does not see leave
+ * it as it is; where it sees them it gets what the formula gives.
  * efim_latent_workspace_bytes is a pure host function: at least 256, 0 for an invalid batch.
  */
 size_t efim_latent_workspace_bytes(const efim_batch_t* batch);

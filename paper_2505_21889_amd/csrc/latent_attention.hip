@@ -159,7 +159,8 @@ constexpr float kPartScale = 0x1p-15f;
 __device__ __forceinline__ float part_scale(float top) { return fmaxf(top * kPartScale, 0x1p-126f); }
 constexpr float kOver = 256.f;  // 2^kSlack: a sum of rounded probabilities is never below its largest one
 constexpr int kZeros = kWaves * kTileBytes;  // 1 KB of zeros behind the tiles, in place of values that are not finite
-constexpr int kLdsBytes = kZeros + 1024;
+constexpr int kTornAt = kZeros + 1024;      // a word for each wave: whether it left a key out
+constexpr int kLdsBytes = kTornAt + 4 * kWaves;
 
 // LDS addresses of a wave's operands in a tile at 0.  The low bits of a chunk take part in the swizzle and need an address
 // each, all else goes into the offset field of the read.
@@ -269,16 +270,28 @@ __device__ __forceinline__ f32x16 score_products(bf16x8 (&ahead)[AHEAD], Key key
 __device__ __forceinline__ void await_scores(f32x16& acc) { asm volatile("s_nop %1" : "+v"(acc) : "n"(kScoreStates)); }
 
 // Masks the scores of the tile whose first key is key0 for a row that sees keys in front of `visible`; returns its unfit keys.
+// Where there are some, sets the word at `torn`.
 // R32: element r of lane i, half `part` is key (r / 4) * 8 + part * 4 + r % 4; R16: (r / 4) * 16 + part * 4 + r % 4.
 template <int ROWS, int N>
-__device__ __forceinline__ uint32_t mask_scores(float (&sc)[N], int key0, int visible, int part) {
+__device__ __forceinline__ uint32_t mask_scores(float (&sc)[N], int key0, int visible, int part, uint32_t torn) {
   const uint32_t unfit = unfit_keys<ROWS>(sc);
+  auto place = [&](int r) { return (r >> 2) * (ROWS == 32 ? 8 : 16) + part * 4 + (r & 3); };
+  if (unfit) *(LDS_PTR(uint32_t))(uintptr_t)torn = 1;
 #pragma unroll
-  for (int r = 0; r < N; ++r) {
-    const int key = key0 + (r >> 2) * (ROWS == 32 ? 8 : 16) + part * 4 + (r & 3);
-    sc[r] = key < visible ? sc[r] : -__builtin_inff();
-  }
+  for (int r = 0; r < N; ++r) sc[r] = key0 + place(r) < visible ? sc[r] : -__builtin_inff();
   return unfit;
+}
+
+// Torn columns.  A row that sees an unfit key at a score of minus infinity has no weight for it, and zero times an infinite
+// value is no number; but the key's row was left out.  So where a key was left out the outputs, once written, lose their numbers
+// in the columns in which a key that the row sees is not finite: 0x7FFF is no number, in bf16 as in binary16.  (In the weightless
+// key's infinite columns, that is, and at any other score the whole row has none.)  Of eight columns of a key:
+__device__ __forceinline__ u32x4 torn_columns(const Gather& gather, const int32_t* pages, int key, int column) {
+  u32x4 v = *reinterpret_cast<const u32x4*>(gather.row_at(pages[key >> gather.page_shift], key) + column * 2);
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    v[c] = ((v[c] & 0x7F80u) == 0x7F80u ? 0x7FFFu : 0u) | ((v[c] & 0x7F800000u) == 0x7F800000u ? 0x7FFF0000u : 0u);
+  return v;
 }
 template <int ROWS, int N>
 __device__ __forceinline__ float row_max(const float (&sc)[N]) {
@@ -389,6 +402,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
     for (int d = 0; d < Op::kBlocks; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    const uint32_t torn = lds0 + kTornAt + 4 * wave;
+    *(LDS_PTR(uint32_t))(uintptr_t)torn = 0;
     float m_run = kNoReference, l_run = 0.f;
     u32x4 pb[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, pn[2];  // probabilities of the tile in front and of the one at hand, as operands
     uint32_t unfit = 0, pb_unfit = ~0u;                  // (in front of the first there is none)
@@ -441,7 +456,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
           float x[16];
 #pragma unroll
           for (int r = 0; r < 16; ++r) x[r] = sc[r];
-          unfit = mask_scores<32>(x, key0, visible, part);
+          unfit = mask_scores<32>(x, key0, visible, part, torn);
           if (tile == 0) m_run = fmaxf(row_max<32>(x) * args.scale_log2, kNoReference);
 #pragma unroll
           for (int r = 0; r < 16; ++r) sc[r] = x[r];
@@ -529,6 +544,24 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
       write_rows(o, staged, out + (it.packed + wave * 32) * kLatentRank, 1.f / l_run, lane, mine,
                  [](float a, float b) { return pack_bf16(a, b); });
     }
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(*(LDS_PTR(uint32_t))(uintptr_t)torn) != 0, 0)) {
+      int own = lane;
+      asm volatile("" : "+v"(own));  // (its addresses are formed here: held from part to part they were spilled)
+      uint16_t* const to = it.slot >= 0 ? args.part_o + ((int64_t)it.slot * TILE + wave * 32) * kLatentRank : out + (it.packed + wave * 32) * kLatentRank;
+      u32x4 marks = {0, 0, 0, 0};
+      int key = it.k0;
+#pragma unroll 1
+      for (int n = 0; n < mine; ++n) {
+        const int end = min(it.k1, it.rq.cached + (it.row0 + wave * 32 + n) / heads + 1);
+        while (key < end) {
+          marks |= torn_columns(gather, pages, key, own * 8);
+          // (the tiles that were masked: the first and those that some row does not see whole)
+          ++key;
+          if (key == it.k0 + kTileKeys) key = max(key, least & -kTileKeys);
+        }
+        *reinterpret_cast<u32x4*>(to + (int64_t)n * kLatentRank + own * 8) |= marks;
+      }
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's place is read
     __syncthreads();
   }
@@ -587,6 +620,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
     for (int d = 0; d < Op::kBlocks; ++d)
 #pragma unroll
       for (int r = 0; r < kAcc; ++r) o[d][r] = 0.f;
+    const uint32_t torn = lds0 + kTornAt;
+    *(LDS_PTR(uint32_t))(uintptr_t)(torn + 4 * wave) = 0;
     float m_run = kNoReference, l_run = 0.f;
     constexpr int kAhead = 6;
     __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -631,7 +666,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
       }
       uint32_t unfit = 0;
       const int key0 = key_of(n, 0);
-      if (key0 + kTileKeys > least) unfit = mask_scores<ROWS>(sc, key0, visible, part);
+      if (key0 + kTileKeys > least) unfit = mask_scores<ROWS>(sc, key0, visible, part, torn + 4 * wave);
       const float mx = row_max<ROWS>(sc) * args.scale_log2;
       if (__any(mx > m_run + kSlack)) {
         const float m_new = mx > m_run + kSlack ? mx : m_run;
@@ -739,6 +774,20 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
           }
           *reinterpret_cast<u32x4*>(dst + round * kStage + c) = words;
         }
+      }
+    }
+    uint32_t some = 0;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) some |= *(LDS_PTR(uint32_t))(uintptr_t)(torn + 4 * k);
+    if (__builtin_amdgcn_readfirstlane(some) && my_row < it.rows) {
+      const int end = min(it.k1, it.rq.cached + (it.row0 + my_row) / heads + 1);
+#pragma unroll 1
+      for (int n = 0; n < kLatentRank / kCols * kPer; n += 8) {
+        const int c = n / kPer * kCols + n % kPer;
+        u32x4 marks = {0, 0, 0, 0};
+#pragma unroll 1
+        for (int key = max(it.k0, least & -kTileKeys); key < end; ++key) marks |= torn_columns(gather, pages, key, my_col + c);
+        *reinterpret_cast<u32x4*>(dst + c) |= marks;
       }
     }
     __syncthreads();  // what was joined has been read

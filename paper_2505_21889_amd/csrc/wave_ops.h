@@ -162,8 +162,9 @@ __device__ __forceinline__ void load_coherent(const float* at, float* a, float* 
 // A key whose row is not finite must not reach, as zero times infinity, the outputs of rows that do not see it.  Where a
 // tile holds keys that some row of the wave does not see, `unfit_keys` names those whose scores are finite for none of
 // the rows (as bits of the tile's 32 keys; a query row that is not finite makes its own scores so, not the others').  The
-// value product then takes zeros in place of their rows.  A row that does see such a key has a score, and so a weight,
-// that is no number, and keeps it.
+// value product then takes zeros in place of their rows.  A row that does see such a key and has it at plus infinity or no
+// number gets a weight that is no number, and keeps that.  At minus infinity its weight is zero: the caller has to see to it
+// that the key's infinite values still leave the row no numbers.
 // ROWS 32: element r is key (r / 4) * 8 + lane / 32 * 4 + r % 4; ROWS 16: key (r / 4) * 16 + lane / 16 * 4 + r % 4.
 template <int ROWS, int N>
 __device__ __forceinline__ uint32_t unfit_keys(const float (&scores)[N]) {

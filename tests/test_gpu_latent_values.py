@@ -1,10 +1,11 @@
-"""The latent attention on values at the ends of bf16."""
+"""The latent attention on values at the ends of bf16: what a row that sees an infinite key gets, by the definition in 64 bits,
+wherever the key lies, what a row that does not see it gets, and values so small that their parts' scale is at the end of fp32."""
 import numpy as np
 import pytest
 import torch
 
 from latent_shapes import ROUTES
-from latent_util import LATENT, ROW, Shared, absorbed
+from latent_util import LATENT, ROW, Shared, absorbed, assert_close, attend
 from oracle.efim_oracle import bf16_to_f64, f64_to_bf16
 from paper_2505_21889_amd import workloads as W
 
@@ -31,3 +32,56 @@ def test_absorbed_values_near_the_least_number(E, name, size):
     values = bf16_to_f64(rows)[:, :LATENT]
     want = (np.cumsum(values, 0) / np.arange(1, len(values) + 1)[:, None])[b.visible() - 1]  # (scores below 1e-27 are zero)
     assert np.all(np.abs(got - want[:, None]) <= 2.0 ** -7 * want[:, None])
+
+
+def _places(cached, new):
+    """Of request 0: a key of its first range, one in the middle, the last in the cache, and of the new ones the first, the last but
+    one and the last."""
+    c, n = cached[0], new[0]
+    return sorted({3, c // 2, c // 2 + 33, max(c - 1, 0), c, c + n - 2, c + n - 1} & set(range(c + n)))
+
+
+def _check(got, clean, sees, above, columns, want, size):
+    """got, clean, want, size [rows, d]; sees, above [rows]: whether the row sees the infinite key, and has it for its maximum.
+    columns: of the values, those that are infinite in the key."""
+    assert np.array_equal(got[~sees], clean[~sees]), "rows that do not see the key"
+    assert np.all(np.isnan(bf16_to_f64(got[sees & above]))), "infinity less infinity"
+    below = sees & ~above
+    assert np.all(np.isnan(bf16_to_f64(got[below][:, columns]))), "no weight times infinity"
+    others = np.setdiff1d(np.arange(got.shape[1]), columns)
+    if len(others) and below.any():
+        assert_close(got[below][:, others], want[below][:, others], size[below][:, others])
+
+
+@pytest.mark.parametrize("column", [7, 300, 530])
+@pytest.mark.parametrize("name", ["rows16", "rows32", "rows32_two_waves", "rows128", "rows128_even"])
+def test_absorbed_one_infinity_in_a_key(E, name, column):
+    """A score of minus infinity is no weight, and no weight times an infinite value is no number: in its column alone."""
+    heads, cached, new = ROUTES[name][:3]
+    rng = np.random.default_rng(9)
+    rows = W.gaussian_bf16(rng, (max(np.add(cached, new)), ROW), 1.0)
+    q = W.gaussian_bf16(rng, (sum(new), heads, ROW), 1.0)
+    b = Shared(cached, new, rows, 10)
+    visible = np.repeat(b.visible(), heads)
+    # rows of request 0, and in front of its end those that see its last keys
+    at = np.unique(np.concatenate([np.arange(new[0] * heads)[-80:], rng.integers(0, new[0] * heads, 60)]))
+    q[:, :, column] = np.where(q[:, :, column] & 0x7FFF == 0, 0x3F80, q[:, :, column])
+    clean = absorbed(E, b, q).reshape(-1, LATENT)
+    q64 = bf16_to_f64(q).reshape(-1, ROW)
+    for key in _places(cached, new):
+        for bits in (0x7F80, 0xFF80):
+            bad = rows.copy()
+            bad[key, column] = bits
+            got = absorbed(E, Shared(cached, new, bad, 10), q).reshape(-1, LATENT)
+            sees, above = visible > key, (q64[:, column] > 0) == (bits == 0x7F80)
+            keys = np.where(np.arange(len(rows))[:, None] == key, 0.0, bf16_to_f64(rows))[:cached[0] + new[0]]
+            alone = visible[at] > 1  # (a row with no other key has no number anywhere)
+            want, size = attend(q64[at[alone]], visible[at[alone]], keys, keys[:, :LATENT], without=[key])
+            _check(got[at[alone]], clean[at[alone]], sees[at[alone]], above[at[alone]], [column] if column < LATENT else [], want, size)
+            # every row of every request: what is a number
+            nan = np.isnan(bf16_to_f64(got))
+            expect = np.zeros_like(nan)
+            expect[sees & (above | (visible == 1))] = True
+            if column < LATENT:
+                expect[sees, column] = True
+            assert not np.any(nan != expect), (key, bits)
