@@ -337,7 +337,7 @@ int efim_latent_attention(const efim_batch_t* batch, const void* q, const void* 
  *   out       DEVICE bf16 [T, H, 128]   must not alias q, w_kv or the cache
  *   workspace as above, efim_latent_expanded_workspace_bytes(batch) bytes: the expanded keys and values of all requests with
  *             new tokens, 640 bytes a key and head (0: an invalid batch or one beyond a launch's reach)
- * Expanded keys and values are rounded to bf16; all sums are fp32.
+ * Expanded keys and values are rounded to bf16; all sums are fp32.  Infinities and NaN as above.
  */
 size_t efim_latent_expanded_workspace_bytes(const efim_batch_t* batch);
 int efim_latent_attention_expanded(const efim_batch_t* batch, const void* q, const void* latent_cache,

@@ -282,16 +282,9 @@ __device__ __forceinline__ uint32_t mask_scores(float (&sc)[N], int key0, int vi
   return unfit;
 }
 
-// Torn columns.  A row that sees an unfit key at a score of minus infinity has no weight for it, and zero times an infinite
-// value is no number; but the key's row was left out.  So where a key was left out the outputs, once written, lose their numbers
-// in the columns in which a key that the row sees is not finite: 0x7FFF is no number, in bf16 as in binary16.  (In the weightless
-// key's infinite columns, that is, and at any other score the whole row has none.)  Of eight columns of a key:
+// Marks of eight columns of a key.
 __device__ __forceinline__ u32x4 torn_columns(const Gather& gather, const int32_t* pages, int key, int column) {
-  u32x4 v = *reinterpret_cast<const u32x4*>(gather.row_at(pages[key >> gather.page_shift], key) + column * 2);
-#pragma unroll
-  for (int c = 0; c < 4; ++c)
-    v[c] = ((v[c] & 0x7F80u) == 0x7F80u ? 0x7FFFu : 0u) | ((v[c] & 0x7F800000u) == 0x7F800000u ? 0x7FFF0000u : 0u);
-  return v;
+  return torn_marks(*reinterpret_cast<const u32x4*>(gather.row_at(pages[key >> gather.page_shift], key) + column * 2));
 }
 template <int ROWS, int N>
 __device__ __forceinline__ float row_max(const float (&sc)[N]) {
@@ -544,6 +537,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
       write_rows(o, staged, out + (it.packed + wave * 32) * kLatentRank, 1.f / l_run, lane, mine,
                  [](float a, float b) { return pack_bf16(a, b); });
     }
+    // torn columns, over what was written
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(*(LDS_PTR(uint32_t))(uintptr_t)torn) != 0, 0)) {
       int own = lane;
       asm volatile("" : "+v"(own));  // (its addresses are formed here: held from part to part they were spilled)
@@ -776,6 +770,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
         }
       }
     }
+    // torn columns, over what this thread wrote
     uint32_t some = 0;
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) some |= *(LDS_PTR(uint32_t))(uintptr_t)(torn + 4 * k);

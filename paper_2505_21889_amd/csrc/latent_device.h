@@ -70,6 +70,20 @@ struct Requests {
   }
 };
 
+// Torn columns.  A row that sees an unfit key (unfit_keys) at a score of minus infinity has no weight for it, and zero times
+// an infinite value is no number; but the key was left out.  So where a wave left a key out its outputs, once formed, lose their
+// numbers in the columns in which the value of a key that the row sees is not finite.  (In the weightless key's infinite
+// columns, that is; at any other score the whole row has none.)  The marks are laid over outputs: 0x7FFF, no number in
+// bf16 as in binary16, for each of eight values that is not finite.
+typedef uint32_t torn_words __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ torn_words torn_marks(torn_words values) {
+  torn_words marks;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    marks[c] = ((values[c] & 0x7F80u) == 0x7F80u ? 0x7FFFu : 0u) | ((values[c] & 0x7F800000u) == 0x7F800000u ? 0x7FFF0000u : 0u);
+  return marks;
+}
+
 // --- tiles of cache rows in LDS ------------------------------------------------------------------------------------------------
 constexpr int kRowBytes = kLatentRow * 2;
 constexpr int kRowChunks = kRowBytes / 16;

@@ -341,13 +341,16 @@ __global__ __launch_bounds__(64 * kTeam * GROUPS, 2) void expanded_attention_ker
                                                                                     uint16_t* __restrict__ out) {
   constexpr int kKeyLoads = kHalfKeys / 1024 / kTeam, kValueLoads = kHalfValues / 1024 / kTeam;  // a wave's, of a half
   constexpr int kZeros = GROUPS * kTeamBytes;  // what a key that is to be left out has for a value
-  __shared__ __attribute__((aligned(1024))) char lds[kZeros + 1024];
+  constexpr int kTornAt = kZeros + 1024;       // a word for each wave: whether it left a key out
+  __shared__ __attribute__((aligned(1024))) char lds[kTornAt + 4 * kTeam * GROUPS];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int set = wave % kTeam, group = wave / kTeam;
   const uint32_t zeros = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + kZeros;
   const uint32_t base = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + group * kTeamBytes;
   *reinterpret_cast<u32x4*>(lds + kZeros + lane * 16) = u32x4{0, 0, 0, 0};  // (by every wave: it reads behind its own writes)
+  const uint32_t torn = zeros + 1024;
+  *(LDS_PTR(uint32_t))(uintptr_t)(torn + 4 * wave) = 0;
   const ExpandedTable& t = args.table;
   const int heads = t.heads;
   const int at = blockIdx.x / heads, head = blockIdx.x - at * heads;
@@ -576,6 +579,7 @@ __global__ __launch_bounds__(64 * kTeam * GROUPS, 2) void expanded_attention_ker
 #pragma unroll
       for (int e = 0; e < 16; ++e) raw[e] = sc[e];
       unfit = unfit_keys<32>(raw);
+      if (unfit) *(LDS_PTR(uint32_t))(uintptr_t)(torn + 4 * wave) = 1;
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (key0 + (e >> 2) * 8 + part * 4 + (e & 3) >= visible) sc[e] = -__builtin_inff();
@@ -643,6 +647,23 @@ __global__ __launch_bounds__(64 * kTeam * GROUPS, 2) void expanded_attention_ker
       }
       *reinterpret_cast<u32x2*>(staged + i * kOutPitch + (d * 32 + e4 * 8 + part * 4) * 2) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     }
+  // torn columns
+  uint32_t some = *(LDS_PTR(uint32_t))(uintptr_t)(torn + 4 * set);
+  if constexpr (GROUPS == 2) some |= *(LDS_PTR(uint32_t))(uintptr_t)(torn + 4 * (kTeam + set));
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(some) != 0, 0)) {
+    const int chunk = lane & 15;
+    u32x4 marks = {0, 0, 0, 0};
+    int key = least & -32;  // (the halves that were masked)
+#pragma unroll 1
+    for (int row = lane >> 4; row < 32; row += 4) {
+      const int end = rq.cached + row0 + min(set * 32 + row, rows - 1) + 1;
+      for (; key < end; ++key) {
+        const char* const value = src + (int64_t)(key / kTileKeys) * kTileBytes + kKeysBytes + (key % kTileKeys) * kValueBytes;
+        marks |= torn_marks(*reinterpret_cast<const u32x4*>(value + ((chunk ^ value_swizzle(key)) << 4)));
+      }
+      *reinterpret_cast<u32x4*>(staged + row * kOutPitch + chunk * 16) |= marks;
+    }
+  }
   uint16_t* dst = out + ((packed + set * 32) * heads + head) * kLatentValue;
 #pragma unroll
   for (int row4 = 0; row4 < 32; row4 += 4) {

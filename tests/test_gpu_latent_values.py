@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from latent_shapes import ROUTES
-from latent_util import LATENT, ROW, Shared, absorbed, assert_close, attend
+from latent_util import LATENT, ROW, Shared, absorbed, assert_close, attend, expanded
 from oracle.efim_oracle import bf16_to_f64, f64_to_bf16
 from paper_2505_21889_amd import workloads as W
 
@@ -85,3 +85,40 @@ def test_absorbed_one_infinity_in_a_key(E, name, column):
             if column < LATENT:
                 expect[sees, column] = True
             assert not np.any(nan != expect), (key, bits)
+
+
+@pytest.mark.parametrize("heads,cached,new", [(3, [100], [140]), (2, [0], [300]), (48, [20], [1500])])
+def test_expanded_one_infinity_in_a_key(E, heads, cached, new):
+    """In the latent: keys and values of the token are infinite throughout.  In the rotated part: its scores alone."""
+    rng = np.random.default_rng(11)
+    rows = W.gaussian_bf16(rng, (cached[0] + new[0], ROW), 1.0)
+    q, w = W.gaussian_bf16(rng, (new[0], heads, 192), 1.0), W.gaussian_bf16(rng, (heads, 256, 512), 512 ** -0.5)
+    column = 5
+    # what column 5 of a latent gives to its keys has the sign of the query's element, or in odd rows the other one
+    sign = np.where(np.arange(new[0]) % 2, -1.0, 1.0)
+    q64, w64 = bf16_to_f64(q), bf16_to_f64(w)
+    q64[:, :, :128] = sign[:, None, None] * (np.abs(q64[:, :, :128]) + 0.01)
+    q64[:, :, 131] = sign[:, None] * (np.abs(q64[:, :, 131]) + 0.01)
+    w64[:, :128, column] = np.abs(w64[:, :128, column]) + 0.01
+    w64[:, 128:, column] += np.where(w64[:, 128:, column] < 0, -0.01, 0.01)
+    q, w = f64_to_bf16(q64), f64_to_bf16(w64)
+    q64, w64 = bf16_to_f64(q), bf16_to_f64(w)
+    b = Shared(cached, new, rows, 12)
+    visible, clean = b.visible(), expanded(E, b, q, w)
+    at = np.unique(np.concatenate([np.arange(new[0])[-40:], rng.integers(0, new[0], 30)]))
+    at = at[visible[at] > 1]
+    for key in _places(cached, new):
+        for where in (column, LATENT + 3):
+            for bits in (0x7F80, 0xFF80):
+                bad = rows.copy()
+                bad[key, where] = bits
+                got = expanded(E, Shared(cached, new, bad, 12), q, w)
+                sees, above = visible > key, (sign > 0) == (bits == 0x7F80)
+                nan = np.isnan(bf16_to_f64(got))
+                expect = sees & (above | (where == column) | (visible == 1))
+                assert not np.any(nan != expect[:, None, None]), (key, where, bits)
+                for h in sorted({0, heads - 1}):
+                    keep = bf16_to_f64(f64_to_bf16(bf16_to_f64(rows[:, :LATENT]) @ w64[h].T))
+                    keys = np.concatenate([keep[:, :128], bf16_to_f64(rows[:, LATENT:])], 1)
+                    want, size = attend(q64[at, h], visible[at], keys, keep[:, 128:], without=[key])
+                    _check(got[at, h], clean[at, h], sees[at], above[at], np.arange(128) if where == column else [], want, size)
