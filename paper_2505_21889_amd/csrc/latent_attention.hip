@@ -66,12 +66,12 @@ __device__ __forceinline__ Place find_tile(const LatentTable& t, const Requests&
   at.units = latent_units_of(q, t.heads, TILE, 0);
   const int tiles = latent_tiles(q, t.heads, TILE);
   if (tiles == 1) return at;
-  for (int t0 = 0; t0 < tiles; t0 += 64) {
+  for (int t0 = 0; t0 < tiles; t0 += kLatentWaveTiles) {
     const int mine = t0 + lane < tiles ? latent_units_of(q, t.heads, TILE, t0 + lane) : 0;
-    int upto = mine;  // of the lanes up to this one (64 tiles of at most 2^25 units)
+    LatentWaveUnits upto = mine;  // of the lanes up to this one
 #pragma unroll
     for (int by = 1; by < 64; by <<= 1) {
-      const int other = __shfl_up(upto, by);
+      const LatentWaveUnits other = __shfl_up(upto, by);
       if (lane >= by) upto += other;
     }
     const uint64_t in_front = __ballot(at.first + upto <= unit);  // tiles that end in front of the unit
@@ -79,10 +79,10 @@ __device__ __forceinline__ Place find_tile(const LatentTable& t, const Requests&
       const int k = __popcll(in_front);
       at.tile = t0 + k;
       at.units = __builtin_amdgcn_readlane(mine, k);
-      at.first += __builtin_amdgcn_readlane(upto, k) - at.units;
+      at.first += (int64_t)(LatentWaveUnits)__builtin_amdgcn_readlane(upto, k) - at.units;
       return at;
     }
-    at.first += __builtin_amdgcn_readlane(upto, 63);
+    at.first += (LatentWaveUnits)__builtin_amdgcn_readlane(upto, 63);
   }
   return at;
 }

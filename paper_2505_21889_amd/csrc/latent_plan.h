@@ -68,6 +68,10 @@ EFIM_HOST_DEVICE inline int latent_units_of(const LatentReq& q, int heads, int r
   return (latent_keys_of(q, heads, row_tile, tile) + kLatentTileKeys - 1) / kLatentTileKeys;
 }
 
+// Units of 64 tiles, which a wave looks through at a time: a request has up to 2^30 keys, and they then 2^31 units.
+constexpr int kLatentWaveTiles = 64;
+using LatentWaveUnits = uint32_t;
+
 // A workgroup has at most two parts of tiles that it does not have whole: its first and its last.
 EFIM_HOST_DEVICE inline int latent_slot(int group, bool first) { return 2 * group + (first ? 0 : 1); }
 
