@@ -84,10 +84,10 @@ __device__ __forceinline__ void load_to_lds_4x16(const void* base, uint32_t off0
       : "memory");
 }
 
-// N (2 to 4) such loads with one offset for all: N KB that lie as they go.
+// N (2 or 3) such loads with one offset for all: N KB that lie as they go.
 template <int N>
 __device__ __forceinline__ void load_to_lds_run(const void* base, uint32_t lane_off, uint32_t lds_addr) {
-  static_assert(N >= 2 && N <= 4, "the offset field holds three further pieces");
+  static_assert(N == 2 || N == 3, "the two forms that are written out");
   uint32_t saved_m0;
   if constexpr (N == 2)
     asm volatile(
@@ -108,19 +108,6 @@ __device__ __forceinline__ void load_to_lds_run(const void* base, uint32_t lane_
         "global_load_lds_dwordx4 %2, %3\n\t"
         "global_load_lds_dwordx4 %2, %3 offset:1024\n\t"
         "global_load_lds_dwordx4 %2, %3 offset:2048\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved_m0)
-        : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(lane_off), "s"(base)
-        : "memory");
-  if constexpr (N == 4)
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %2, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:1024\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:2048\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:3072\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved_m0)
         : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(lane_off), "s"(base)
