@@ -268,7 +268,7 @@ int efim_decode_step_fp8_table(const efim_batch_t* batch, const void* q, const v
  *   norm_eps  finite, >= 0
  *   inv_freq, rotary_dim, rope_interleaved  as efim_rope_append_table
  * The _fp8 form appends to an 8-bit cache as efim_rope_append_fp8 does.  No host state is kept and only kernels
- * are launched: both may be captured into a HIP graph.
+ * are launched: both may be captured into a HIP graph, which replays the lengths of the captured call.
  * Errors: as efim_rope_append_table; EFIM_ERR_INVALID_ARG also for norm_eps and for q without q_out or the reverse;
  * EFIM_ERR_UNSUPPORTED for 2^26 new tokens or more.
  * ------------------------------------------------------------------------------------- */
@@ -288,7 +288,8 @@ int efim_norm_rope_append_fp8(const efim_batch_t* batch, const void* q, void* q_
  *
  * batch: as for the other calls with num_kv_heads = 1 and head_dim = 576; num_q_heads (H) 1 .. 256,
  * any number.  EFIM_ERR_UNSUPPORTED for other head layouts and for more than 2^30 query rows (T * H).
- * None of these calls keeps host state and all launch only kernels: they may be captured into a HIP graph.
+ * None of these calls keeps host state and all launch only kernels: they may be captured into a HIP graph, which replays
+ * the lengths of the captured call (the block table's and the tensors' contents may change).
  * ------------------------------------------------------------------------------------- */
 
 /*
@@ -319,9 +320,14 @@ int efim_latent_append(const efim_batch_t* batch, const void* q_rope, int64_t q_
  *   sm_scale  finite, > 0 (the scale of the unabsorbed heads, e.g. 192^-1/2)
  *   workspace DEVICE, 256-byte aligned, at least efim_latent_workspace_bytes(batch) bytes, contents irrelevant; not to
  *             be used by an overlapping call
- * Scores and sums are fp32; probabilities enter the second product as bf16.  A row's result does not depend on the run, only
- * on the batch.  Slots at or beyond C_r + N_r may hold anything.  Infinities and NaN in rows that a query row does not see leave
- * it as it is; where it sees them it gets what the formula gives.
+ * Scores and sums are fp32; probabilities enter the second product as bf16.  Where the keys of a row are divided among
+ * workgroups, the sums of each part wait for their join as binary16 multiples of 2^-15 of the row's largest one (11
+ * significant bits down to 2^-29 of it).  A row's result does not depend on the run, only on the batch.
+ * All requests of a call are computed in tiles of 16, 32 or 128 rows (N_r * H), by the longest of them: a few long requests among
+ * many short ones are better a call of their own.  In tiles of 128 rows the time depends on the scores too: where they rise
+ * along the context it is up to 1.6 times that of level ones.
+ * Slots at or beyond C_r + N_r may hold anything.  Infinities and NaN in rows that a query row does not see leave it as
+ * it is; where it sees them it gets what the formula gives.
  * efim_latent_workspace_bytes is a pure host function: at least 256, 0 for an invalid batch.
  */
 size_t efim_latent_workspace_bytes(const efim_batch_t* batch);
@@ -337,7 +343,9 @@ int efim_latent_attention(const efim_batch_t* batch, const void* q, const void* 
  *   out       DEVICE bf16 [T, H, 128]   must not alias q, w_kv or the cache
  *   workspace as above, efim_latent_expanded_workspace_bytes(batch) bytes: the expanded keys and values of all requests with
  *             new tokens, 640 bytes a key and head (0: an invalid batch or one beyond a launch's reach)
- * Expanded keys and values are rounded to bf16; all sums are fp32.  Infinities and NaN as above.
+ * Expanded keys, expanded values and probabilities are rounded to bf16; all sums are fp32.  The result is about 2.8e-3 of its
+ * norm from the exact one, of which the outputs' own rounding is 1.7e-3.  Infinities and NaN as above; scores that rise along the
+ * context cost up to 1.2 times the time of level ones.
  */
 size_t efim_latent_expanded_workspace_bytes(const efim_batch_t* batch);
 int efim_latent_attention_expanded(const efim_batch_t* batch, const void* q, const void* latent_cache,
@@ -363,7 +371,8 @@ int efim_latent_attention_expanded(const efim_batch_t* batch, const void* q, con
  *   tokens        DEVICE int32, packed likewise: the a accepted tokens, the drawn one, then -1
  *   accepted      DEVICE int32 [B]: a
  *   workspace     DEVICE, 256-byte aligned, efim_verify_workspace_bytes(batch, vocab) bytes, contents irrelevant
- * Only kernels are launched and no host state is kept: the call may be captured into a HIP graph.
+ * Only kernels are launched and no host state is kept: the call may be captured into a HIP graph, which replays the
+ * num_drafts of the captured call.
  * Errors: EFIM_ERR_INVALID_ARG, EFIM_ERR_UNSUPPORTED (more than 63 drafted tokens of a request, a vocabulary above
  * 2^22), EFIM_ERR_WORKSPACE, EFIM_ERR_LAUNCH.
  * ------------------------------------------------------------------------------------- */

@@ -1,7 +1,7 @@
 // efim_latent_append: the new tokens' latent vectors normed, the rotary part of keys and queries rotated at the tokens'
 // positions, latent and rotated key written as one row of the paged latent cache.
 //   row = [ c * (mean(c^2) + eps)^(-1/2) * w | rot(k_r) ],  q_r -> rot(q_r), each rounded once to bf16
-// Streaming kernel, bound by HBM bandwidth: 4 * 576 + 256 * Hq bytes per token, 795 MB in 172 us = 4.6 TB/s read and written (a copy's
+// Streaming kernel, bound by HBM bandwidth: 4 * 576 + 256 * Hq bytes per token, 795 MB in 170 to 177 us = 4.6 TB/s read and written (a copy's
 // rate); two tokens 3.7 us.  Squares, norm and rotation are fp32, the angle fp64.
 #include <type_traits>
 

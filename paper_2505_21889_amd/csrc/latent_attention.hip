@@ -332,10 +332,14 @@ __device__ __forceinline__ void write_rows(const f32x16 (&o)[16], char* staged, 
 //   * adds the value product of h - 1 and beside it turns the scores of h into probabilities; behind the last read of
 //     values, six products before the end, the waves meet: the buffer of h - 1 is free and tile h + 1 is there for all, and
 //     beside the six go the first reads of its keys.
-// No maximum is formed on the way: the reference is the row's maximum over the part's first key tile, and moves where a tile's
-// sum of probabilities tells that one of them passed 2^kSlack.
-// A tile takes 3.7k cycles, 2.2k of them products; a part's queries in and outputs out 20 to 25k.  32 requests of 128 rows, 88k keys:
-// 42 us; 1014 tokens of 28 heads over 164k keys: 312 us = 1.01 PFLOP/s, products 49 % of the cycles (371 on a hot card).
+// No maximum is formed on the way: the reference is the row's maximum over the part's first key tile.  A tile of which a lane's
+// sixteen probabilities sum to 2^kSlack is looked at again, and the references of rows move whose maximum is beyond 2^kSlack.  Rows
+// whose keys lie 4 to kSlack log2 units above the part's first are thus looked at in every tile without moving; it costs
+// about the time of a tile.  1014 tokens of 28 heads over 164k keys: level scores 327 us, 2 units more every 1000 keys 437, 16 more
+// 530, all behind a request's first 32 keys higher by 5 480.
+// A tile takes 3.7k cycles, 2.2k of them products; a part's queries in and outputs out 20 to 25k, reloads of 35 spilled
+// registers among them (the tile loop's common path has none).  32 requests of 128 rows, 88k keys: 43 us; the 1014 tokens above 320 to
+// 350 us (the kernel alone) = 0.90 to 0.98 PFLOP/s, products 49 % of the cycles.
 __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
                                                                      const uint16_t* __restrict__ cache,
                                                                      const int32_t* __restrict__ block_table,
@@ -488,7 +492,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
         __builtin_amdgcn_sched_barrier(0);
       }
       if (tile == ntiles) break;
-      // where a probability passed the slack its row's reference moves to its maximum and they are formed again
+      // where the sum says that a probability may have passed the slack: a reference moves to its row's maximum if that did, and the
+      // probabilities are formed again
       if (__any(sum >= kOver)) {
         float x[16];
 #pragma unroll
@@ -563,8 +568,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_rows_kernel(const Laten
 
 // Items of at most ROWS (16 or 32) query rows: all waves take the same rows, the key tiles in turn, in LDS of their own, and join
 // their results at the end.  Such a step is bound by reading the cache; the waves wait for nothing but their own gathers, so
-// that some load while others compute; two waves have a second place each and load while they compute.  32 requests, 176k keys, 16 heads: 38 us = 5.3 TB/s (45 where the cache
-// comes from HBM); one request of 2345 keys 11 us.
+// that some load while others compute; two waves have a second place each and load while they compute.  The reference follows
+// the maximum, so the time does not depend on the scores.  32 requests, 176k keys, 16 heads: 39 us = 5.3 TB/s (45 where the
+// cache comes from HBM); one request of 2345 keys 11 us.
 template <int ROWS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const LatentArgs args, const uint16_t* __restrict__ q,
                                                                      const uint16_t* __restrict__ cache,
@@ -699,7 +705,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
     if constexpr (!Op::R32) l_run = cross_quarter_sum(l_run);
     l_run = cross_half_sum(l_run);
 
-    // join of the four waves, kStage columns at a time (more of 32 rows cost registers): [wave][row][kStage + 4], and behind them
+    // join of the waves, kStage columns at a time (more of 32 rows cost registers): [wave][row][kStage + 4], and behind them
     // [wave][row] (reference, sum, largest magnitude, -)
     constexpr int kCols = 128, kStage = ROWS == 16 ? 512 : 128, kPitch = kStage + 4;
     static_assert(WAVES * ROWS * (kPitch + 4) * 4 <= kZeros, "the join fits the tiles' place");
@@ -731,7 +737,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
       const f32x4 ml = s_ml[k * ROWS + my_row];
       const float weight = __builtin_amdgcn_exp2f(ml[0] - my_m);
       my_l += ml[1] * weight;
-      my_top += ml[2] * weight;  // (no sum of the four is larger)
+      my_top += ml[2] * weight;  // (no sum over the waves is larger)
     }
     const int64_t at = (int64_t)it.slot * ROWS + my_row;
     if (it.slot >= 0 && my_col == 0 && my_row < it.rows) *reinterpret_cast<f32x4*>(args.part_ml + at * 4) = f32x4{my_m, my_l, part_scale(my_top), 0.f};
@@ -791,8 +797,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void latent_keys_kernel(const Latent
 
 // Joins the parts of a tile that several workgroups share: with M = max m, out = sum 2^(m - M) O / sum 2^(m - M) l, in the parts'
 // order.  blockIdx.y stands for the first workgroup whose share begins inside the tile; a wave takes every
-// 4 gridDim.x-th row, eight columns to a lane, eight parts' loads at a time.  A launch and 33 MB of parts 9.6 us, 67 MB and as many
-// outputs 18.5 us, 4 MB 5 us.
+// 4 gridDim.x-th row, eight columns to a lane, eight parts' loads at a time.  A launch and 33 MB of parts 10 us, 67 MB and as many
+// outputs 18 us, 4 MB 5 us.
 template <int TILE>
 __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs args, uint16_t* __restrict__ out) {
   const LatentTable& t = args.table;

@@ -7,8 +7,9 @@
 // Two kernels.  The first is a product of the gathered latents with the weight, whose results it leaves in the workspace
 // as the second one's LDS tiles: of 64 keys and a head, 24 KB of keys and 16 KB of values, chunks swizzled, so that the
 // second gathers a tile with plain 1 KB loads.  The second is the attention, 32 query rows to a wave: scores and values as in the
-// absorbed form, sums fp32, expanded keys, values and probabilities bf16 (as the weight and the latents are).
-// 12 prompts of 20k new tokens, 26k keys and 32 heads: 225 us (214 GFLOP, 523 MB written) and 600 us (536 GFLOP that count).
+// absorbed form, sums fp32, expanded keys, values and probabilities bf16 (as the weight and the latents are, and with their range):
+// 2.8e-3 of the result's norm from the exact one, where its own rounding alone leaves 1.7e-3.
+// 12 prompts of 20k new tokens, 26k keys and 32 heads: 228 to 240 us (214 GFLOP, 523 MB written) and 590 to 630 us (536 GFLOP that count).
 #include <cstddef>
 #include <type_traits>
 #include <utility>
@@ -84,7 +85,7 @@ __device__ __forceinline__ void expand_product(f32x16& acc, bf16x8 weight, bf16x
 // in each of eight waves, and the slice's latents pass by in LDS, 32 at a time: so a latent is fetched once a head.  A wave's
 // results W C^T are, a lane, four neighbouring outputs of one token; beside the products of a unit those of the unit in front
 // go out through LDS, in runs of 64 bytes, and the gather of the unit two further on.  Without the gathers and the stores the
-// products take 160 us of the 225 above, alone 110.  (Four waves of 64 rows, for which an operand read from LDS serves
+// products take 160 us of the 228 above, alone 110.  (Four waves of 64 rows, for which an operand read from LDS serves
 // two products, measured the same; tiles of 128 tokens and 256 outputs with the weight in LDS, 2.5 GB gathered, 290 us.)
 __global__ __launch_bounds__(64 * kExpandWaves, 2) void expand_kernel(const ExpandedTable t, const uint16_t* __restrict__ cache,
                                                                       const uint16_t* __restrict__ w_kv,
@@ -314,14 +315,16 @@ struct ExpandedArgs {
 // request's last rows, which see most keys, first.  A team of four waves, one on each SIMD, takes the rows, 32 each.  GROUPS 1: a
 // workgroup is one team and a unit holds two workgroups, so that each computes through the other's meetings, first loads
 // and last stores.  GROUPS 2: it is two teams, which divide the keys and join at the end.  Bound by the products and what has to
-// be issued beside them (45 % of the cycles are products), at a clock that their power sets.  One workgroup of eight waves
+// be issued beside them (49 % of the cycles are products), at a clock that their power sets.  One workgroup of eight waves
 // and 256 rows to a unit took 2 % more, four waves of 64 rows, whose operands serve two products, 15 % more.
 //
 // A wave works off its keys in halves of tiles, three at a time: while the scores of half n are turned into probabilities, the
 // products form the scores of n + 1 and add the values of n - 1.  The waves meet in front of every round.  Keys are
 // gathered three halves ahead and values, which are wanted two halves later, two.  No maximum is formed on the way: the
-// reference is the row's maximum over the first half and moves where a half's sum of probabilities tells that one of
-// them passed 2^kSlack.
+// reference is the row's maximum over the first half.  A half of which a lane's sixteen probabilities sum to 2^kSlack is looked at
+// again, and the references of rows move whose maximum is beyond 2^kSlack.  Rows whose keys lie 4 to kSlack log2 units above the
+// first half's are thus looked at in every half without moving: the prompts above 839 us level (both kernels), 930 where scores rise
+// by 8 units every 1000 keys, 1001 where all behind the first 32 keys are higher by 6.
 constexpr int kTeam = 4;                              // waves
 constexpr int kHalfKeys = kKeysBytes / 2, kHalfValues = (kTileBytes - kKeysBytes) / 2;
 constexpr int kKeyStages = 4, kValueStages = 3;       // halves in a team's LDS
@@ -538,7 +541,8 @@ __global__ __launch_bounds__(64 * kTeam * GROUPS, 2) void expanded_attention_ker
     if (n + 4 < count) fetch_keys(n + 4);
   };
 
-  // Where a probability passed the slack its row's reference moves to its maximum and they are formed again.
+  // Where the sum says that a probability may have passed the slack: a reference moves to its row's maximum if that did, and
+  // the probabilities are formed again.
   auto settle = [&](const f32x16& sc, u32x4 (&pn)[2], float sum) __attribute__((always_inline)) {
     if (__any(sum >= kOver)) {
       const float mx = row_max(sc);
