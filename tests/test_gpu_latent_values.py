@@ -122,3 +122,41 @@ def test_expanded_one_infinity_in_a_key(E, heads, cached, new):
                     keys = np.concatenate([keep[:, :128], bf16_to_f64(rows[:, LATENT:])], 1)
                     want, size = attend(q64[at, h], visible[at], keys, keep[:, 128:], without=[key])
                     _check(got[at, h], clean[at, h], sees[at], above[at], np.arange(128) if where == column else [], want, size)
+
+
+@pytest.mark.parametrize("name", ["rows16", "rows32", "rows32_two_waves", "rows128", "rows128_even"])
+def test_absorbed_queries_that_are_no_numbers_keep_to_themselves(E, name):
+    """Runs of query rows, some of them whole waves': the other rows keep their bits."""
+    heads, cached, new = ROUTES[name][:3]
+    rng = np.random.default_rng(13)
+    b = Shared(cached, new, W.gaussian_bf16(rng, (max(np.add(cached, new)), ROW), 1.0), 14)
+    q = W.gaussian_bf16(rng, (b.total, heads, ROW), 1.0)
+    clean = absorbed(E, b, q).reshape(-1, LATENT)
+    bad = np.arange(len(clean)) % 89 < 37
+    for bits in (0x7FC0, 0xFF80):
+        q2 = q.copy().reshape(-1, ROW)
+        q2[bad] = bits
+        got = absorbed(E, b, q2.reshape(q.shape)).reshape(-1, LATENT)
+        assert np.array_equal(got[~bad], clean[~bad]) and np.all(np.isnan(bf16_to_f64(got[bad])))
+
+
+@pytest.mark.parametrize("heads,cached,new", [(3, [100, 7], [140, 300]), (48, [20, 900], [1500, 200])])
+def test_expanded_rows_that_are_no_numbers_keep_to_themselves(E, heads, cached, new):
+    """Runs of query rows; a new token's latent, which the rows in front of it do not see."""
+    rng = np.random.default_rng(15)
+    rows = W.gaussian_bf16(rng, (max(np.add(cached, new)), ROW), 1.0)
+    q, w = W.gaussian_bf16(rng, (sum(new), heads, 192), 1.0), W.gaussian_bf16(rng, (heads, 256, 512), 512 ** -0.5)
+    b = Shared(cached, new, rows, 16)
+    clean, visible = expanded(E, b, q, w), b.visible()
+    bad = np.arange(sum(new)) % 89 < 37
+    for bits in (0x7FC0, 0xFF80):
+        q2, rows2 = q.copy(), rows.copy()
+        q2[bad] = bits
+        got = expanded(E, b, q2, w)
+        assert np.array_equal(got[~bad], clean[~bad]) and np.all(np.isnan(bf16_to_f64(got[bad])))
+        for key in (cached[0] + 33, cached[0] + new[0] - 1):
+            rows2[key] = bits
+            got = expanded(E, Shared(cached, new, rows2, 16), q, w)
+            seen = visible > np.nonzero((rows2 != rows).any(1))[0].min()
+            assert np.array_equal(got[~seen], clean[~seen]) and np.all(np.isnan(bf16_to_f64(got[seen])))
+            rows2 = rows.copy()
