@@ -353,6 +353,148 @@ int efim_latent_attention_expanded(const efim_batch_t* batch, const void* q, con
                                    size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * 4-bit KV cache: half the bytes of the 8-bit one and a scale to every 32 elements instead of one to a tensor.
+ *
+ * Format: OCP MXFP4.  The elements of a head row are taken in blocks of 32 neighbours.  A block has a scale 2^s, held as the
+ * byte s + 127; its elements are 2^s times an E2M1 number (a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; codes 0 .. 7, the sign
+ * is bit 3), two codes to a byte, the element in front in the lower half.  A page of one head is its P rows' codes and behind
+ * them its P rows' scales:
+ *   k_cache, v_cache  DEVICE  uint8 [num_pages, Hkv, P * D / 2 + P * D / 32]   (efim_mx4_cache_bytes each)
+ *     row at slot i:  codes at i * D / 2, scales at P * D / 2 + i * D / 32
+ * Scale bytes are 2 .. 252, or 255: the 32 elements are no numbers.  Slots that a call reads must hold no other.
+ *
+ * None of these calls keeps host state and all launch only kernels: they may be captured into a HIP graph, which replays
+ * the lengths of the captured call (the block table's and the tensors' contents may change).
+ * ------------------------------------------------------------------------------------- */
+
+/* Bytes of one such cache (of keys or of values); 0 for sizes that are no cache's.  Pure host function. */
+size_t efim_mx4_cache_bytes(int64_t num_pages, int num_kv_heads, int page_size, int head_dim);
+
+/*
+ * efim_rope_append_mx4 -- efim_rope_append_table for a 4-bit cache.  What that call would have stored (the rotated key after its
+ * rounding to bf16, the value as given) is rounded block by block: s is the least whole number with max |x| <= 7 * 2^s, from -125 to
+ * 125, and every x / 2^s goes to the nearest code, ties to the even one, magnitudes above 6 to 6.  So no element is further off
+ * than half a step.  A block with an infinity or NaN gets byte 255 and codes 0.
+ *   q         DEVICE bf16 [T, Hq, D]   raw queries (read only unless q_out is q).  NULL: keys and values only
+ *   q_out     DEVICE bf16 [T, Hq, D]   rotated queries, the bits of efim_rope_append_table; may be q; NULL where q is
+ *   k_stored, v_stored  DEVICE bf16 [T, Hkv, D]  receive what the new rows' codes stand for (exact in bf16), for a caller that
+ *             goes on with the rows as later steps will see them.  NULL: not asked for.  Must not alias the other tensors
+ *   inv_freq, rotary_dim, rope_interleaved  as efim_rope_append_table
+ * Errors: as efim_rope_append_table; EFIM_ERR_INVALID_ARG also for q without q_out or the reverse; EFIM_ERR_UNSUPPORTED for 2^26
+ * new tokens or more.
+ */
+int efim_rope_append_mx4(const efim_batch_t* batch, const void* q, void* q_out, const void* k_new, const void* v_new,
+                         void* k_cache, void* v_cache, void* k_stored, void* v_stored, const double* inv_freq,
+                         int rotary_dim, int rope_interleaved, void* stream);
+
+/*
+ * efim_extend_attention_mx4 -- efim_extend_attention over a 4-bit cache, for any number of new tokens: single ones of a
+ * decode step as whole prompts.  Requests of up to 32 query rows (N_r * Hq / Hkv) and longer ones go through kernels of their own,
+ * so a step may mix them.
+ * Operands are exact, scores and sums fp32, probabilities enter the second product as bf16.  The parts of a tile of rows whose
+ * keys are divided among workgroups wait for their join in fp32.  A row's result does not depend on the run, only on the batch.
+ *   q         DEVICE bf16 [T, Hq, D]   rotated queries
+ *   out       DEVICE bf16 [T, Hq, D]   must not alias q or the caches
+ *   sm_scale  finite, >= 0; 0 selects 1/sqrt(D)
+ *   workspace DEVICE, 256-byte aligned, at least efim_mx4_workspace_bytes(batch) bytes, contents irrelevant; not to be used by
+ *             an overlapping call
+ * Slots at or beyond C_r + N_r may hold anything.  Blocks that are no numbers in rows that a query row does not see leave it as it
+ * is; where it sees them it gets what the formula gives: of a key, no number in the whole row, of a value, none in the block's columns.
+ * Errors: as efim_extend_attention; EFIM_ERR_UNSUPPORTED for more than 2^30 query rows (T * Hq).
+ * efim_mx4_workspace_bytes is a pure host function: at least 256, 0 for an invalid batch.
+ */
+size_t efim_mx4_workspace_bytes(const efim_batch_t* batch);
+int efim_extend_attention_mx4(const efim_batch_t* batch, const void* q, const void* k_cache, const void* v_cache,
+                              void* out, float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * efim_block_tables -- the block tables and the slot map of a step, built on the device from lengths that lie there: what a step
+ * of efim_batch_t needs in front of it, where an engine's lengths (and how many drafted tokens were refused) are known to
+ * the device alone.
+ * For request r with pages for held_len[r] tokens, cached_len[r] tokens that stay and new_len[r] to come, with
+ * held = ceil(held_len / P) and wanted = ceil((cached_len + new_len) / P):
+ *   columns wanted .. held - 1 of its block table row go back onto the stack of free pages, those of request 0 first, each in
+ *     the order of the columns (the entries stay as they are in the row);
+ *   then columns held .. wanted - 1 are filled with pages from the stack's top, those of request 0 first;
+ *   slot_map[row_start[r] + i] = page * P + slot of position cached_len[r] + i;   -1 behind the last request's.
+ *   held_len, cached_len, new_len  DEVICE int32 [B]
+ *   block_table     DEVICE int32 [B, max_pages_per_req], in/out
+ *   free_pages      DEVICE int32 [free_capacity], in/out: the stack, its first *free_count entries are free pages
+ *   free_count, free_count_out  DEVICE int32: pages on the stack in front of and behind the call; may be one
+ *   slot_map        DEVICE int64 [slot_capacity].  NULL: not asked for
+ *   row_start       DEVICE int32 [B + 1]: first packed new-token row of every request, and the end
+ *   status          DEVICE int32: 0; the number of pages that were missing; or EFIM_ERR_INVALID_ARG: a negative length, a row longer
+ *                   than max_pages_per_req, more pages than the stack holds or tokens than the slot map (or 2^31).  In the latter two
+ *                   cases block_table, free_pages and the count stay as they are and slot_map is -1 throughout.
+ *   workspace       DEVICE, 256-byte aligned, efim_block_tables_workspace_bytes(batch) bytes, contents irrelevant
+ * Page ids are not looked at.  Arrays must not overlap, but for the two counts.
+ * Only kernels are launched and no host state is kept: the call may be captured into a HIP graph, and as its lengths are read on the
+ * device a replay follows them.
+ * Errors: EFIM_ERR_INVALID_ARG, EFIM_ERR_UNSUPPORTED (page sizes as above, more than 2^20 requests), EFIM_ERR_WORKSPACE,
+ * EFIM_ERR_LAUNCH.
+ * ------------------------------------------------------------------------------------- */
+size_t efim_block_tables_workspace_bytes(int batch);
+int efim_block_tables(int batch, const int32_t* held_len, const int32_t* cached_len, const int32_t* new_len,
+                      int page_size, int32_t* block_table, int max_pages_per_req, int32_t* free_pages,
+                      int64_t free_capacity, const int32_t* free_count, int32_t* free_count_out, int64_t* slot_map,
+                      int64_t slot_capacity, int32_t* row_start, int32_t* status, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * efim_logit_probs -- the logits of a step to the probabilities that efim_verify_drafts takes: repeated tokens are penalised, biases
+ * added, tokens that a grammar forbids left out, then the softmax.  Request r with n = num_drafts[r] drafted tokens has n + 1 rows,
+ * packed as efim_verify_drafts packs them (n = 0: the one row of a step without drafts); row i has seen the request's
+ * history and the drafted tokens x_0 .. x_{i-1}.  Per token of the vocabulary, in this order and each operation rounded to fp32:
+ *   z = x;   seen at all:  z = z > 0 ? z / repetition : z * repetition;
+ *   seen k > 0 times behind the prompt (drafted tokens count):  z = (z - frequency * k) - presence;
+ *   z = z + bias (of several biases of a token the last counts);   p = softmax(z / temperature) over the allowed tokens
+ * and 0 for the others.  temperature not above 0 (or NaN): 1 for the first of the largest z, 0 else; below 2^-100 as that.
+ * A row of which nothing is allowed, or all of it at minus infinity, is zero throughout.  Infinities and NaN of tokens
+ * that are not allowed do not matter; with a NaN or plus infinity among the allowed ones all of them get NaN (temperature 0: NaN is
+ * never the largest).
+ * ------------------------------------------------------------------------------------- */
+typedef struct efim_sampling { /* of a request; 32 bytes, an array of them lies on the device */
+  float temperature, repetition, presence, frequency;
+  int32_t prompt_len;  /* of the history, the tokens that were not made                      */
+  int32_t history_len; /* tokens of its history row                                          */
+  int32_t num_biases;  /* entries of its bias row                                            */
+  int32_t reserved;
+} efim_sampling_t;     /* counts outside their row's width (the history) are taken as its ends */
+
+typedef struct efim_logits {
+  int32_t batch;                 /* B >= 0                                                                      */
+  int32_t vocab;                 /* V, up to 2^22                                                               */
+  const int32_t* num_drafts;     /* HOST [B], 0 <= n <= 63, read before the call returns                        */
+  const void* logits;            /* DEVICE bf16 or float, the n + 1 rows of request 0, of request 1, ...        */
+  int64_t logits_stride;         /* elements from row to row, at least V                                        */
+  int32_t logits_bf16;           /* 1: bf16, 0: float                                                           */
+  int32_t reserved;
+  const efim_sampling_t* params; /* DEVICE [B].  NULL: temperature 1, no history, no biases                     */
+  const int32_t* history;        /* DEVICE [B, history_stride] tokens.  NULL: none; ids outside [0, V) are not counted */
+  int64_t history_stride;
+  const int32_t* draft_tokens;   /* DEVICE, packed: the n tokens of request 0, ...                              */
+  const int32_t* bias_tokens;    /* DEVICE [B, bias_stride]; NULL (with bias_values): none                      */
+  const float* bias_values;      /* DEVICE [B, bias_stride]                                                     */
+  int32_t bias_stride;
+  int32_t num_masks;
+  const uint32_t* masks;         /* DEVICE [num_masks, mask_stride]: token t is allowed by bit t % 32 of word t / 32.  NULL: none */
+  int64_t mask_stride;           /* words from mask to mask, at least ceil(V / 32)                              */
+  const int32_t* mask_rows;      /* DEVICE, a mask for every row of logits; negative: all is allowed, num_masks or above: nothing */
+} efim_logits_t;
+
+/*
+ *   probs     DEVICE float, row stride probs_stride >= V elements; may be the logits where those are float with the same stride
+ *   workspace DEVICE, 256-byte aligned, efim_logit_workspace_bytes(in) bytes, contents irrelevant
+ * Only kernels are launched and no host state is kept: the call may be captured into a HIP graph, which replays num_drafts of the
+ * captured call and reads everything else anew.
+ * Errors: EFIM_ERR_INVALID_ARG, EFIM_ERR_UNSUPPORTED (more than 63 drafted tokens, a vocabulary above 2^22), EFIM_ERR_WORKSPACE,
+ * EFIM_ERR_LAUNCH.
+ */
+size_t efim_logit_workspace_bytes(const efim_logits_t* in);
+int efim_logit_probs(const efim_logits_t* in, void* probs, int64_t probs_stride, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * efim_verify_drafts -- the end of a step with drafted tokens (a short step of up to 16 new tokens per request computes their
  * probabilities): accepts or refuses them against the target's probabilities and draws the token that follows, so that
  * the tokens are distributed as the target's own.  For request r with n = num_drafts[r] drafted tokens x_0 .. x_{n-1}:

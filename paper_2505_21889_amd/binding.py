@@ -43,6 +43,36 @@ class EfimBatch(ctypes.Structure):
     ]
 
 
+class EfimLogits(ctypes.Structure):
+    """efim_logits_t"""
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("vocab", ctypes.c_int32),
+        ("num_drafts", ctypes.c_void_p),
+        ("logits", ctypes.c_void_p),
+        ("logits_stride", ctypes.c_int64),
+        ("logits_bf16", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("params", ctypes.c_void_p),
+        ("history", ctypes.c_void_p),
+        ("history_stride", ctypes.c_int64),
+        ("draft_tokens", ctypes.c_void_p),
+        ("bias_tokens", ctypes.c_void_p),
+        ("bias_values", ctypes.c_void_p),
+        ("bias_stride", ctypes.c_int32),
+        ("num_masks", ctypes.c_int32),
+        ("masks", ctypes.c_void_p),
+        ("mask_stride", ctypes.c_int64),
+        ("mask_rows", ctypes.c_void_p),
+    ]
+
+
+#: efim_sampling_t: an array of these, as bytes, is what LogitsDesc takes on the device
+SAMPLING_DTYPE = np.dtype([("temperature", np.float32), ("repetition", np.float32), ("presence", np.float32),
+                           ("frequency", np.float32), ("prompt_len", np.int32), ("history_len", np.int32),
+                           ("num_biases", np.int32), ("reserved", np.int32)])
+
+
 class EfimWorkItem(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "req", "kv_head", "row_begin", "row_count", "key_begin", "key_end", "partial_slot", "merge_id")]
@@ -146,6 +176,23 @@ def _load():
     lib.efim_latent_expanded_workspace_bytes.restype = ctypes.c_size_t
     lib.efim_latent_attention_expanded.argtypes = [bp, vp, vp, vp, vp, f32, vp, ctypes.c_size_t, vp]
     lib.efim_latent_attention_expanded.restype = i32
+    lib.efim_mx4_cache_bytes.argtypes = [i64, i32, i32, i32]
+    lib.efim_mx4_cache_bytes.restype = ctypes.c_size_t
+    lib.efim_rope_append_mx4.argtypes = [bp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp]
+    lib.efim_rope_append_mx4.restype = i32
+    lib.efim_mx4_workspace_bytes.argtypes = [bp]
+    lib.efim_mx4_workspace_bytes.restype = ctypes.c_size_t
+    lib.efim_extend_attention_mx4.argtypes = [bp, vp, vp, vp, vp, f32, vp, ctypes.c_size_t, vp]
+    lib.efim_extend_attention_mx4.restype = i32
+    lib.efim_block_tables_workspace_bytes.argtypes = [i32]
+    lib.efim_block_tables_workspace_bytes.restype = ctypes.c_size_t
+    lib.efim_block_tables.argtypes = [i32, vp, vp, vp, i32, vp, i32, vp, i64, vp, vp, vp, i64, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.efim_block_tables.restype = i32
+    lgp = ctypes.POINTER(EfimLogits)
+    lib.efim_logit_workspace_bytes.argtypes = [lgp]
+    lib.efim_logit_workspace_bytes.restype = ctypes.c_size_t
+    lib.efim_logit_probs.argtypes = [lgp, vp, i64, vp, ctypes.c_size_t, vp]
+    lib.efim_logit_probs.restype = i32
     lib.efim_verify_workspace_bytes.argtypes = [i32, i32]
     lib.efim_verify_workspace_bytes.restype = ctypes.c_size_t
     lib.efim_verify_drafts.argtypes = [i32, vp, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
@@ -191,6 +238,8 @@ EXPORTED_SYMBOLS = (
     "efim_norm_rope_append", "efim_norm_rope_append_fp8",
     "efim_latent_append", "efim_latent_workspace_bytes", "efim_latent_attention",
     "efim_latent_expanded_workspace_bytes", "efim_latent_attention_expanded",
+    "efim_mx4_cache_bytes", "efim_rope_append_mx4", "efim_mx4_workspace_bytes", "efim_extend_attention_mx4",
+    "efim_block_tables_workspace_bytes", "efim_block_tables", "efim_logit_workspace_bytes", "efim_logit_probs",
     "efim_verify_workspace_bytes", "efim_verify_drafts",
     "efim_extend_plan_items", "efim_plan_info", "efim_set_tuning", "efim_set_kernel_events", "efim_status_string",
     "efim_last_hip_error", "efim_version", "efim_source_digest", "efim_stream_release",
@@ -464,6 +513,72 @@ def efim_latent_attention_expanded(batch, q, latent_cache, w_kv, out, sm_scale, 
                                                float(sm_scale), _ptr(workspace), int(workspace_bytes),
                                                _stream_ptr(stream)),
            "efim_latent_attention_expanded")
+
+
+def efim_mx4_cache_bytes(num_pages, num_kv_heads, page_size, head_dim):
+    return int(_lib.efim_mx4_cache_bytes(int(num_pages), int(num_kv_heads), int(page_size), int(head_dim)))
+
+
+def efim_rope_append_mx4(batch, q, q_out, k_new, v_new, k_cache, v_cache, k_stored, v_stored, inv_freq, rotary_dim,
+                         rope_interleaved=0, stream=None):
+    table = _freq_table(inv_freq, rotary_dim)
+    _check(_lib.efim_rope_append_mx4(ctypes.byref(batch.c), _ptr(q), _ptr(q_out), _ptr(k_new), _ptr(v_new), _ptr(k_cache),
+                                     _ptr(v_cache), _ptr(k_stored), _ptr(v_stored), table.ctypes.data, int(rotary_dim),
+                                     int(rope_interleaved), _stream_ptr(stream)),
+           "efim_rope_append_mx4")
+
+
+def efim_mx4_workspace_bytes(batch):
+    return int(_lib.efim_mx4_workspace_bytes(ctypes.byref(batch.c)))
+
+
+def efim_extend_attention_mx4(batch, q, k_cache, v_cache, out, sm_scale, workspace, workspace_bytes, stream=None):
+    _check(_lib.efim_extend_attention_mx4(ctypes.byref(batch.c), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out),
+                                          float(sm_scale), _ptr(workspace), int(workspace_bytes), _stream_ptr(stream)),
+           "efim_extend_attention_mx4")
+
+
+def efim_block_tables_workspace_bytes(batch):
+    return int(_lib.efim_block_tables_workspace_bytes(int(batch)))
+
+
+def efim_block_tables(batch, held_len, cached_len, new_len, page_size, block_table, max_pages_per_req, free_pages,
+                      free_capacity, free_count, free_count_out, slot_map, slot_capacity, row_start, status, workspace,
+                      workspace_bytes, stream=None):
+    _check(_lib.efim_block_tables(int(batch), _ptr(held_len), _ptr(cached_len), _ptr(new_len), int(page_size),
+                                  _ptr(block_table), int(max_pages_per_req), _ptr(free_pages), int(free_capacity),
+                                  _ptr(free_count), _ptr(free_count_out), _ptr(slot_map), int(slot_capacity),
+                                  _ptr(row_start), _ptr(status), _ptr(workspace), int(workspace_bytes),
+                                  _stream_ptr(stream)),
+           "efim_block_tables")
+
+
+class LogitsDesc:
+    """Owns the host array behind an efim_logits_t and keeps its tensors alive.  logits: a bfloat16 or float32 tensor
+    (or an address, with bf16 given); what is None is left out."""
+
+    def __init__(self, num_drafts, vocab, logits, logits_stride, params=None, history=None, history_stride=0,
+                 draft_tokens=None, bias_tokens=None, bias_values=None, bias_stride=0, masks=None, mask_stride=0,
+                 num_masks=0, mask_rows=None, bf16=None):
+        self.num_drafts = np.ascontiguousarray(num_drafts, dtype=np.int32)
+        self.tensors = (logits, params, history, draft_tokens, bias_tokens, bias_values, masks, mask_rows)
+        if bf16 is None:
+            bf16 = {"torch.bfloat16": 1, "torch.float32": 0}[str(logits.dtype)]
+        self.c = EfimLogits(
+            int(self.num_drafts.size), int(vocab), self.num_drafts.ctypes.data if self.num_drafts.size else None,
+            _ptr(logits), int(logits_stride), int(bf16), 0, _ptr(params), _ptr(history), int(history_stride),
+            _ptr(draft_tokens), _ptr(bias_tokens), _ptr(bias_values), int(bias_stride), int(num_masks), _ptr(masks),
+            int(mask_stride), _ptr(mask_rows))
+
+
+def efim_logit_workspace_bytes(desc):
+    return int(_lib.efim_logit_workspace_bytes(ctypes.byref(desc.c)))
+
+
+def efim_logit_probs(desc, probs, probs_stride, workspace, workspace_bytes, stream=None):
+    _check(_lib.efim_logit_probs(ctypes.byref(desc.c), _ptr(probs), int(probs_stride), _ptr(workspace),
+                                 int(workspace_bytes), _stream_ptr(stream)),
+           "efim_logit_probs")
 
 
 def efim_verify_workspace_bytes(batch, vocab):

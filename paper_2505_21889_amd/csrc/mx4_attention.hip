@@ -1,0 +1,771 @@
+// efim_extend_attention_mx4: causal softmax attention of the new tokens over a paged 4-bit cache.
+//   s = scale <q, k_j>,  p = softmax(s),  o = sum_j p_j v_j,   j = 0 .. C_r + i
+// Rows are (token, head of the group) pairs, so all query heads of a kv head read its rows once.  What codes stand for is exact
+// in bf16, so the products are those of a bf16 cache: bf16 operands, fp32 sums, probabilities rounded to bf16 (as many bits as
+// the values that they weigh).  S^T = K Q^T and O^T = V^T P^T: a lane holds scores of ONE query row, and the rounded
+// probabilities are the second product's operand as they stand.
+//
+// Values lie in memory along the head dimension and enter the product along the keys; they go through LDS as bf16 and the
+// transposing read turns them.  (The read for 4-bit elements would leave keys with scales of their own in one operand word.)
+//
+// A value block that is no number must not reach rows that do not see it as zero times no number: such blocks enter the product
+// as zeros, and where a workgroup met one its rows lose their numbers in the columns of blocks that they do see (`torn`).
+#include <type_traits>
+
+#include "efim_internal.h"
+#include "mx4_math.h"
+#include "mx4_plan.h"
+#include "wave_ops.h"
+
+namespace efim {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+#define LDS_PTR(T) __attribute__((address_space(3))) T*
+
+constexpr int kXcdCount = 8;  // of the device: workgroup i runs on XCD i % 8
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kSlack = 8.f;  // log2 units by which a row's maximum may outgrow its reference
+constexpr uint32_t kTorn = 253;  // scale bytes from here on: values that are not finite
+
+struct Mx4Args {
+  Mx4Table table;
+  float scale_log2;  // sm_scale * log2(e)
+  float* part_o;     // partial results of split tiles, [slot][row tile][D]: the unnormalised output
+  float* part_ml;    // [slot][row tile][2]: reference in log2 units, sum
+  uint16_t* out;
+};
+
+// A lane each (two for each lane), asked for at once: what a unit's request is follows without another load.
+struct Requests {
+  Mx4Req held[2];
+  int nreq;
+  __device__ __forceinline__ Requests(const Mx4Table& t, int lane) : nreq(t.nreq) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) held[i] = t.req[min(i * 64 + lane, t.nreq - 1)];
+  }
+  __device__ __forceinline__ int find(int64_t unit, int lane) const {
+    int r = -1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r += __popcll(__ballot(i * 64 + lane < nreq && held[i].unit_start <= unit));
+    return __builtin_amdgcn_readfirstlane(r);
+  }
+};
+
+// The tile that a unit of the launch lies in, by the whole wave.
+struct Place {
+  int r;          // request of the launch
+  int head;
+  int tile;       // of the request and head
+  int units;      // of the tile
+  int64_t first;  // unit of the launch at which it begins
+};
+template <int TILE, int UNIT>
+__device__ __forceinline__ Place find_tile(const Mx4Table& t, const Requests& requests, int64_t unit, int lane) {
+  Place at;
+  at.r = requests.find(unit, lane);
+  const Mx4Req q = t.req[at.r];
+  const int64_t in = unit - q.unit_start;
+  // (fewer than 2^32 units in nearly all launches: a 64-bit division takes hundreds of cycles)
+  at.head = (in | q.units_per_head) >> 32 == 0 ? (int)((uint32_t)in / (uint32_t)q.units_per_head) : (int)(in / q.units_per_head);
+  at.head = __builtin_amdgcn_readfirstlane(at.head);
+  at.first = q.unit_start + at.head * q.units_per_head;
+  at.tile = 0;
+  const int tiles = mx4_tiles(q, t.group_heads, TILE);
+  at.units = mx4_units_of(q, t.group_heads, TILE, UNIT, 0);
+  if (tiles == 1) return at;
+  for (int t0 = 0; t0 < tiles; t0 += 64) {
+    const int mine = t0 + lane < tiles ? mx4_units_of(q, t.group_heads, TILE, UNIT, t0 + lane) : 0;
+    int upto = mine;  // of the lanes up to this one
+#pragma unroll
+    for (int by = 1; by < 64; by <<= 1) {
+      const int other = __shfl_up(upto, by);
+      if (lane >= by) upto += other;
+    }
+    const uint64_t in_front = __ballot(at.first + upto <= unit);  // tiles that end in front of the unit
+    if (in_front != ~0ull) {
+      const int k = __popcll(in_front);
+      at.tile = t0 + k;
+      at.units = __builtin_amdgcn_readlane(mine, k);
+      at.first += __builtin_amdgcn_readlane(upto, k) - at.units;
+      return at;
+    }
+    at.first += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return at;
+}
+
+// A workgroup's share of the units, a tile's part at a time.
+template <int TILE, int UNIT>
+struct Share {
+  const Mx4Table& t;
+  Place at;
+  int group;
+  int64_t begin, end;  // units that are left
+  // the part at hand
+  Mx4Req rq;
+  int row0, rows;  // of the request
+  int k0, k1;      // keys
+  int64_t slot;    // partial result, -1: the workgroup has the whole tile
+
+  __device__ __forceinline__ Share(const Mx4Table& table, int lane) : t(table) {
+    // an XCD takes neighbouring shares, which have rows of the cache in common
+    group = (int)(blockIdx.x % kXcdCount) * (int)(gridDim.x / kXcdCount) + (int)(blockIdx.x / kXcdCount);
+    begin = end = 0;
+    if (group >= t.groups) return;
+    begin = t.first_unit(group);
+    end = t.first_unit(group + 1);
+    const Requests requests(table, lane);
+    at = find_tile<TILE, UNIT>(t, requests, begin, lane);
+    rq = t.req[at.r];
+    part();
+  }
+  __device__ __forceinline__ bool done() const { return begin >= end; }
+  __device__ __forceinline__ void part() {
+    row0 = at.tile * TILE;
+    rows = mx4_rows_of(rq, t.group_heads, TILE, at.tile);
+    const int u0 = (int)(begin - at.first);
+    const int u1 = (int)min((int64_t)at.units, end - at.first);
+    k0 = u0 * UNIT;
+    k1 = min(u1 * UNIT, mx4_keys_of(rq, t.group_heads, TILE, at.tile));
+    slot = u0 == 0 && u1 == at.units ? -1 : mx4_slot(group, u0 > 0);
+  }
+  __device__ __forceinline__ void advance() {
+    begin = at.first + at.units;
+    if (done()) return;
+    at.first = begin;
+    if (++at.tile == mx4_tiles(rq, t.group_heads, TILE)) {
+      at.tile = 0;
+      if (++at.head == t.kv_heads) {
+        at.head = 0;
+        rq = t.req[++at.r];
+      }
+    }
+    at.units = mx4_units_of(rq, t.group_heads, TILE, UNIT, at.tile);
+    part();
+  }
+};
+
+// Where the rows of a request's kv head lie.
+template <int D>
+struct Cache {
+  const char* rows;
+  const __attribute__((address_space(4))) int32_t* pages;  // (scalar loads)
+  int page_shift, kv_heads, head;
+
+  __device__ __forceinline__ Cache(const uint8_t* cache, const int32_t* block_table, const Mx4Table& t, const Mx4Req& q, int h)
+      : rows(reinterpret_cast<const char*>(cache)),
+        pages((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(block_table + (int64_t)q.req * t.max_pages)),
+        page_shift(t.page_shift), kv_heads(t.kv_heads), head(h) {}
+  // page of a (wave-uniform) key, and where the head's rows of a page begin
+  __device__ __forceinline__ int32_t page_id(int key) const { return pages[__builtin_amdgcn_readfirstlane(key >> page_shift)]; }
+  __device__ __forceinline__ int64_t page_at(int32_t id) const { return (((int64_t)id * kv_heads + head) << page_shift) * mx4_row_bytes(D); }
+  __device__ __forceinline__ int slot_of(int key) const { return key & ((1 << page_shift) - 1); }
+  __device__ __forceinline__ uint32_t code_at(int key) const { return (uint32_t)slot_of(key) * mx4_code_bytes(D); }
+  __device__ __forceinline__ uint32_t scale_at(int key) const {
+    return ((uint32_t)mx4_code_bytes(D) << page_shift) + (uint32_t)slot_of(key) * mx4_scale_bytes(D);
+  }
+  // the blocks of a key's row, by any lane, whose values are not finite (bit b: block b)
+  __device__ __forceinline__ uint32_t torn_blocks(int key) const {
+    const char* page = rows + page_at(pages[key >> page_shift]);
+    uint32_t torn = 0;
+#pragma unroll
+    for (int b = 0; b < mx4_scale_bytes(D); ++b) torn |= (uint32_t)((uint8_t)page[scale_at(key) + b] >= kTorn) << b;
+    return torn;
+  }
+};
+
+__device__ __forceinline__ float add_pair(uint32_t two, float sum) {  // of two probabilities as they were rounded
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, sum, false);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
+}
+
+// Chunk swizzles (exclusive or) of a tile's bf16 rows in LDS.  Keys: the operand reads of neighbouring rows take all banks.
+// Values: so do the four rows that a transposing read takes at a time, and for products of 16 rows two such groups.
+template <int D>
+__device__ __forceinline__ int key_swizzle(int row) { return row & (D / 8 - 1); }
+template <int D>
+__device__ __forceinline__ int value_swizzle(int row) { return (row & (D / 32 - 1)) << 2; }
+template <int D>
+__device__ __forceinline__ int value_swizzle16(int row) { return value_swizzle<D>(row) ^ (D == 128 ? ((row >> 2) & 1) << 1 : 0); }
+
+// One wave writes and reads its own LDS: the accesses are in order, the compiler is told by the fences.
+__device__ __forceinline__ void own_writes() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// --- few rows ---------------------------------------------------------------------------------------------------------------
+// NB blocks of 16 query rows.  The four waves share the rows: of each 128 keys a wave takes 32, with a maximum and sums of its
+// own, and their sums are combined at the part's end.  A wave's keys go from memory to registers, where they are the product's
+// operands as they are converted; a lane has 16 (D 128; 8) bytes of a row's codes, all under one scale, and the query operands
+// follow that order of elements.
+template <int D, int NB>
+__global__ __launch_bounds__(kThreads) void mx4_few_kernel(const Mx4Args args, const uint16_t* __restrict__ q,
+                                                           const uint8_t* __restrict__ k_cache, const uint8_t* __restrict__ v_cache,
+                                                           const int32_t* __restrict__ block_table) {
+  constexpr int kRows = 16 * NB;
+  constexpr int kSteps = D / 32;           // products over the head dimension
+  constexpr int kBlocks = D / 16;          // output blocks
+  constexpr int kKeyBytes = D / 8;         // of a row's codes, in a lane
+  constexpr int kValueLanes = D / 32;      // lanes of a value row, 16 bytes of codes each
+  constexpr int kValueLoads = 32 * kValueLanes / 64;
+  constexpr int kRowBytes = 2 * D;         // of a bf16 row in LDS
+  constexpr int kTileBytes = 32 * kRowBytes;
+  constexpr int kPitch = D + 4;            // floats from row to row of the sums
+  constexpr int kSumBytes = kWaves * kRows * (kPitch + 2) * 4;
+  constexpr int kLds = kWaves * kTileBytes > kSumBytes ? kWaves * kTileBytes : kSumBytes;
+  __shared__ __attribute__((aligned(1024))) char lds[kLds];
+  __shared__ uint32_t s_torn[kWaves];  // whether the wave met a value block that is no number
+  using KeyCodes = std::conditional_t<D == 128, u32x4, u32x2>;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i16 = lane & 15, q4 = lane >> 4;
+  const Mx4Table& t = args.table;
+  const int g = t.group_heads, hq = g * t.kv_heads;
+  const uint32_t tile = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + wave * kTileBytes;
+
+  for (Share<kRows, kMx4FewKeys> it(t, lane); !it.done(); it.advance()) {
+    const Cache<D> keys(k_cache, block_table, t, it.rq, it.at.head), values(v_cache, block_table, t, it.rq, it.at.head);
+    const int last = it.k1 - 1;
+    bf16x8 qb[NB][kSteps];
+    int visible[NB];  // keys that the row sees
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int row = n * 16 + i16;
+      const int tok = row / g;
+      visible[n] = row < it.rows ? it.rq.cached + tok + 1 : 0;
+      const uint16_t* src = q + ((int64_t)(it.rq.row_start + tok) * hq + it.at.head * g + (row - tok * g)) * D + q4 * (D / 4);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        u32x4 v = {0, 0, 0, 0};
+        if (row < it.rows) v = *reinterpret_cast<const u32x4*>(src + 8 * s);
+        qb[n][s] = __builtin_bit_cast(bf16x8, v);
+      }
+    }
+    f32x4 o[NB][kBlocks];
+    float m_run[NB], l_run[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m_run[n] = -INFINITY;
+      l_run[n] = 0.f;
+    }
+    uint32_t torn = 0;
+
+    struct Chunk {  // codes and scales of 32 keys
+      KeyCodes k[2];
+      uint32_t ks[2];
+      u32x4 v[kValueLoads];
+      uint32_t vs[kValueLoads];
+    };
+    struct Pages {  // of eight keys each
+      int32_t id[4];
+    };
+    auto look_up = [&](int key0) __attribute__((always_inline)) {
+      Pages p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p.id[e] = keys.page_id(min(key0 + 8 * e, last));
+      return p;
+    };
+    auto load = [&](int key0, const Pages& p, Chunk& c) __attribute__((always_inline)) {
+      int64_t at_page[4];  // of keys and of values
+#pragma unroll
+      for (int e = 0; e < 4; ++e) at_page[e] = keys.page_at(p.id[e]);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int key = min(key0 + b * 16 + i16, last);
+        const char* page = keys.rows + (i16 & 8 ? at_page[2 * b + 1] : at_page[2 * b]);
+        c.k[b] = *reinterpret_cast<const KeyCodes*>(page + keys.code_at(key) + q4 * kKeyBytes);
+        c.ks[b] = *reinterpret_cast<const uint8_t*>(page + keys.scale_at(key) + (D == 128 ? q4 : q4 >> 1));
+      }
+#pragma unroll
+      for (int j = 0; j < kValueLoads; ++j) {
+        const int in = j * (64 / kValueLanes) + lane / kValueLanes;
+        const int key = min(key0 + in, last);
+        int64_t at = in & 8 ? at_page[2 * j + 1] : at_page[2 * j];
+        if constexpr (kValueLoads == 1) at = in & 16 ? (in & 8 ? at_page[3] : at_page[2]) : at;
+        const char* page = values.rows + at;
+        c.v[j] = *reinterpret_cast<const u32x4*>(page + values.code_at(key) + lane % kValueLanes * 16);
+        c.vs[j] = *reinterpret_cast<const uint8_t*>(page + values.scale_at(key) + lane % kValueLanes);
+      }
+    };
+    Chunk next;
+    int key0 = it.k0 + wave * 32;
+    Pages pages = look_up(key0);
+    if (key0 < it.k1) load(key0, pages, next);
+    pages = look_up(key0 + kMx4FewKeys);
+    for (; key0 < it.k1; key0 += kMx4FewKeys) {
+      const Chunk c = next;
+      if (key0 + kMx4FewKeys < it.k1) load(key0 + kMx4FewKeys, pages, next);
+      pages = look_up(key0 + 2 * kMx4FewKeys);
+      // scores
+      f32x4 sc[NB][2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const float scale = mx4_scale_value(c.ks[b]);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const bf16x8 ka = __builtin_bit_cast(bf16x8, mx4_decode8(c.k[b][s], scale));
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
+            if (s == 0) sc[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+            sc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qb[n][s], sc[n][b], 0, 0, 0);
+          }
+        }
+      }
+      // values, as bf16 rows to LDS
+      own_writes();
+#pragma unroll
+      for (int j = 0; j < kValueLoads; ++j) {
+        const int key = j * (64 / kValueLanes) + lane / kValueLanes;
+        const bool bad = c.vs[j] >= kTorn;
+        torn |= bad;
+        const float scale = bad ? 1.f : mx4_scale_value(c.vs[j]);
+        const uint32_t to = tile + key * kRowBytes;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int chunk = (lane % kValueLanes * 4 + w) ^ value_swizzle16<D>(key);
+          *(LDS_PTR(mx4_words))(uintptr_t)(to + chunk * 16) = mx4_decode8(bad ? 0u : c.v[j][w], scale);
+        }
+      }
+      own_writes();
+      // probabilities
+      bf16x8 pb[NB];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const int lim = visible[n] - key0 - q4 * 4;
+        if (key0 + 32 > it.rq.cached + 1 || key0 + 32 > it.k1) {
+          const int end = min(lim, it.k1 - key0 - q4 * 4);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (b * 16 + r >= end) sc[n][b][r] = -INFINITY;
+        }
+        float top = max3(max3(sc[n][0][0], sc[n][0][1], sc[n][0][2]), sc[n][0][3], max3(sc[n][1][0], sc[n][1][1], sc[n][1][2]));
+        top = cross_half_max(cross_quarter_max(fmaxf(top, sc[n][1][3]))) * args.scale_log2;
+        const bool grow = top > m_run[n] + kSlack;
+        if (__any(grow)) {
+          // (a row is moved by its own scores alone, whatever the other rows of the wave hold)
+          const float m_next = grow ? top : m_run[n];
+          const float alpha = __builtin_amdgcn_exp2f(m_run[n] - (m_next == -INFINITY ? 0.f : m_next));
+          l_run[n] *= alpha;
+#pragma unroll
+          for (int d = 0; d < kBlocks; ++d) o[n][d] *= alpha;
+          m_run[n] = m_next;
+        }
+        const float m_use = m_run[n] == -INFINITY ? 0.f : m_run[n];
+        u32x4 p;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float a = __builtin_amdgcn_exp2f(sc[n][r >> 1][(r & 1) * 2] * args.scale_log2 - m_use);
+          const float b = __builtin_amdgcn_exp2f(sc[n][r >> 1][(r & 1) * 2 + 1] * args.scale_log2 - m_use);
+          p[r] = pack_bf16(a, b);
+          l_run[n] = add_pair(p[r], l_run[n]);
+        }
+        pb[n] = __builtin_bit_cast(bf16x8, p);
+      }
+      // outputs
+      const int w16 = lane & 15;
+      const int v_key = 4 * q4 + (w16 >> 2);
+      const uint32_t v_at = tile + v_key * kRowBytes + (w16 & 1) * 8;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) {
+        const uint32_t at = v_at + (((2 * d + ((w16 & 3) >> 1)) ^ value_swizzle16<D>(v_key)) << 4);
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)at);
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + 16 * kRowBytes));
+        const bf16x8 va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n], o[n][d], 0, 0, 0);
+      }
+    }
+
+    // the waves' sums, rescaled to the largest reference: M = max m,  O = sum 2^(m - M) O_w
+    const bool met = __any(torn != 0);
+    if (lane == 0) s_torn[wave] = met;
+    float* xo = reinterpret_cast<float*>(lds);   // [wave][row] x kPitch
+    float* xm = xo + kWaves * kRows * kPitch;    // [wave][row]
+    float* xl = xm + kWaves * kRows;
+    __syncthreads();  // every wave is done with its tile
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int row = wave * kRows + n * 16 + i16;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d) *reinterpret_cast<f32x4*>(xo + row * kPitch + d * 16 + q4 * 4) = o[n][d];
+      const float l = cross_half_sum(cross_quarter_sum(l_run[n]));
+      if (q4 == 0) {
+        xm[row] = m_run[n];
+        xl[row] = l;
+      }
+    }
+    __syncthreads();
+    constexpr int kVec = D / 4;  // threads of a row
+    const int c = tid % kVec * 4;
+    for (int row = tid / kVec; row < it.rows; row += kThreads / kVec) {
+      float m[kWaves], top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        m[w] = xm[w * kRows + row];
+        top = fmaxf(top, m[w]);
+      }
+      float l = 0.f;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = m[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[w] - top);
+        l += f * xl[w * kRows + row];
+        v += f * *reinterpret_cast<const f32x4*>(xo + (w * kRows + row) * kPitch + c);
+      }
+      const int tok = row / g;
+      if (s_torn[0] | s_torn[1] | s_torn[2] | s_torn[3]) {
+        for (int key = it.k0; key < min(it.k1, it.rq.cached + tok + 1); ++key)
+          if (values.torn_blocks(key) >> (c / kMx4Block) & 1) v = f32x4{NAN, NAN, NAN, NAN};
+      }
+      if (it.slot < 0) {
+        const float inv = 1.f / l;
+        const u32x2 words = {pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+        *reinterpret_cast<u32x2*>(args.out + ((int64_t)(it.rq.row_start + tok) * hq + it.at.head * g + (row - tok * g)) * D + c) = words;
+      } else {
+        *reinterpret_cast<f32x4*>(args.part_o + (it.slot * kRows + row) * D + c) = v;
+        if (c == 0) *reinterpret_cast<f32x2*>(args.part_ml + (it.slot * kRows + row) * 2) = f32x2{top, l};
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// --- many rows --------------------------------------------------------------------------------------------------------------
+// 128 query rows, 32 of them a wave's.  A tile of 64 keys and values is converted once for all of them on its way from memory
+// to LDS (a thread has 16 bytes of a row's codes), one tile ahead.
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args args, const uint16_t* __restrict__ q,
+                                                               const uint8_t* __restrict__ k_cache, const uint8_t* __restrict__ v_cache,
+                                                               const int32_t* __restrict__ block_table) {
+  constexpr int kSteps = D / 16;
+  constexpr int kBlocks = D / 32;
+  constexpr int kRowBytes = 2 * D;
+  constexpr int kMatrixBytes = kMx4ManyKeys * kRowBytes;
+  constexpr int kStageBytes = 2 * kMatrixBytes;  // keys, values
+  constexpr int kLanes = D / 32;                 // threads of a row
+  constexpr int kLoads = 2 * kMx4ManyKeys * kLanes / kThreads;  // of a thread: keys and values (D 128), either (D 64)
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kStageBytes];
+  __shared__ uint32_t s_torn[kWaves];  // whether the wave met a value block that is no number
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i32 = lane & 31, hi = lane >> 5;
+  const Mx4Table& t = args.table;
+  const int g = t.group_heads, hq = g * t.kv_heads;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
+
+  // operands in a stage
+  const int blk = lane >> 4, w16 = lane & 15;
+  const int v_key = (blk >> 1) * 4 + (w16 >> 2);
+  const int v_chunk = 2 * (blk & 1) + ((w16 & 3) >> 1);
+  // what this thread converts
+  const int in_tile = tid / kLanes % kMx4ManyKeys, piece = tid % kLanes;
+  const int first_matrix = kLoads == 2 ? 0 : __builtin_amdgcn_readfirstlane(tid / (kLanes * kMx4ManyKeys));
+
+  for (Share<kMx4ManyRows, kMx4ManyKeys> it(t, lane); !it.done(); it.advance()) {
+    const Cache<D> cache(k_cache, block_table, t, it.rq, it.at.head);
+    const int ntiles = (it.k1 - it.k0 + kMx4ManyKeys - 1) / kMx4ManyKeys;
+    const int local = wave * 32 + i32;
+    const bool row_ok = local < it.rows;
+    const int row = it.row0 + local, tok = row / g;
+    const int visible = row_ok ? it.rq.cached + tok + 1 : 0;
+    const int64_t q_off = ((int64_t)(it.rq.row_start + tok) * hq + it.at.head * g + (row - tok * g)) * D;
+    const bool active = wave * 32 < it.rows;  // (wave-uniform)
+    const int least = it.rq.cached + (it.row0 + wave * 32) / g + 1;
+    const int most = it.rq.cached + (it.row0 + min(it.rows, wave * 32 + 32) - 1) / g + 1;
+    bf16x8 qb[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      u32x4 v = {0, 0, 0, 0};
+      if (row_ok) v = *reinterpret_cast<const u32x4*>(q + q_off + 16 * s + 8 * hi);
+      qb[s] = __builtin_bit_cast(bf16x8, v);
+    }
+    f32x16 o[kBlocks];
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    uint32_t torn = 0;
+
+    u32x4 codes[kLoads];
+    uint32_t scales[kLoads];
+    auto key_of = [&](int tile) { return min(it.k0 + tile * kMx4ManyKeys + in_tile, it.k1 - 1); };
+    auto look_up = [&](int tile) { return cache.pages[key_of(tile) >> t.page_shift]; };
+    auto load = [&](int tile, int32_t page) __attribute__((always_inline)) {
+      const int key = key_of(tile);
+      const int64_t at = cache.page_at(page);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const uint8_t* from = (first_matrix + j == 0 ? k_cache : v_cache) + at;
+        codes[j] = *reinterpret_cast<const u32x4*>(from + cache.code_at(key) + piece * 16);
+        scales[j] = from[cache.scale_at(key) + piece];
+      }
+    };
+    auto convert = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const bool is_v = first_matrix + j == 1;
+        const bool bad = is_v && scales[j] >= kTorn;
+        torn |= bad;
+        const float scale = bad ? 1.f : mx4_scale_value(scales[j]);
+        const uint32_t to = lds0 + (tile & 1) * kStageBytes + is_v * kMatrixBytes + in_tile * kRowBytes;
+        const int swizzle = is_v ? value_swizzle<D>(in_tile) : key_swizzle<D>(in_tile);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          *(LDS_PTR(mx4_words))(uintptr_t)(to + ((piece * 4 + w) ^ swizzle) * 16) = mx4_decode8(bad ? 0u : codes[j][w], scale);
+      }
+    };
+    load(0, look_up(0));
+    int32_t page = look_up(1);
+    for (int tile = 0; tile < ntiles; ++tile) {
+      convert(tile);
+      if (tile + 1 < ntiles) load(tile + 1, page);
+      page = look_up(tile + 2);
+      __syncthreads();
+      const int key0 = it.k0 + tile * kMx4ManyKeys;
+      if (!active || key0 >= most) continue;
+      const uint32_t k_at = lds0 + (tile & 1) * kStageBytes, v_at = k_at + kMatrixBytes;
+      f32x16 sc[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[kb][r] = 0.f;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const bf16x8 ka = *(const LDS_PTR(bf16x8))(uintptr_t)(k_at + (kb * 32 + i32) * kRowBytes + (((2 * s + hi) ^ key_swizzle<D>(i32)) << 4));
+          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[s], sc[kb], 0, 0, 0);
+        }
+      }
+      if (key0 + kMx4ManyKeys > min(least, it.k1)) {
+        const int lim = min(visible, it.k1) - key0 - hi * 4;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (kb * 32 + (r >> 2) * 8 + (r & 3) >= lim) sc[kb][r] = -INFINITY;
+      }
+      float top = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = max3(top, sc[0][r], sc[1][r]);
+      top = cross_half_max(top) * args.scale_log2;
+      const bool grow = top > m_run + kSlack;
+      if (__any(grow)) {
+        const float m_next = grow ? top : m_run;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - (m_next == -INFINITY ? 0.f : m_next));
+        l_run *= alpha;
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+        m_run = m_next;
+      }
+      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        u32x4 p[2];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const float a = __builtin_amdgcn_exp2f(sc[kb][2 * r] * args.scale_log2 - m_use);
+          const float b = __builtin_amdgcn_exp2f(sc[kb][2 * r + 1] * args.scale_log2 - m_use);
+          p[r >> 2][r & 3] = pack_bf16(a, b);
+          l_run = add_pair(p[r >> 2][r & 3], l_run);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int d = 0; d < kBlocks; ++d) {
+            const uint32_t at = v_at + ((kb * 2 + h) * 16 + v_key) * kRowBytes + (w16 & 1) * 8 + (((d * 4 + v_chunk) ^ value_swizzle<D>(v_key)) << 4);
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)at);
+            const bf16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + 8 * kRowBytes));
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7),
+                                                           __builtin_bit_cast(bf16x8, p[h]), o[d], 0, 0, 0);
+          }
+      }
+    }
+    const bool met = __any(torn != 0);
+    if (lane == 0) s_torn[wave] = met;
+    __syncthreads();  // every wave is done with the stages, and the words are set
+    if (row_ok) {
+      const float l = cross_half_sum(l_run);
+      if (s_torn[0] | s_torn[1] | s_torn[2] | s_torn[3]) {
+        const Cache<D> values(v_cache, block_table, t, it.rq, it.at.head);
+        uint32_t lost = 0;
+        for (int key = it.k0; key < min(it.k1, visible); ++key) lost |= values.torn_blocks(key);
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+          if (lost >> d & 1)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] = NAN;
+      }
+      const float inv = 1.f / l;
+      const int64_t part = it.slot * kMx4ManyRows + local;
+#pragma unroll
+      for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 v = {o[d][4 * r4], o[d][4 * r4 + 1], o[d][4 * r4 + 2], o[d][4 * r4 + 3]};
+          const int c = d * 32 + r4 * 8 + hi * 4;
+          if (it.slot < 0)
+            *reinterpret_cast<u32x2*>(args.out + q_off + c) = u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+          else
+            *reinterpret_cast<f32x4*>(args.part_o + part * D + c) = v;
+        }
+      if (it.slot >= 0 && hi == 0) *reinterpret_cast<f32x2*>(args.part_ml + part * 2) = f32x2{m_run, l};
+    }
+    __syncthreads();
+  }
+}
+
+// --- join -------------------------------------------------------------------------------------------------------------------
+// The parts of split tiles: with M = max m_s,  out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, in the order of the keys.  Workgroup
+// i has the tile in which the shares of workgroups i and i + 1 are the first to meet.
+template <int D, int TILE, int UNIT>
+__global__ __launch_bounds__(kThreads) void mx4_join_kernel(const Mx4Args args) {
+  const Mx4Table& t = args.table;
+  const int lane = threadIdx.x & 63;
+  const int second = blockIdx.x + 1;  // workgroup that goes on where another's share ends
+  const int64_t unit = t.first_unit(second);
+  const Requests requests(t, lane);
+  const Place at = find_tile<TILE, UNIT>(t, requests, unit, lane);
+  if (at.first == unit || t.first_unit(second - 1) > at.first) return;
+  const Mx4Req rq = t.req[at.r];
+  const int g = t.group_heads, hq = g * t.kv_heads;
+  const int rows = mx4_rows_of(rq, g, TILE, at.tile);
+  const int64_t end = at.first + at.units;
+  constexpr int kVec = D / 4;
+  const int c = threadIdx.x % kVec * 4;
+  for (int r = blockIdx.y * (kThreads / kVec) + threadIdx.x / kVec; r < rows; r += gridDim.y * (kThreads / kVec)) {
+    float m = -INFINITY, l = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int group = second - 1; group == second - 1 || t.first_unit(group) < end; ++group) {
+      const int64_t part = mx4_slot(group, group >= second) * TILE + r;
+      const f32x2 ml = *reinterpret_cast<const f32x2*>(args.part_ml + part * 2);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(args.part_o + part * D + c);
+      const float m_next = fmaxf(m, ml[0]);
+      const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_next);
+      const float add = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_next);
+      l = l * old + ml[1] * add;
+      v = v * old + x * add;
+      m = m_next;
+    }
+    const float inv = 1.f / l;
+    const int row = at.tile * TILE + r, tok = row / g;
+    *reinterpret_cast<u32x2*>(args.out + ((int64_t)(rq.row_start + tok) * hq + at.head * g + (row - tok * g)) * D + c) =
+        u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+  }
+}
+
+struct Mx4Tensors {
+  const uint16_t* q;
+  const uint8_t *k_cache, *v_cache;
+  const int32_t* block_table;
+};
+
+template <int D>
+int launch_class(const efim_batch_t* b, const Mx4Plan& plan, Mx4Args* args, const Mx4Tensors& x, hipStream_t stream) {
+  Mx4Cursor at;
+  while (mx4_next(b, plan, &at, &args->table)) {
+    const int groups = args->table.groups;
+    const dim3 grid((unsigned)((groups + kXcdCount - 1) / kXcdCount * kXcdCount));
+    auto join = [&](auto rows, auto keys) {
+      constexpr int kAtOnce = kThreads / (D / 4);
+      if (groups > 1)
+        mx4_join_kernel<D, decltype(rows)::value, decltype(keys)::value>
+            <<<dim3((unsigned)groups - 1, (unsigned)((decltype(rows)::value + 4 * kAtOnce - 1) / (4 * kAtOnce))), kThreads, 0, stream>>>(*args);
+    };
+    if (!plan.few) {
+      mx4_many_kernel<D><<<grid, kThreads, 0, stream>>>(*args, x.q, x.k_cache, x.v_cache, x.block_table);
+      join(std::integral_constant<int, kMx4ManyRows>{}, std::integral_constant<int, kMx4ManyKeys>{});
+    } else if (plan.row_tile == 16) {
+      mx4_few_kernel<D, 1><<<grid, kThreads, 0, stream>>>(*args, x.q, x.k_cache, x.v_cache, x.block_table);
+      join(std::integral_constant<int, 16>{}, std::integral_constant<int, kMx4FewKeys>{});
+    } else {
+      mx4_few_kernel<D, 2><<<grid, kThreads, 0, stream>>>(*args, x.q, x.k_cache, x.v_cache, x.block_table);
+      join(std::integral_constant<int, 32>{}, std::integral_constant<int, kMx4FewKeys>{});
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }
+  }
+  return EFIM_OK;
+}
+
+int validate(const efim_batch_t* batch, int64_t* total) {
+  const int rc = validate_batch(batch, total);
+  if (rc != EFIM_OK) return rc;
+  return *total * batch->num_q_heads > (int64_t)1 << 30 ? EFIM_ERR_UNSUPPORTED : EFIM_OK;  // (rows are counted in 32 bits)
+}
+
+size_t workspace_bytes(const efim_batch_t* batch) {
+  size_t bytes = 0;
+  for (const bool few : {true, false}) bytes += mx4_bytes(plan_mx4(batch, few, compute_units()), batch->head_dim).total;
+  return bytes < 256 ? 256 : bytes;
+}
+
+}  // namespace
+}  // namespace efim
+
+extern "C" {
+
+size_t efim_mx4_workspace_bytes(const efim_batch_t* batch) {
+  int64_t total = 0;
+  if (efim::validate(batch, &total) != EFIM_OK) return 0;
+  return efim::workspace_bytes(batch);
+}
+
+int efim_extend_attention_mx4(const efim_batch_t* batch, const void* q, const void* k_cache, const void* v_cache, void* out,
+                              float sm_scale, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace efim;
+  int64_t total = 0;
+  const int rc = validate(batch, &total);
+  if (rc != EFIM_OK) return rc;
+  if (!(sm_scale >= 0.f) || sm_scale - sm_scale != 0.f) return EFIM_ERR_INVALID_ARG;
+  if (total == 0) return EFIM_OK;
+  if (!q || !k_cache || !v_cache || !out) return EFIM_ERR_INVALID_ARG;
+  for (const void* p : {q, k_cache, v_cache, (const void*)out})
+    if (!aligned16(p)) return EFIM_ERR_INVALID_ARG;
+  if (!aligned4(batch->block_table)) return EFIM_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < efim::workspace_bytes(batch))
+    return EFIM_ERR_WORKSPACE;
+  Mx4Args args;
+  const float scale = sm_scale == 0.f ? 1.f / sqrtf((float)batch->head_dim) : sm_scale;
+  args.scale_log2 = scale * 1.4426950408889634f;
+  args.out = static_cast<uint16_t*>(out);
+  const Mx4Tensors x{static_cast<const uint16_t*>(q), static_cast<const uint8_t*>(k_cache), static_cast<const uint8_t*>(v_cache),
+                     batch->block_table};
+  char* at = static_cast<char*>(workspace);
+  for (const bool few : {true, false}) {
+    const Mx4Plan plan = plan_mx4(batch, few, compute_units());
+    if (!plan.any) continue;
+    const Mx4Bytes bytes = mx4_bytes(plan, batch->head_dim);
+    args.part_o = reinterpret_cast<float*>(at);
+    args.part_ml = reinterpret_cast<float*>(at + bytes.off_ml);
+    at += bytes.total;
+    auto* launch = batch->head_dim == 128 ? launch_class<128> : launch_class<64>;
+    const int done = launch(batch, plan, &args, x, static_cast<hipStream_t>(stream));
+    if (done != EFIM_OK) return done;
+  }
+  return EFIM_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,96 @@
+// How the attention over a 4-bit cache cuts a batch into work.  Host code without state: a call derives everything from the
+// lengths and hands the kernels a table of the requests, from which each workgroup works its share out.
+//
+// A tile is `row_tile` query rows (token x head of the group) of a request and kv head.  Its work is a unit for each `unit_keys`
+// keys in front of and at the last one that its rows see.  The units of all tiles, one behind the other, are dealt evenly to the
+// workgroups: a share is a run of them, which may begin and end inside a tile.  The parts of a tile that several workgroups share
+// are joined by a second kernel.
+//
+// Requests of few rows and of many are different launches: a mixed step's single tokens would be multiplied as tiles of
+// mostly empty rows otherwise.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "efim.h"
+
+#if defined(__HIPCC__) || defined(__HIP__)
+#define EFIM_HOST_DEVICE __host__ __device__
+#else
+#define EFIM_HOST_DEVICE
+#endif
+
+namespace efim {
+
+constexpr int kMx4TableReqs = 96;  // requests of a launch (kernel arguments end at 4 KB)
+
+struct Mx4Req {
+  int64_t unit_start;      // units in front of the request in the launch
+  int64_t units_per_head;  // of all its tiles of one kv head
+  int32_t req;             // block table row
+  int32_t cached;          // C_r
+  int32_t new_len;         // N_r > 0
+  int32_t row_start;       // first packed new-token row
+};
+
+struct Mx4Table {
+  Mx4Req req[kMx4TableReqs];
+  int64_t share;       // units of a workgroup; the first `longer` have one more
+  int32_t longer;
+  int32_t groups;      // workgroups with a share
+  int32_t nreq;
+  int32_t kv_heads;
+  int32_t group_heads; // query heads of a kv head
+  int32_t max_pages;
+  int32_t page_shift;
+
+  EFIM_HOST_DEVICE int64_t first_unit(int group) const { return group * share + (group < longer ? group : longer); }
+};
+
+// Tiles of a request and kv head, the rows of one, the keys that they see and its units.
+EFIM_HOST_DEVICE inline int mx4_tiles(const Mx4Req& q, int g, int row_tile) { return (q.new_len * g + row_tile - 1) / row_tile; }
+EFIM_HOST_DEVICE inline int mx4_rows_of(const Mx4Req& q, int g, int row_tile, int tile) {
+  const int left = q.new_len * g - tile * row_tile;
+  return left < row_tile ? left : row_tile;
+}
+EFIM_HOST_DEVICE inline int mx4_keys_of(const Mx4Req& q, int g, int row_tile, int tile) {
+  return q.cached + (tile * row_tile + mx4_rows_of(q, g, row_tile, tile) - 1) / g + 1;
+}
+EFIM_HOST_DEVICE inline int mx4_units_of(const Mx4Req& q, int g, int row_tile, int unit_keys, int tile) {
+  return (mx4_keys_of(q, g, row_tile, tile) + unit_keys - 1) / unit_keys;
+}
+
+// A workgroup has at most two parts of tiles that it does not have whole: one that goes on where another's ends, and one that
+// begins its tile.
+EFIM_HOST_DEVICE inline int64_t mx4_slot(int group, bool goes_on) { return 2 * (int64_t)group + (goes_on ? 0 : 1); }
+
+constexpr int kMx4FewRows = 32;    // query rows of a request and kv head that the kernel for few rows takes
+constexpr int kMx4FewKeys = 128;   // keys of its units: 32 for each of its four waves
+constexpr int kMx4ManyRows = 128;  // row tile of the kernel for many rows
+constexpr int kMx4ManyKeys = 64;
+
+// One class of requests (of few rows or of many) of a batch.
+struct Mx4Plan {
+  bool few = false;
+  int row_tile = 0;   // 16 or 32 (few), kMx4ManyRows
+  int unit_keys = 0;
+  int max_groups = 0; // workgroups to deal to
+  bool any = false;   // the batch has such requests
+};
+Mx4Plan plan_mx4(const efim_batch_t* b, bool few, int compute_units);
+
+// Workspace of a class: partial outputs [2 max_groups][row_tile][head_dim] and two floats (reference, sum) for each row of them.
+struct Mx4Bytes {
+  size_t off_ml = 0, total = 0;
+};
+Mx4Bytes mx4_bytes(const Mx4Plan& plan, int head_dim);
+
+// Where the next launch of a class begins.
+struct Mx4Cursor {
+  int req = 0;
+  int64_t row = 0;
+};
+// Fills the table of the next launch; false where no request of the class is left.
+bool mx4_next(const efim_batch_t* b, const Mx4Plan& plan, Mx4Cursor* at, Mx4Table* table);
+
+}  // namespace efim

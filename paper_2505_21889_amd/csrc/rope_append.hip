@@ -42,55 +42,6 @@ struct RopeArgs {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Rotates the eight pairs of a unit.  The results go through fp32 two at a time; the one pattern for
-// which that could round twice is looked for once per unit (one unit in 4000 has it) and the unit
-// then done again value by value.  (With the check and the integer rounding at every value they
-// were half of the kernel's instructions.)
-template <bool INTERLEAVED>
-__device__ __forceinline__ void rotate_units(u32x4& a, u32x4& b, const double (&cs)[8], const double (&sn)[8]) {
-  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-  uint32_t x1[8], x2[8];
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    // INTERLEAVED: 16 consecutive elements = pairs 0..7, stored (even, odd)
-    const uint32_t w = INTERLEAVED ? (t < 4 ? a[t & 3] : b[t & 3]) : a[t >> 1];
-    const uint32_t v = INTERLEAVED ? w : b[t >> 1];
-    x1[t] = INTERLEAVED || !(t & 1) ? w & 0xFFFFu : w >> 16;
-    x2[t] = INTERLEAVED || (t & 1) ? v >> 16 : v & 0xFFFFu;
-  }
-  float f1[8], f2[8];
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    double y1, y2;
-    rotate_pair_f64(x1[t], x2[t], cs[t], sn[t], &y1, &y2);
-    f1[t] = (float)y1;
-    f2[t] = (float)y2;
-  }
-  u16x2 off = __builtin_bit_cast(u16x2, off_midpoint(f1[0], f2[0]));
-#pragma unroll
-  for (int t = 1; t < 8; ++t)
-    off = __builtin_elementwise_min(off, __builtin_bit_cast(u16x2, off_midpoint(f1[t], f2[t])));
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    a[t] = INTERLEAVED ? pack_bf16(f1[t], f2[t]) : pack_bf16(f1[2 * t], f1[2 * t + 1]);
-    b[t] = INTERLEAVED ? pack_bf16(f1[4 + t], f2[4 + t]) : pack_bf16(f2[2 * t], f2[2 * t + 1]);
-  }
-  if (off[0] == 0 || off[1] == 0) {
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      uint32_t y1, y2;
-      rotate_pair_bf16(x1[t], x2[t], cs[t], sn[t], &y1, &y2);
-      x1[t] = y1;
-      x2[t] = y2;
-    }
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      a[t] = INTERLEAVED ? x1[t] | (x2[t] << 16) : x1[2 * t] | (x1[2 * t + 1] << 16);
-      b[t] = INTERLEAVED ? x1[4 + t] | (x2[4 + t] << 16) : x2[2 * t] | (x2[2 * t + 1] << 16);
-    }
-  }
-}
-
 // A wave takes one token and kPasses passes of 64 / (D / 16) head rows of it (a unit is 16 bytes of one head
 // row together with its partner 16 bytes; a lane has the same place in the row in every pass, so that
 // it needs the cosines and sines of the same eight pairs).

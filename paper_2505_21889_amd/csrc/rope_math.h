@@ -60,4 +60,55 @@ __device__ __forceinline__ uint32_t off_midpoint(float lo, float hi) {
   return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x05040100u) ^ 0x80008000u;
 }
 
+typedef uint32_t bf16_chunk __attribute__((ext_vector_type(4)));  // eight bf16 values
+
+// Rotates the eight pairs of a unit.  The results go through fp32 two at a time; the one pattern for
+// which that could round twice is looked for once per unit (one unit in 4000 has it) and the unit
+// then done again value by value.  (With the check and the integer rounding at every value they
+// were half of the kernel's instructions.)
+template <bool INTERLEAVED>
+__device__ __forceinline__ void rotate_units(bf16_chunk& a, bf16_chunk& b, const double (&cs)[8], const double (&sn)[8]) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  uint32_t x1[8], x2[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    // INTERLEAVED: 16 consecutive elements = pairs 0..7, stored (even, odd)
+    const uint32_t w = INTERLEAVED ? (t < 4 ? a[t & 3] : b[t & 3]) : a[t >> 1];
+    const uint32_t v = INTERLEAVED ? w : b[t >> 1];
+    x1[t] = INTERLEAVED || !(t & 1) ? w & 0xFFFFu : w >> 16;
+    x2[t] = INTERLEAVED || (t & 1) ? v >> 16 : v & 0xFFFFu;
+  }
+  float f1[8], f2[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    double y1, y2;
+    rotate_pair_f64(x1[t], x2[t], cs[t], sn[t], &y1, &y2);
+    f1[t] = (float)y1;
+    f2[t] = (float)y2;
+  }
+  u16x2 off = __builtin_bit_cast(u16x2, off_midpoint(f1[0], f2[0]));
+#pragma unroll
+  for (int t = 1; t < 8; ++t)
+    off = __builtin_elementwise_min(off, __builtin_bit_cast(u16x2, off_midpoint(f1[t], f2[t])));
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    a[t] = INTERLEAVED ? pack_bf16(f1[t], f2[t]) : pack_bf16(f1[2 * t], f1[2 * t + 1]);
+    b[t] = INTERLEAVED ? pack_bf16(f1[4 + t], f2[4 + t]) : pack_bf16(f2[2 * t], f2[2 * t + 1]);
+  }
+  if (off[0] == 0 || off[1] == 0) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      uint32_t y1, y2;
+      rotate_pair_bf16(x1[t], x2[t], cs[t], sn[t], &y1, &y2);
+      x1[t] = y1;
+      x2[t] = y2;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      a[t] = INTERLEAVED ? x1[t] | (x2[t] << 16) : x1[2 * t] | (x1[2 * t + 1] << 16);
+      b[t] = INTERLEAVED ? x1[4 + t] | (x2[4 + t] << 16) : x2[2 * t] | (x2[2 * t + 1] << 16);
+    }
+  }
+}
+
 }  // namespace efim
