@@ -35,6 +35,8 @@ constexpr int kXcdCount = 8;  // of the device: workgroup i runs on XCD i % 8
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr float kSlack = 8.f;  // log2 units by which a row's maximum may outgrow its reference
+constexpr float kOver = 256.f;  // 2^kSlack: a sum of rounded probabilities is never below its largest one
+constexpr float kNoReference = -3.0e38f;  // of a row that has seen no key: any finite score moves it
 constexpr uint32_t kTorn = 253;  // scale bytes from here on: values that are not finite
 
 struct Mx4Args {
@@ -162,9 +164,10 @@ struct Cache {
   const __attribute__((address_space(4))) int32_t* pages;  // (scalar loads)
   int page_shift, kv_heads, head;
 
-  __device__ __forceinline__ Cache(const uint8_t* cache, const int32_t* block_table, const Mx4Table& t, const Mx4Req& q, int h)
+  template <typename Table>
+  __device__ __forceinline__ Cache(const uint8_t* cache, const int32_t* block_table, const Table& t, int req, int h)
       : rows(reinterpret_cast<const char*>(cache)),
-        pages((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(block_table + (int64_t)q.req * t.max_pages)),
+        pages((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(block_table + (int64_t)req * t.max_pages)),
         page_shift(t.page_shift), kv_heads(t.kv_heads), head(h) {}
   // page of a (wave-uniform) key, and where the head's rows of a page begin
   __device__ __forceinline__ int32_t page_id(int key) const { return pages[__builtin_amdgcn_readfirstlane(key >> page_shift)]; }
@@ -209,15 +212,55 @@ __device__ __forceinline__ void own_writes() {
 }
 
 // --- few rows ---------------------------------------------------------------------------------------------------------------
+template <int MAXREQ>
+struct Mx4FewArgs {
+  Mx4FewTable<MAXREQ> table;
+  float scale_log2;
+  float* part_o;
+  float* part_ml;
+  uint16_t* out;
+};
+
+// A wave's copy of the table, 64 requests to a load, all asked for at once.
+template <int MAXREQ>
+struct FewLanes {
+  static constexpr int kLoads = (MAXREQ + 63) / 64;
+  int group_start[kLoads], parts[kLoads], split_start[kLoads], slot_start[kLoads], req[kLoads], cached[kLoads], new_len[kLoads], row_start[kLoads];
+  int nreq, lane;
+  __device__ __forceinline__ FewLanes(const Mx4FewTable<MAXREQ>& t, int l) : nreq(t.nreq), lane(l) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int k = min(i * 64 + l, t.nreq - 1);
+      group_start[i] = t.group_start[k];
+      parts[i] = t.parts[k];
+      split_start[i] = t.split_start[k];
+      slot_start[i] = t.slot_start[k];
+      req[i] = t.req[k];
+      cached[i] = t.cached[k];
+      new_len[i] = t.new_len[k];
+      row_start[i] = t.row_start[k];
+    }
+  }
+  // the last request that starts at or in front of a workgroup or split tile
+  __device__ __forceinline__ int find(const int (&starts)[kLoads], int index) const {
+    int r = -1;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) r += __popcll(__ballot(i * 64 + lane < nreq && starts[i] <= index));
+    return __builtin_amdgcn_readfirstlane(r);
+  }
+  __device__ __forceinline__ int of(const int (&field)[kLoads], int r) const {
+    return __builtin_amdgcn_readlane(kLoads == 2 && r >= 64 ? field[kLoads - 1] : field[0], r & 63);
+  }
+};
+
 // NB blocks of 16 query rows.  The four waves share the rows: of each 128 keys a wave takes 32, with a maximum and sums of its
 // own, and their sums are combined at the part's end.  A wave's keys go from memory to registers, where they are the product's
 // operands as they are converted; a lane has 16 (D 128; 8) bytes of a row's codes, all under one scale, and the query operands
 // follow that order of elements.
-template <int D, int NB>
-__global__ __launch_bounds__(kThreads) void mx4_few_kernel(const Mx4Args args, const uint16_t* __restrict__ q,
-                                                           const uint8_t* __restrict__ k_cache, const uint8_t* __restrict__ v_cache,
-                                                           const int32_t* __restrict__ block_table) {
-  constexpr int kRows = 16 * NB;
+template <int D, int NB, int MAXREQ>
+__global__ __launch_bounds__(kThreads, NB == 1 ? 3 : 2) void mx4_few_kernel(
+    const Mx4FewArgs<MAXREQ> args, const uint16_t* __restrict__ q, const uint8_t* __restrict__ k_cache,
+    const uint8_t* __restrict__ v_cache, const int32_t* __restrict__ block_table) {
   constexpr int kSteps = D / 32;           // products over the head dimension
   constexpr int kBlocks = D / 16;          // output blocks
   constexpr int kKeyBytes = D / 8;         // of a row's codes, in a lane
@@ -226,7 +269,7 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(const Mx4Args args, c
   constexpr int kRowBytes = 2 * D;         // of a bf16 row in LDS
   constexpr int kTileBytes = 32 * kRowBytes;
   constexpr int kPitch = D + 4;            // floats from row to row of the sums
-  constexpr int kSumBytes = kWaves * kRows * (kPitch + 2) * 4;
+  constexpr int kSumBytes = kWaves * 16 * (kPitch + 2) * 4;
   constexpr int kLds = kWaves * kTileBytes > kSumBytes ? kWaves * kTileBytes : kSumBytes;
   __shared__ __attribute__((aligned(1024))) char lds[kLds];
   __shared__ uint32_t s_torn[kWaves];  // whether the wave met a value block that is no number
@@ -235,218 +278,356 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(const Mx4Args args, c
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, q4 = lane >> 4;
-  const Mx4Table& t = args.table;
-  const int g = t.group_heads, hq = g * t.kv_heads;
+  const auto& t = args.table;
+  const int g = t.group_heads, hq = g * t.kv_heads, page_shift = t.page_shift;
   const uint32_t tile = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + wave * kTileBytes;
 
-  for (Share<kRows, kMx4FewKeys> it(t, lane); !it.done(); it.advance()) {
-    const Cache<D> keys(k_cache, block_table, t, it.rq, it.at.head), values(v_cache, block_table, t, it.rq, it.at.head);
-    const int last = it.k1 - 1;
-    bf16x8 qb[NB][kSteps];
-    int visible[NB];  // keys that the row sees
+  // the workgroup's part
+  const FewLanes<MAXREQ> requests(t, lane);
+  const int group = blockIdx.x;
+  const int r = requests.find(requests.group_start, group);
+  const int in = group - requests.of(requests.group_start, r), parts = requests.of(requests.parts, r);
+  const int head = in / parts, cached = requests.of(requests.cached, r);
+  const int rows = requests.of(requests.new_len, r) * g, row_start = requests.of(requests.row_start, r);
+  const int all_keys = cached + requests.of(requests.new_len, r);
+  const int units = (all_keys + kMx4FewKeys - 1) / kMx4FewKeys;
+  const int k0 = mx4_first_of(units, parts, in - head * parts) * kMx4FewKeys;
+  const int k1 = min(mx4_first_of(units, parts, in - head * parts + 1) * kMx4FewKeys, all_keys);
+  const int slot = parts == 1 ? -1 : requests.of(requests.slot_start, r) + in;
+  const Cache<D> keys(k_cache, block_table, t, requests.of(requests.req, r), head);
+  const Cache<D> values(v_cache, block_table, t, requests.of(requests.req, r), head);
+  const int last = k1 - 1;
+
+  struct Pages {  // of eight keys each
+    int32_t id[4];
+  };
+  auto look_up = [&](int key0) __attribute__((always_inline)) {
+    Pages p;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const int row = n * 16 + i16;
-      const int tok = row / g;
-      visible[n] = row < it.rows ? it.rq.cached + tok + 1 : 0;
-      const uint16_t* src = q + ((int64_t)(it.rq.row_start + tok) * hq + it.at.head * g + (row - tok * g)) * D + q4 * (D / 4);
+    for (int e = 0; e < 4; ++e) p.id[e] = keys.page_id(min(key0 + 8 * e, last));
+    return p;
+  };
+  struct Chunk {  // codes and scales of 32 keys
+    KeyCodes k[2];
+    uint32_t ks[2];
+    u32x4 v[kValueLoads];
+    uint32_t vs[kValueLoads];
+  };
+  const int v_row = lane / kValueLanes, v_piece = lane % kValueLanes;
+  const uint32_t k_code = i16 * mx4_code_bytes(D) + q4 * kKeyBytes, k_scale = i16 * mx4_scale_bytes(D) + (D == 128 ? q4 : q4 >> 1);
+  const uint32_t v_code = v_row * mx4_code_bytes(D) + v_piece * 16, v_scale = v_row * mx4_scale_bytes(D) + v_piece;
+  auto load = [&](int key0, const Pages& p, Chunk& c) __attribute__((always_inline)) {
+    if (page_shift >= 4 && key0 + 32 <= k1) {
+      // sixteen rows lie in one page: wave-uniform bases, the lane's place in them is known
+      int64_t codes[2], scales[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int64_t page = keys.page_at(p.id[2 * b]);
+        codes[b] = page + keys.code_at(key0 + 16 * b);
+        scales[b] = page + keys.scale_at(key0 + 16 * b);
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        c.k[b] = *reinterpret_cast<const KeyCodes*>(keys.rows + codes[b] + k_code);
+        c.ks[b] = *reinterpret_cast<const uint8_t*>(keys.rows + scales[b] + k_scale);
+      }
+#pragma unroll
+      for (int j = 0; j < kValueLoads; ++j) {
+        int64_t code = codes[j], scale = scales[j];
+        if constexpr (kValueLoads == 1) {  // (32 rows to a load, the second sixteen from their own base)
+          const int64_t code2 = codes[1] - 16 * mx4_code_bytes(D), scale2 = scales[1] - 16 * mx4_scale_bytes(D);
+          code = v_row < 16 ? code : code2;
+          scale = v_row < 16 ? scale : scale2;
+        }
+        c.v[j] = *reinterpret_cast<const u32x4*>(values.rows + code + v_code);
+        c.vs[j] = *reinterpret_cast<const uint8_t*>(values.rows + scale + v_scale);
+      }
+      return;
+    }
+    int64_t at_page[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) at_page[e] = keys.page_at(p.id[e]);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int key = min(key0 + b * 16 + i16, last);
+      const int64_t low = at_page[2 * b], high = at_page[2 * b + 1];  // (values: chosen between where they lie they would be memory)
+      const char* page = keys.rows + (i16 & 8 ? high : low);
+      c.k[b] = *reinterpret_cast<const KeyCodes*>(page + keys.code_at(key) + q4 * kKeyBytes);
+      c.ks[b] = *reinterpret_cast<const uint8_t*>(page + keys.scale_at(key) + (D == 128 ? q4 : q4 >> 1));
+    }
+#pragma unroll
+    for (int j = 0; j < kValueLoads; ++j) {
+      const int row = j * (64 / kValueLanes) + v_row;
+      const int key = min(key0 + row, last);
+      const int64_t low = at_page[2 * j], high = at_page[2 * j + 1];
+      int64_t at = row & 8 ? high : low;
+      if constexpr (kValueLoads == 1) {
+        const int64_t low2 = at_page[2], high2 = at_page[3];
+        at = row & 16 ? (row & 8 ? high2 : low2) : at;
+      }
+      const char* page = values.rows + at;
+      c.v[j] = *reinterpret_cast<const u32x4*>(page + values.code_at(key) + v_piece * 16);
+      c.vs[j] = *reinterpret_cast<const uint8_t*>(page + values.scale_at(key) + v_piece);
+    }
+  };
+
+  Chunk even, odd;
+  int key0 = k0 + wave * 32;
+  Pages pages = look_up(key0);
+  // queries
+  bf16x8 qb[NB][kSteps];
+  int visible[NB];  // keys that the row sees
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const int row = n * 16 + i16, tok = row / g;
+    visible[n] = row < rows ? cached + tok + 1 : 0;
+    const uint16_t* src = q + ((int64_t)(row_start + tok) * hq + head * g + (row - tok * g)) * D + q4 * (D / 4);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      u32x4 v = {0, 0, 0, 0};
+      if (row < rows) v = *reinterpret_cast<const u32x4*>(src + 8 * s);
+      qb[n][s] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  f32x4 o[NB][kBlocks];
+  float m_run[NB], l_run[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[n] = kNoReference;
+    l_run[n] = 0.f;
+  }
+  bool torn = false;
+
+  auto work = [&](int key0, Chunk& c) __attribute__((always_inline)) {
+    // scores
+    f32x4 sc[NB][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const float scale = mx4_scale_value(c.ks[b]);
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
-        u32x4 v = {0, 0, 0, 0};
-        if (row < it.rows) v = *reinterpret_cast<const u32x4*>(src + 8 * s);
-        qb[n][s] = __builtin_bit_cast(bf16x8, v);
+        const bf16x8 ka = __builtin_bit_cast(bf16x8, mx4_decode8(c.k[b][s], scale));
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          if (s == 0) sc[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+          sc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qb[n][s], sc[n][b], 0, 0, 0);
+        }
       }
     }
-    f32x4 o[NB][kBlocks];
-    float m_run[NB], l_run[NB];
+    // values, as bf16 rows to LDS
+    own_writes();
+#pragma unroll
+    for (int j = 0; j < kValueLoads; ++j) {
+      if (__any(c.vs[j] >= kTorn)) {
+        torn = true;
+        if (c.vs[j] >= kTorn) {
+          c.v[j] = u32x4{0, 0, 0, 0};
+          c.vs[j] = 127;
+        }
+      }
+      const float scale = mx4_scale_value(c.vs[j]);
+      const int key = j * (64 / kValueLanes) + v_row;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        *(LDS_PTR(mx4_words))(uintptr_t)(tile + key * kRowBytes + (((v_piece * 4 + w) ^ value_swizzle16<D>(key)) << 4)) = mx4_decode8(c.v[j][w], scale);
+    }
+    own_writes();
+    // Probabilities.  No maximum is formed on the way: the reference of a row is a maximum that was, and a chunk whose weights
+    // sum to 2^kSlack in a lane is looked at again.
+    bf16x8 pb[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
+      if (key0 + 32 > min(cached + 1, k1)) {
+        const int end = min(visible[n], k1) - key0 - q4 * 4;
 #pragma unroll
-      for (int d = 0; d < kBlocks; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m_run[n] = -INFINITY;
-      l_run[n] = 0.f;
-    }
-    uint32_t torn = 0;
-
-    struct Chunk {  // codes and scales of 32 keys
-      KeyCodes k[2];
-      uint32_t ks[2];
-      u32x4 v[kValueLoads];
-      uint32_t vs[kValueLoads];
-    };
-    struct Pages {  // of eight keys each
-      int32_t id[4];
-    };
-    auto look_up = [&](int key0) __attribute__((always_inline)) {
-      Pages p;
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p.id[e] = keys.page_id(min(key0 + 8 * e, last));
-      return p;
-    };
-    auto load = [&](int key0, const Pages& p, Chunk& c) __attribute__((always_inline)) {
-      int64_t at_page[4];  // of keys and of values
-#pragma unroll
-      for (int e = 0; e < 4; ++e) at_page[e] = keys.page_at(p.id[e]);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int key = min(key0 + b * 16 + i16, last);
-        const char* page = keys.rows + (i16 & 8 ? at_page[2 * b + 1] : at_page[2 * b]);
-        c.k[b] = *reinterpret_cast<const KeyCodes*>(page + keys.code_at(key) + q4 * kKeyBytes);
-        c.ks[b] = *reinterpret_cast<const uint8_t*>(page + keys.scale_at(key) + (D == 128 ? q4 : q4 >> 1));
+          for (int e = 0; e < 4; ++e)
+            if (b * 16 + e >= end) sc[n][b][e] = -INFINITY;
       }
+      u32x4 p;
+      auto weigh = [&]() __attribute__((always_inline)) {
+        float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < kValueLoads; ++j) {
-        const int in = j * (64 / kValueLanes) + lane / kValueLanes;
-        const int key = min(key0 + in, last);
-        int64_t at = in & 8 ? at_page[2 * j + 1] : at_page[2 * j];
-        if constexpr (kValueLoads == 1) at = in & 16 ? (in & 8 ? at_page[3] : at_page[2]) : at;
-        const char* page = values.rows + at;
-        c.v[j] = *reinterpret_cast<const u32x4*>(page + values.code_at(key) + lane % kValueLanes * 16);
-        c.vs[j] = *reinterpret_cast<const uint8_t*>(page + values.scale_at(key) + lane % kValueLanes);
-      }
-    };
-    Chunk next;
-    int key0 = it.k0 + wave * 32;
-    Pages pages = look_up(key0);
-    if (key0 < it.k1) load(key0, pages, next);
-    pages = look_up(key0 + kMx4FewKeys);
-    for (; key0 < it.k1; key0 += kMx4FewKeys) {
-      const Chunk c = next;
-      if (key0 + kMx4FewKeys < it.k1) load(key0 + kMx4FewKeys, pages, next);
-      pages = look_up(key0 + 2 * kMx4FewKeys);
-      // scores
-      f32x4 sc[NB][2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const float scale = mx4_scale_value(c.ks[b]);
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const bf16x8 ka = __builtin_bit_cast(bf16x8, mx4_decode8(c.k[b][s], scale));
-#pragma unroll
-          for (int n = 0; n < NB; ++n) {
-            if (s == 0) sc[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-            sc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qb[n][s], sc[n][b], 0, 0, 0);
-          }
+        for (int e = 0; e < 4; ++e) {
+          const float x = __builtin_amdgcn_exp2f(sc[n][e >> 1][(e & 1) * 2] * args.scale_log2 - m_run[n]);
+          const float y = __builtin_amdgcn_exp2f(sc[n][e >> 1][(e & 1) * 2 + 1] * args.scale_log2 - m_run[n]);
+          p[e] = pack_bf16(x, y);
+          sum = add_pair(p[e], sum);
         }
-      }
-      // values, as bf16 rows to LDS
-      own_writes();
-#pragma unroll
-      for (int j = 0; j < kValueLoads; ++j) {
-        const int key = j * (64 / kValueLanes) + lane / kValueLanes;
-        const bool bad = c.vs[j] >= kTorn;
-        torn |= bad;
-        const float scale = bad ? 1.f : mx4_scale_value(c.vs[j]);
-        const uint32_t to = tile + key * kRowBytes;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int chunk = (lane % kValueLanes * 4 + w) ^ value_swizzle16<D>(key);
-          *(LDS_PTR(mx4_words))(uintptr_t)(to + chunk * 16) = mx4_decode8(bad ? 0u : c.v[j][w], scale);
-        }
-      }
-      own_writes();
-      // probabilities
-      bf16x8 pb[NB];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const int lim = visible[n] - key0 - q4 * 4;
-        if (key0 + 32 > it.rq.cached + 1 || key0 + 32 > it.k1) {
-          const int end = min(lim, it.k1 - key0 - q4 * 4);
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (b * 16 + r >= end) sc[n][b][r] = -INFINITY;
-        }
+        return sum;
+      };
+      float sum = weigh();
+      if (__any(sum >= kOver)) {
         float top = max3(max3(sc[n][0][0], sc[n][0][1], sc[n][0][2]), sc[n][0][3], max3(sc[n][1][0], sc[n][1][1], sc[n][1][2]));
         top = cross_half_max(cross_quarter_max(fmaxf(top, sc[n][1][3]))) * args.scale_log2;
-        const bool grow = top > m_run[n] + kSlack;
-        if (__any(grow)) {
-          // (a row is moved by its own scores alone, whatever the other rows of the wave hold)
-          const float m_next = grow ? top : m_run[n];
-          const float alpha = __builtin_amdgcn_exp2f(m_run[n] - (m_next == -INFINITY ? 0.f : m_next));
-          l_run[n] *= alpha;
+        // (a row is moved by its own scores alone, whatever the other rows of the wave hold)
+        const float m_next = top > m_run[n] + kSlack ? top : m_run[n];
+        const float f = m_next == m_run[n] ? 1.f : __builtin_amdgcn_exp2f(m_run[n] - m_next);
+        l_run[n] *= f;
 #pragma unroll
-          for (int d = 0; d < kBlocks; ++d) o[n][d] *= alpha;
-          m_run[n] = m_next;
-        }
-        const float m_use = m_run[n] == -INFINITY ? 0.f : m_run[n];
-        u32x4 p;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float a = __builtin_amdgcn_exp2f(sc[n][r >> 1][(r & 1) * 2] * args.scale_log2 - m_use);
-          const float b = __builtin_amdgcn_exp2f(sc[n][r >> 1][(r & 1) * 2 + 1] * args.scale_log2 - m_use);
-          p[r] = pack_bf16(a, b);
-          l_run[n] = add_pair(p[r], l_run[n]);
-        }
-        pb[n] = __builtin_bit_cast(bf16x8, p);
+        for (int d = 0; d < kBlocks; ++d) o[n][d] *= f;
+        m_run[n] = m_next;
+        sum = weigh();
       }
-      // outputs
-      const int w16 = lane & 15;
-      const int v_key = 4 * q4 + (w16 >> 2);
-      const uint32_t v_at = tile + v_key * kRowBytes + (w16 & 1) * 8;
-#pragma unroll
-      for (int d = 0; d < kBlocks; ++d) {
-        const uint32_t at = v_at + (((2 * d + ((w16 & 3) >> 1)) ^ value_swizzle16<D>(v_key)) << 4);
-        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)at);
-        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + 16 * kRowBytes));
-        const bf16x8 va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n], o[n][d], 0, 0, 0);
-      }
+      l_run[n] += sum;
+      pb[n] = __builtin_bit_cast(bf16x8, p);
     }
+    // outputs
+    const int v_key = 4 * q4 + (i16 >> 2);
+    const uint32_t v_at = tile + v_key * kRowBytes + (i16 & 1) * 8;
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) {
+      const uint32_t at = v_at + (((2 * d + ((i16 & 3) >> 1)) ^ value_swizzle16<D>(v_key)) << 4);
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)at);
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + 16 * kRowBytes));
+      const bf16x8 va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n], o[n][d], 0, 0, 0);
+    }
+  };
+  if (key0 < k1) load(key0, pages, even);
+  pages = look_up(key0 + kMx4FewKeys);
+  while (key0 < k1) {
+    if (key0 + kMx4FewKeys < k1) load(key0 + kMx4FewKeys, pages, odd);
+    pages = look_up(key0 + 2 * kMx4FewKeys);
+    work(key0, even);
+    key0 += kMx4FewKeys;
+    if (key0 >= k1) break;
+    if (key0 + kMx4FewKeys < k1) load(key0 + kMx4FewKeys, pages, even);
+    pages = look_up(key0 + 2 * kMx4FewKeys);
+    work(key0, odd);
+    key0 += kMx4FewKeys;
+  }
 
-    // the waves' sums, rescaled to the largest reference: M = max m,  O = sum 2^(m - M) O_w
-    const bool met = __any(torn != 0);
-    if (lane == 0) s_torn[wave] = met;
-    float* xo = reinterpret_cast<float*>(lds);   // [wave][row] x kPitch
-    float* xm = xo + kWaves * kRows * kPitch;    // [wave][row]
-    float* xl = xm + kWaves * kRows;
-    __syncthreads();  // every wave is done with its tile
+  // The waves' sums, rescaled to the largest reference: M = max m,  O = sum 2^(m - M) O_w.  A block of rows at a time.
+  if (lane == 0) s_torn[wave] = torn;
+  float* xo = reinterpret_cast<float*>(lds);  // [wave][row] x kPitch
+  float* xm = xo + kWaves * 16 * kPitch;      // [wave][row]
+  float* xl = xm + kWaves * 16;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const int row = wave * kRows + n * 16 + i16;
+  for (int n = 0; n < NB; ++n) {
+    if (n * 16 >= rows) break;
+    __syncthreads();  // every wave is done with its tile, or with the block in front
 #pragma unroll
-      for (int d = 0; d < kBlocks; ++d) *reinterpret_cast<f32x4*>(xo + row * kPitch + d * 16 + q4 * 4) = o[n][d];
-      const float l = cross_half_sum(cross_quarter_sum(l_run[n]));
-      if (q4 == 0) {
-        xm[row] = m_run[n];
-        xl[row] = l;
-      }
+    for (int d = 0; d < kBlocks; ++d) *reinterpret_cast<f32x4*>(xo + (wave * 16 + i16) * kPitch + d * 16 + q4 * 4) = o[n][d];
+    const float l_wave = cross_half_sum(cross_quarter_sum(l_run[n]));
+    if (q4 == 0) {
+      xm[wave * 16 + i16] = m_run[n];
+      xl[wave * 16 + i16] = l_wave;
     }
     __syncthreads();
     constexpr int kVec = D / 4;  // threads of a row
     const int c = tid % kVec * 4;
-    for (int row = tid / kVec; row < it.rows; row += kThreads / kVec) {
-      float m[kWaves], top = -INFINITY;
+    for (int in_block = tid / kVec; in_block < min(16, rows - n * 16); in_block += kThreads / kVec) {
+      const int row = n * 16 + in_block;
+      float m[kWaves], top = kNoReference;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        m[w] = xm[w * kRows + row];
+        m[w] = xm[w * 16 + in_block];
         top = fmaxf(top, m[w]);
       }
       float l = 0.f;
       f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float f = m[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[w] - top);
-        l += f * xl[w * kRows + row];
-        v += f * *reinterpret_cast<const f32x4*>(xo + (w * kRows + row) * kPitch + c);
+        const float f = __builtin_amdgcn_exp2f(m[w] - top);
+        l += f * xl[w * 16 + in_block];
+        v += f * *reinterpret_cast<const f32x4*>(xo + (w * 16 + in_block) * kPitch + c);
       }
       const int tok = row / g;
       if (s_torn[0] | s_torn[1] | s_torn[2] | s_torn[3]) {
-        for (int key = it.k0; key < min(it.k1, it.rq.cached + tok + 1); ++key)
+        for (int key = k0; key < min(k1, cached + tok + 1); ++key)
           if (values.torn_blocks(key) >> (c / kMx4Block) & 1) v = f32x4{NAN, NAN, NAN, NAN};
       }
-      if (it.slot < 0) {
+      if (slot < 0) {
         const float inv = 1.f / l;
         const u32x2 words = {pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
-        *reinterpret_cast<u32x2*>(args.out + ((int64_t)(it.rq.row_start + tok) * hq + it.at.head * g + (row - tok * g)) * D + c) = words;
+        *reinterpret_cast<u32x2*>(args.out + ((int64_t)(row_start + tok) * hq + head * g + (row - tok * g)) * D + c) = words;
       } else {
-        *reinterpret_cast<f32x4*>(args.part_o + (it.slot * kRows + row) * D + c) = v;
-        if (c == 0) *reinterpret_cast<f32x2*>(args.part_ml + (it.slot * kRows + row) * 2) = f32x2{top, l};
+        const int64_t part = (int64_t)slot * (16 * NB) + row;
+        *reinterpret_cast<f32x4*>(args.part_o + part * D + c) = v;
+        if (c == 0) *reinterpret_cast<f32x2*>(args.part_ml + part * 2) = f32x2{top, l};
       }
     }
-    __syncthreads();
+  }
+}
+
+// The parts of a split tile: with M = max m_s,  out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A workgroup for each; where it has
+// more threads than the rows need, they share the parts and are joined through LDS.  Bound by latency: four parts at a time.
+template <int D, int ROWS, int MAXREQ>
+__global__ __launch_bounds__(kThreads) void mx4_few_join_kernel(const Mx4FewArgs<MAXREQ> args) {
+  constexpr int kVec = D / 4;                // threads of a row
+  constexpr int kPlaces = kThreads / kVec;   // rows (and slices of their parts) at a time
+  constexpr int kAtOnce = 4;
+  __shared__ __attribute__((aligned(16))) float s_o[kPlaces][D];
+  __shared__ float s_m[kPlaces], s_l[kPlaces];
+  const auto& t = args.table;
+  const int g = t.group_heads, hq = g * t.kv_heads;
+  const FewLanes<MAXREQ> requests(t, threadIdx.x & 63);
+  const int r = requests.find(requests.split_start, blockIdx.x);
+  const int head = blockIdx.x - requests.of(requests.split_start, r), parts = requests.of(requests.parts, r);
+  const int rows = requests.of(requests.new_len, r) * g, row_start = requests.of(requests.row_start, r);
+  const int64_t first = requests.of(requests.slot_start, r) + (int64_t)head * parts;
+  const int c = threadIdx.x % kVec * 4, place = threadIdx.x / kVec;
+  int at_once = 1;  // rows at a time
+  while (at_once < rows && at_once < kPlaces) at_once *= 2;
+  const int slices = kPlaces / at_once, slice = place / at_once;
+  // (where the rows are fewer than the places they are the first workgroup's, else a workgroup has as many as there are places)
+  for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {
+    const int row = min(row0 + place % at_once, rows - 1);
+    float m = kNoReference, l = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = slice; s0 < parts; s0 += kAtOnce * slices) {
+      f32x2 ml[kAtOnce];
+      f32x4 x[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t part = (first + min(s0 + i * slices, parts - 1)) * ROWS + row;
+        ml[i] = *reinterpret_cast<const f32x2*>(args.part_ml + part * 2);
+        x[i] = *reinterpret_cast<const f32x4*>(args.part_o + part * D + c);
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i][0]);
+      const float back = __builtin_amdgcn_exp2f(m - top);
+      l *= back;
+      v *= back;
+      m = top;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        if (s0 + i * slices >= parts) break;
+        const float f = __builtin_amdgcn_exp2f(ml[i][0] - top);
+        l += f * ml[i][1];
+        v += f * x[i];
+      }
+    }
+    if (slices > 1) {
+      *reinterpret_cast<f32x4*>(&s_o[place][c]) = v;
+      if (c == 0) {
+        s_m[place] = m;
+        s_l[place] = l;
+      }
+      __syncthreads();
+      if (slice > 0) continue;
+      float top = m;
+      for (int i = 1; i < slices; ++i) top = fmaxf(top, s_m[i * at_once + place]);
+      const float back = __builtin_amdgcn_exp2f(m - top);
+      l *= back;
+      v *= back;
+      for (int i = 1; i < slices; ++i) {
+        const float f = __builtin_amdgcn_exp2f(s_m[i * at_once + place] - top);
+        l += f * s_l[i * at_once + place];
+        v += f * *reinterpret_cast<const f32x4*>(&s_o[i * at_once + place][c]);
+      }
+    }
+    if (row0 + place % at_once >= rows) continue;
+    const float inv = 1.f / l;
+    const int tok = row / g;
+    *reinterpret_cast<u32x2*>(args.out + ((int64_t)(row_start + tok) * hq + head * g + (row - tok * g)) * D + c) =
+        u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
   }
 }
 
@@ -483,7 +664,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
   const int first_matrix = kLoads == 2 ? 0 : __builtin_amdgcn_readfirstlane(tid / (kLanes * kMx4ManyKeys));
 
   for (Share<kMx4ManyRows, kMx4ManyKeys> it(t, lane); !it.done(); it.advance()) {
-    const Cache<D> cache(k_cache, block_table, t, it.rq, it.at.head);
+    const Cache<D> cache(k_cache, block_table, t, it.rq.req, it.at.head);
     const int ntiles = (it.k1 - it.k0 + kMx4ManyKeys - 1) / kMx4ManyKeys;
     const int local = wave * 32 + i32;
     const bool row_ok = local < it.rows;
@@ -609,7 +790,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
     if (row_ok) {
       const float l = cross_half_sum(l_run);
       if (s_torn[0] | s_torn[1] | s_torn[2] | s_torn[3]) {
-        const Cache<D> values(v_cache, block_table, t, it.rq, it.at.head);
+        const Cache<D> values(v_cache, block_table, t, it.rq.req, it.at.head);
         uint32_t lost = 0;
         for (int key = it.k0; key < min(it.k1, visible); ++key) lost |= values.torn_blocks(key);
 #pragma unroll
@@ -680,46 +861,72 @@ struct Mx4Tensors {
   const uint16_t* q;
   const uint8_t *k_cache, *v_cache;
   const int32_t* block_table;
+  uint16_t* out;
+  float scale_log2;
 };
 
-template <int D>
-int launch_class(const efim_batch_t* b, const Mx4Plan& plan, Mx4Args* args, const Mx4Tensors& x, hipStream_t stream) {
+int last_error() {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return EFIM_OK;
+  set_last_hip_error(e);
+  return EFIM_ERR_LAUNCH;
+}
+
+template <int D, int NB, int MAXREQ>
+int launch_few(const efim_batch_t* b, const Mx4FewPlan& plan, const Mx4Tensors& x, char* workspace, hipStream_t stream) {
+  Mx4FewArgs<MAXREQ> args;
+  args.scale_log2 = x.scale_log2;
+  args.part_o = reinterpret_cast<float*>(workspace);
+  args.part_ml = reinterpret_cast<float*>(workspace + mx4_bytes(plan.slots, plan.row_tile, D).off_ml);
+  args.out = x.out;
   Mx4Cursor at;
-  while (mx4_next(b, plan, &at, &args->table)) {
-    const int groups = args->table.groups;
-    const dim3 grid((unsigned)((groups + kXcdCount - 1) / kXcdCount * kXcdCount));
-    auto join = [&](auto rows, auto keys) {
-      constexpr int kAtOnce = kThreads / (D / 4);
-      if (groups > 1)
-        mx4_join_kernel<D, decltype(rows)::value, decltype(keys)::value>
-            <<<dim3((unsigned)groups - 1, (unsigned)((decltype(rows)::value + 4 * kAtOnce - 1) / (4 * kAtOnce))), kThreads, 0, stream>>>(*args);
-    };
-    if (!plan.few) {
-      mx4_many_kernel<D><<<grid, kThreads, 0, stream>>>(*args, x.q, x.k_cache, x.v_cache, x.block_table);
-      join(std::integral_constant<int, kMx4ManyRows>{}, std::integral_constant<int, kMx4ManyKeys>{});
-    } else if (plan.row_tile == 16) {
-      mx4_few_kernel<D, 1><<<grid, kThreads, 0, stream>>>(*args, x.q, x.k_cache, x.v_cache, x.block_table);
-      join(std::integral_constant<int, 16>{}, std::integral_constant<int, kMx4FewKeys>{});
-    } else {
-      mx4_few_kernel<D, 2><<<grid, kThreads, 0, stream>>>(*args, x.q, x.k_cache, x.v_cache, x.block_table);
-      join(std::integral_constant<int, 32>{}, std::integral_constant<int, kMx4FewKeys>{});
-    }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) { set_last_hip_error(e); return EFIM_ERR_LAUNCH; }
+  while (mx4_next(b, plan, &at, &args.table)) {
+    mx4_few_kernel<D, NB, MAXREQ><<<args.table.groups, kThreads, 0, stream>>>(args, x.q, x.k_cache, x.v_cache, x.block_table);
+    if (args.table.splits > 0) mx4_few_join_kernel<D, 16 * NB, MAXREQ><<<dim3((unsigned)args.table.splits, (16 * NB + kThreads / (D / 4) - 1) / (kThreads / (D / 4))), kThreads, 0, stream>>>(args);
+    const int rc = last_error();
+    if (rc != EFIM_OK) return rc;
   }
   return EFIM_OK;
 }
 
+template <int D>
+int launch_many(const efim_batch_t* b, const Mx4ManyPlan& plan, const Mx4Tensors& x, char* workspace, hipStream_t stream) {
+  Mx4Args args;
+  args.scale_log2 = x.scale_log2;
+  args.part_o = reinterpret_cast<float*>(workspace);
+  args.part_ml = reinterpret_cast<float*>(workspace + mx4_bytes(2 * (size_t)plan.max_groups, kMx4ManyRows, D).off_ml);
+  args.out = x.out;
+  constexpr int kAtOnce = kThreads / (D / 4);
+  Mx4Cursor at;
+  while (mx4_next(b, plan, &at, &args.table)) {
+    const int groups = args.table.groups;
+    mx4_many_kernel<D><<<(groups + kXcdCount - 1) / kXcdCount * kXcdCount, kThreads, 0, stream>>>(args, x.q, x.k_cache, x.v_cache, x.block_table);
+    if (groups > 1)
+      mx4_join_kernel<D, kMx4ManyRows, kMx4ManyKeys>
+          <<<dim3((unsigned)groups - 1, (kMx4ManyRows + 4 * kAtOnce - 1) / (4 * kAtOnce)), kThreads, 0, stream>>>(args);
+    const int rc = last_error();
+    if (rc != EFIM_OK) return rc;
+  }
+  return EFIM_OK;
+}
+
+// The plans of a batch's two classes and where their partial results lie.
+struct Mx4Work {
+  Mx4FewPlan few;
+  Mx4ManyPlan many;
+  size_t many_at = 0, total = 0;
+  explicit Mx4Work(const efim_batch_t* b) : few(plan_mx4_few(b, compute_units())), many(plan_mx4_many(b, compute_units())) {
+    if (few.any) many_at = mx4_bytes(few.slots, few.row_tile, b->head_dim).total;
+    total = many_at + (many.any ? mx4_bytes(2 * (size_t)many.max_groups, kMx4ManyRows, b->head_dim).total : 0);
+    if (total < 256) total = 256;
+  }
+};
+
 int validate(const efim_batch_t* batch, int64_t* total) {
   const int rc = validate_batch(batch, total);
   if (rc != EFIM_OK) return rc;
-  return *total * batch->num_q_heads > (int64_t)1 << 30 ? EFIM_ERR_UNSUPPORTED : EFIM_OK;  // (rows are counted in 32 bits)
-}
-
-size_t workspace_bytes(const efim_batch_t* batch) {
-  size_t bytes = 0;
-  for (const bool few : {true, false}) bytes += mx4_bytes(plan_mx4(batch, few, compute_units()), batch->head_dim).total;
-  return bytes < 256 ? 256 : bytes;
+  // (rows and workgroups are counted in 32 bits)
+  return batch->num_kv_heads > 1 << 16 || *total * batch->num_q_heads > (int64_t)1 << 30 ? EFIM_ERR_UNSUPPORTED : EFIM_OK;
 }
 
 }  // namespace
@@ -730,7 +937,7 @@ extern "C" {
 size_t efim_mx4_workspace_bytes(const efim_batch_t* batch) {
   int64_t total = 0;
   if (efim::validate(batch, &total) != EFIM_OK) return 0;
-  return efim::workspace_bytes(batch);
+  return efim::Mx4Work(batch).total;
 }
 
 int efim_extend_attention_mx4(const efim_batch_t* batch, const void* q, const void* k_cache, const void* v_cache, void* out,
@@ -745,26 +952,23 @@ int efim_extend_attention_mx4(const efim_batch_t* batch, const void* q, const vo
   for (const void* p : {q, k_cache, v_cache, (const void*)out})
     if (!aligned16(p)) return EFIM_ERR_INVALID_ARG;
   if (!aligned4(batch->block_table)) return EFIM_ERR_INVALID_ARG;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < efim::workspace_bytes(batch))
-    return EFIM_ERR_WORKSPACE;
-  Mx4Args args;
+  const Mx4Work work(batch);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < work.total) return EFIM_ERR_WORKSPACE;
   const float scale = sm_scale == 0.f ? 1.f / sqrtf((float)batch->head_dim) : sm_scale;
-  args.scale_log2 = scale * 1.4426950408889634f;
-  args.out = static_cast<uint16_t*>(out);
-  const Mx4Tensors x{static_cast<const uint16_t*>(q), static_cast<const uint8_t*>(k_cache), static_cast<const uint8_t*>(v_cache),
-                     batch->block_table};
+  const Mx4Tensors x{static_cast<const uint16_t*>(q),     static_cast<const uint8_t*>(k_cache), static_cast<const uint8_t*>(v_cache),
+                     batch->block_table, static_cast<uint16_t*>(out), scale * 1.4426950408889634f};
+  hipStream_t s = static_cast<hipStream_t>(stream);
   char* at = static_cast<char*>(workspace);
-  for (const bool few : {true, false}) {
-    const Mx4Plan plan = plan_mx4(batch, few, compute_units());
-    if (!plan.any) continue;
-    const Mx4Bytes bytes = mx4_bytes(plan, batch->head_dim);
-    args.part_o = reinterpret_cast<float*>(at);
-    args.part_ml = reinterpret_cast<float*>(at + bytes.off_ml);
-    at += bytes.total;
-    auto* launch = batch->head_dim == 128 ? launch_class<128> : launch_class<64>;
-    const int done = launch(batch, plan, &args, x, static_cast<hipStream_t>(stream));
+  const bool wide = batch->head_dim == 128, small = batch->batch <= 64;
+  if (work.few.any) {
+    auto* launch = work.few.row_tile == 16 ? (wide ? (small ? launch_few<128, 1, 64> : launch_few<128, 1, kMx4FewReqs>)
+                                                   : (small ? launch_few<64, 1, 64> : launch_few<64, 1, kMx4FewReqs>))
+                                           : (wide ? (small ? launch_few<128, 2, 64> : launch_few<128, 2, kMx4FewReqs>)
+                                                   : (small ? launch_few<64, 2, 64> : launch_few<64, 2, kMx4FewReqs>));
+    const int done = launch(batch, work.few, x, at, s);
     if (done != EFIM_OK) return done;
   }
+  if (work.many.any) return (wide ? launch_many<128> : launch_many<64>)(batch, work.many, x, at + work.many_at, s);
   return EFIM_OK;
 }
 

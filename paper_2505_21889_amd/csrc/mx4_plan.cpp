@@ -7,52 +7,129 @@ namespace efim {
 
 namespace {
 
-bool is_few(const efim_batch_t* b, int r) {
-  return (int64_t)b->new_len[r] * (b->num_q_heads / b->num_kv_heads) <= kMx4FewRows;
+int group_of(const efim_batch_t* b) { return b->num_q_heads / b->num_kv_heads; }
+bool is_few(const efim_batch_t* b, int r) { return b->new_len[r] > 0 && (int64_t)b->new_len[r] * group_of(b) <= kMx4FewRows; }
+bool is_many(const efim_batch_t* b, int r) { return (int64_t)b->new_len[r] * group_of(b) > kMx4FewRows; }
+int page_shift_of(const efim_batch_t* b) {
+  int shift = 0;
+  while ((1 << shift) < b->page_size) ++shift;
+  return shift;
 }
+
+// Units of a request of few rows, and its parts of at most `most` of them.
+int few_units(const efim_batch_t* b, int r) {
+  return (int)(((int64_t)b->cached_len[r] + b->new_len[r] + kMx4FewKeys - 1) / kMx4FewKeys);
+}
+int few_parts(const efim_batch_t* b, int r, int most) { return (few_units(b, r) + most - 1) / most; }
 
 }  // namespace
 
-Mx4Plan plan_mx4(const efim_batch_t* b, bool few, int compute_units) {
-  Mx4Plan plan;
-  plan.few = few;
-  int64_t most = 0;
+Mx4FewPlan plan_mx4_few(const efim_batch_t* b, int compute_units) {
+  Mx4FewPlan plan;
+  int64_t most = 0, units = 0, tiles = 0;
+  int longest = 1;
   for (int r = 0; r < b->batch; ++r) {
-    if (b->new_len[r] == 0 || is_few(b, r) != few) continue;
+    if (!is_few(b, r)) continue;
     plan.any = true;
-    const int64_t rows = (int64_t)b->new_len[r] * (b->num_q_heads / b->num_kv_heads);
+    const int64_t rows = (int64_t)b->new_len[r] * group_of(b);
     most = rows > most ? rows : most;
+    const int mine = few_units(b, r);
+    longest = mine > longest ? mine : longest;
+    units += (int64_t)mine * b->num_kv_heads;
+    tiles += b->num_kv_heads;
   }
-  plan.row_tile = few ? (most <= 16 ? 16 : 32) : kMx4ManyRows;
-  plan.unit_keys = few ? kMx4FewKeys : kMx4ManyKeys;
-  plan.max_groups = compute_units * (few ? (plan.row_tile == 16 ? 4 : 2) : 2);
+  if (!plan.any) return plan;
+  plan.row_tile = most <= 16 ? 16 : 32;
+  // As many workgroups as the device holds at a time, none longer than it has to be; where the tiles alone are more than those,
+  // the ones of more than the mean work of a place are cut.  us with one, two, three and six times as many as there are compute
+  // units: 32 requests of 2048..8192 keys, 28/4 heads - / 29.3 / 28.2 / 33.5, 16 of 1024..4096 and 24 rows 28.5 / 27.0 / 33.5 / -.
+  // Parts of two units at least: with one the join of one request of 2344 keys, 32/8 heads takes longer (11.5, two 11.0, three 11.4),
+  // and short requests have one.
+  constexpr int kLeastUnits = 2;
+  const int64_t places = (int64_t)compute_units * (plan.row_tile == 16 ? 3 : 2);
+  int low = kLeastUnits, high = longest > low ? longest : low;
+  if (tiles >= places) {
+    low = high = (int)((units + places - 1) / places);
+  }
+  while (low < high) {
+    const int middle = (low + high) / 2;
+    int64_t groups = 0;
+    for (int r = 0; r < b->batch; ++r)
+      if (is_few(b, r)) groups += (int64_t)few_parts(b, r, middle) * b->num_kv_heads;
+    if (groups <= places) high = middle;
+    else low = middle + 1;
+  }
+  plan.part_units = low;
+  Mx4Cursor at;
+  Mx4FewTable<kMx4FewReqs> t;
+  while (mx4_next(b, plan, &at, &t)) plan.slots = t.slots > plan.slots ? t.slots : plan.slots;
   return plan;
 }
 
-Mx4Bytes mx4_bytes(const Mx4Plan& plan, int head_dim) {
+Mx4ManyPlan plan_mx4_many(const efim_batch_t* b, int compute_units) {
+  Mx4ManyPlan plan;
+  for (int r = 0; r < b->batch; ++r) plan.any = plan.any || is_many(b, r);
+  plan.max_groups = 2 * compute_units;
+  return plan;
+}
+
+Mx4Bytes mx4_bytes(size_t slots, int row_tile, int head_dim) {
   Mx4Bytes at;
-  if (!plan.any) return at;
-  const size_t rows = (size_t)2 * plan.max_groups * plan.row_tile;
+  const size_t rows = slots * row_tile;
   at.off_ml = rows * head_dim * sizeof(float);
   at.total = (at.off_ml + rows * 2 * sizeof(float) + 255) / 256 * 256;
   return at;
 }
 
-bool mx4_next(const efim_batch_t* b, const Mx4Plan& plan, Mx4Cursor* at, Mx4Table* t) {
+template <int MAXREQ>
+bool mx4_next(const efim_batch_t* b, const Mx4FewPlan& plan, Mx4Cursor* at, Mx4FewTable<MAXREQ>* t) {
+  t->nreq = t->groups = t->splits = t->slots = 0;
+  t->kv_heads = b->num_kv_heads;
+  t->group_heads = group_of(b);
+  t->max_pages = b->max_pages_per_req;
+  t->page_shift = page_shift_of(b);
+  for (; at->req < b->batch && t->nreq < MAXREQ; ++at->req) {
+    const int r = at->req;
+    if (is_few(b, r)) {
+      const int n = few_parts(b, r, plan.part_units);
+      const int64_t groups = (int64_t)n * t->kv_heads;
+      if (t->nreq > 0 && t->groups + groups > kMx4MostGroups) break;  // (a request alone has fewer than 2^30)
+      const int k = t->nreq++;
+      t->group_start[k] = t->groups;
+      t->parts[k] = n;
+      t->split_start[k] = t->splits;
+      t->slot_start[k] = t->slots;
+      t->req[k] = r;
+      t->cached[k] = b->cached_len[r];
+      t->new_len[k] = b->new_len[r];
+      t->row_start[k] = (int32_t)at->row;
+      t->groups += (int32_t)groups;
+      if (n > 1) {
+        t->splits += t->kv_heads;
+        t->slots += (int32_t)groups;
+      }
+    }
+    at->row += b->new_len[r];
+  }
+  return t->nreq > 0;
+}
+template bool mx4_next<64>(const efim_batch_t*, const Mx4FewPlan&, Mx4Cursor*, Mx4FewTable<64>*);
+template bool mx4_next<kMx4FewReqs>(const efim_batch_t*, const Mx4FewPlan&, Mx4Cursor*, Mx4FewTable<kMx4FewReqs>*);
+
+bool mx4_next(const efim_batch_t* b, const Mx4ManyPlan& plan, Mx4Cursor* at, Mx4Table* t) {
   t->nreq = 0;
   t->kv_heads = b->num_kv_heads;
-  t->group_heads = b->num_q_heads / b->num_kv_heads;
+  t->group_heads = group_of(b);
   t->max_pages = b->max_pages_per_req;
-  t->page_shift = 0;
-  while ((1 << t->page_shift) < b->page_size) ++t->page_shift;
+  t->page_shift = page_shift_of(b);
   int64_t units = 0;
   for (; at->req < b->batch && t->nreq < kMx4TableReqs; ++at->req) {
     const int n = b->new_len[at->req];
-    if (n > 0 && is_few(b, at->req) == plan.few) {
+    if (is_many(b, at->req)) {
       Mx4Req& q = t->req[t->nreq++];
       q = Mx4Req{units, 0, at->req, b->cached_len[at->req], n, (int32_t)at->row};
-      for (int tile = mx4_tiles(q, t->group_heads, plan.row_tile) - 1; tile >= 0; --tile)
-        q.units_per_head += mx4_units_of(q, t->group_heads, plan.row_tile, plan.unit_keys, tile);
+      for (int tile = mx4_tiles(q, t->group_heads, kMx4ManyRows) - 1; tile >= 0; --tile)
+        q.units_per_head += mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, tile);
       units += q.units_per_head * t->kv_heads;
     }
     at->row += n;

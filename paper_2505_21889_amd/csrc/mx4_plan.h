@@ -1,13 +1,8 @@
 // How the attention over a 4-bit cache cuts a batch into work.  Host code without state: a call derives everything from the
 // lengths and hands the kernels a table of the requests, from which each workgroup works its share out.
 //
-// A tile is `row_tile` query rows (token x head of the group) of a request and kv head.  Its work is a unit for each `unit_keys`
-// keys in front of and at the last one that its rows see.  The units of all tiles, one behind the other, are dealt evenly to the
-// workgroups: a share is a run of them, which may begin and end inside a tile.  The parts of a tile that several workgroups share
-// are joined by a second kernel.
-//
-// Requests of few rows and of many are different launches: a mixed step's single tokens would be multiplied as tiles of
-// mostly empty rows otherwise.
+// A tile is `row_tile` query rows (token x head of the group) of a request and kv head.  Requests of few rows and of many are
+// different launches: a mixed step's single tokens would be multiplied as tiles of mostly empty rows otherwise.
 #pragma once
 #include <cstddef>
 #include <cstdint>
@@ -22,7 +17,51 @@
 
 namespace efim {
 
-constexpr int kMx4TableReqs = 96;  // requests of a launch (kernel arguments end at 4 KB)
+constexpr int kMx4FewRows = 32;    // query rows of a request and kv head that the kernel for few rows takes
+constexpr int kMx4FewKeys = 128;   // keys of its units: 32 for each of its four waves
+constexpr int kMx4ManyRows = 128;  // row tile of the kernel for many rows
+constexpr int kMx4ManyKeys = 64;   // keys of its units
+
+// --- few rows ---------------------------------------------------------------------------------------------------------------
+// A request is one tile a kv head.  Its keys are cut into parts of as many units, a workgroup each; the parts of a tile that has
+// several are joined by a second kernel.
+template <int MAXREQ>
+struct Mx4FewTable {
+  int32_t group_start[MAXREQ];  // workgroups in front of the request in the launch
+  int32_t parts[MAXREQ];        // of each of its tiles
+  int32_t split_start[MAXREQ];  // split tiles in front of it
+  int32_t slot_start[MAXREQ];   // partial results in front of it
+  int32_t req[MAXREQ];          // block table row
+  int32_t cached[MAXREQ];       // C_r
+  int32_t new_len[MAXREQ];      // N_r > 0
+  int32_t row_start[MAXREQ];    // first packed new-token row
+  int32_t nreq;
+  int32_t groups;               // workgroups of the launch
+  int32_t splits;               // split tiles
+  int32_t slots;                // partial results
+  int32_t kv_heads;
+  int32_t group_heads;          // query heads of a kv head
+  int32_t max_pages;
+  int32_t page_shift;
+};
+constexpr int64_t kMx4MostGroups = 1 << 22;  // of a launch (its threads are counted in 32 bits)
+constexpr int kMx4FewReqs = 120;  // of a launch (kernel arguments end at 4 KB); batches of up to 64 take a smaller table
+
+// The first of a tile's units that part j of n has.
+EFIM_HOST_DEVICE inline int mx4_first_of(int units, int n, int j) { return units / n * j + (j < units % n ? j : units % n); }
+
+struct Mx4FewPlan {
+  bool any = false;    // the batch has such requests
+  int row_tile = 0;    // 16 or 32
+  int part_units = 0;  // the most units of a part
+  int slots = 0;       // partial results of the largest launch
+};
+
+// --- many rows --------------------------------------------------------------------------------------------------------------
+// A tile's work is a unit for each 64 keys in front of and at the last one that its rows see.  The units of all tiles, one behind
+// the other, are dealt evenly to the workgroups: a share is a run of them, which may begin and end inside a tile.  The parts of
+// a tile that several workgroups share are joined by a second kernel.
+constexpr int kMx4TableReqs = 96;  // requests of a launch
 
 struct Mx4Req {
   int64_t unit_start;      // units in front of the request in the launch
@@ -64,33 +103,28 @@ EFIM_HOST_DEVICE inline int mx4_units_of(const Mx4Req& q, int g, int row_tile, i
 // begins its tile.
 EFIM_HOST_DEVICE inline int64_t mx4_slot(int group, bool goes_on) { return 2 * (int64_t)group + (goes_on ? 0 : 1); }
 
-constexpr int kMx4FewRows = 32;    // query rows of a request and kv head that the kernel for few rows takes
-constexpr int kMx4FewKeys = 128;   // keys of its units: 32 for each of its four waves
-constexpr int kMx4ManyRows = 128;  // row tile of the kernel for many rows
-constexpr int kMx4ManyKeys = 64;
-
-// One class of requests (of few rows or of many) of a batch.
-struct Mx4Plan {
-  bool few = false;
-  int row_tile = 0;   // 16 or 32 (few), kMx4ManyRows
-  int unit_keys = 0;
-  int max_groups = 0; // workgroups to deal to
-  bool any = false;   // the batch has such requests
+struct Mx4ManyPlan {
+  bool any = false;
+  int max_groups = 0;  // workgroups to deal to
 };
-Mx4Plan plan_mx4(const efim_batch_t* b, bool few, int compute_units);
-
-// Workspace of a class: partial outputs [2 max_groups][row_tile][head_dim] and two floats (reference, sum) for each row of them.
-struct Mx4Bytes {
-  size_t off_ml = 0, total = 0;
-};
-Mx4Bytes mx4_bytes(const Mx4Plan& plan, int head_dim);
 
 // Where the next launch of a class begins.
 struct Mx4Cursor {
   int req = 0;
   int64_t row = 0;
 };
-// Fills the table of the next launch; false where no request of the class is left.
-bool mx4_next(const efim_batch_t* b, const Mx4Plan& plan, Mx4Cursor* at, Mx4Table* table);
+
+Mx4FewPlan plan_mx4_few(const efim_batch_t* b, int compute_units);
+Mx4ManyPlan plan_mx4_many(const efim_batch_t* b, int compute_units);
+// Fill the table of the next launch; false where no request of the class is left.
+template <int MAXREQ>
+bool mx4_next(const efim_batch_t* b, const Mx4FewPlan& plan, Mx4Cursor* at, Mx4FewTable<MAXREQ>* table);
+bool mx4_next(const efim_batch_t* b, const Mx4ManyPlan& plan, Mx4Cursor* at, Mx4Table* table);
+
+// Workspace of a class: partial outputs [slots][row tile][head_dim] and two floats (reference, sum) for each row of them.
+struct Mx4Bytes {
+  size_t off_ml = 0, total = 0;
+};
+Mx4Bytes mx4_bytes(size_t slots, int row_tile, int head_dim);
 
 }  // namespace efim
