@@ -252,12 +252,12 @@ EXPORTED_SYMBOLS = (
 
 def _ptr(x):
     """Address of a torch tensor / numpy array, or an integer address, or None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(x, np.ndarray):
         return x.ctypes.data
     raise TypeError("cannot take the address of %r" % type(x))

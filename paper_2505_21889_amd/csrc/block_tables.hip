@@ -1,8 +1,7 @@
 // efim_block_tables: the block tables and the slot map of a step from its requests' lengths, which lie on the device.  Pages behind
 // a request's end go back onto the stack of free pages, missing ones are taken from its top.
 //
-// Bound by latency: a scan over the requests (one workgroup), and behind it the entries, which depend on each other only through
-// the stack.
+// Bound by latency: a scan over the requests, and behind it the entries, which depend on each other only through the stack.
 #include <cstdint>
 
 #include "efim_internal.h"
@@ -169,6 +168,91 @@ __global__ __launch_bounds__(kFillThreads) void tables_fill_kernel(const TablesA
   }
 }
 
+// Up to 64 requests, one launch: every wave reads all lengths, a lane each, and sums them by lane exchanges, so that a workgroup
+// (a request's, in slices; the last ones have the slots behind the last token) needs no answer of another.  A page that is taken in
+// the step in which it comes back is looked up in the row that gives it.  The counts are two words: workgroups read the one while
+// another writes the other.
+__global__ __launch_bounds__(kFillThreads) void tables_small_kernel(const TablesArgs a) {
+  __shared__ int64_t s_taken[64], s_returned[64], s_first[65];
+  __shared__ int64_t s_wanted[64];
+  const int lane = threadIdx.x & 63;
+  const int64_t count = *a.free_count;
+  const int r = min(lane, a.batch - 1);
+  const Request q(a, r);
+  const bool mine = lane < a.batch;
+  const bool bad = __any(mine && !q.ok);
+  int64_t taken = mine && q.ok ? q.taken() : 0, returned = mine && q.ok ? q.returned() : 0, tokens = mine && q.ok ? q.new_len : 0;
+  const int64_t own_taken = taken, own_returned = returned, own_tokens = tokens;
+  // (sums of 64 numbers below 2^24 stay within 32 bits: three exchanges a step instead of six)
+  if (!__any((taken | returned | tokens) >> 24)) {
+    uint32_t x = (uint32_t)taken, y = (uint32_t)returned, z = (uint32_t)tokens;
+#pragma unroll
+    for (int by = 1; by < 64; by <<= 1) {
+      const uint32_t u = __shfl_up(x, by), v = __shfl_up(y, by), w = __shfl_up(z, by);
+      if (lane >= by) x += u, y += v, z += w;
+    }
+    taken = x, returned = y, tokens = z;
+  } else {
+#pragma unroll
+    for (int by = 1; by < 64; by <<= 1) {
+      const int64_t u = shuffle_up(taken, by), v = shuffle_up(returned, by), w = shuffle_up(tokens, by);
+      if (lane >= by) taken += u, returned += v, tokens += w;
+    }
+  }
+  auto last = [](int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32);
+  };
+  const int64_t all_taken = last(taken), all_returned = last(returned), all_tokens = last(tokens);
+  const bool counted = !bad && all_tokens <= INT32_MAX;
+  const bool fits = counted && count >= 0 && count + all_returned <= a.capacity && (!a.slots || all_tokens <= a.slot_capacity);
+  const int64_t missing = all_taken - count - all_returned;
+  const bool ok = fits && missing <= 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64) {
+    if (mine) a.row_start[lane] = counted ? (int32_t)(tokens - own_tokens) : 0;
+    if (lane == 0) {
+      a.row_start[a.batch] = counted ? (int32_t)all_tokens : 0;
+      *a.status = !fits ? EFIM_ERR_INVALID_ARG : missing > 0 ? (int32_t)min(missing, (int64_t)INT32_MAX) : 0;
+      *a.free_count_out = (int32_t)(ok ? count + all_returned - all_taken : count);
+    }
+  }
+  const int t = blockIdx.y * kFillThreads + threadIdx.x, threads = gridDim.y * kFillThreads;
+  if ((int)blockIdx.x == a.batch || !ok) {
+    if (a.slots && (int)blockIdx.x == a.batch)
+      for (int64_t at = (ok ? all_tokens : 0) + t; at < a.slot_capacity; at += threads) a.slots[at] = -1;
+    return;
+  }
+  if (threadIdx.x < 64) {
+    s_taken[lane] = taken - own_taken;
+    s_returned[lane] = returned - own_returned;
+    s_first[lane] = tokens - own_tokens;
+    s_wanted[lane] = q.wanted;
+  }
+  __syncthreads();
+  const int me = blockIdx.x;
+  const Request my(a, me);
+  int32_t* row = a.block_table + (int64_t)me * a.max_pages;
+  int32_t* to = a.free_pages + count + s_returned[me];
+  for (int64_t j = t; j < my.returned(); j += threads) to[j] = row[my.wanted + j];
+  // the page at a place of the stack as it is when all have come back
+  auto stacked = [&](int64_t place) {
+    if (place < count) return a.free_pages[place];
+    int from = 0;  // the last request with pages in front of or at the place
+    for (int by = 32; by > 0; by >>= 1)
+      if (from + by < a.batch && s_returned[from + by] <= place - count) from += by;
+    return a.block_table[(int64_t)from * a.max_pages + s_wanted[from] + (place - count - s_returned[from])];
+  };
+  const int64_t top = count + all_returned - 1 - s_taken[me];
+  for (int64_t j = t; j < my.taken(); j += threads) row[my.held + j] = stacked(top - j);
+  if (!a.slots) return;
+  for (int64_t j = t; j < my.new_len; j += threads) {
+    const int64_t pos = my.cached + j, column = pos >> a.page_shift;
+    const int64_t page = column < my.held ? row[column] : stacked(top - (column - my.held));
+    a.slots[s_first[me] + j] = (page << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+  }
+}
+
+__global__ void tables_count_kernel(const int32_t* from, int32_t* to) { *to = *from; }
+
 size_t tables_bytes(int batch) {
   const size_t bytes = (2 * (size_t)batch + 1) * sizeof(int64_t);
   return bytes < 256 ? 256 : bytes;
@@ -217,7 +301,16 @@ int efim_block_tables(int batch, const int32_t* held_len, const int32_t* cached_
   a.status = status;
   a.plan = static_cast<int64_t*>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (a.slot_capacity <= 2048 && batch <= 128) {
+  if (batch > 0 && batch <= 64) {
+    // (one word for both counts: the new one waits in the workspace until all have read the old one)
+    const bool same = free_count == free_count_out;
+    if (same) a.free_count_out = static_cast<int32_t*>(workspace);
+    // two of the mean request's tokens to a thread at most (a thread's slots wait for their pages one behind the other: 80k tokens
+    // of 64 requests with eight to a thread 10 us)
+    const int64_t slices = (a.slot_capacity / batch * 2 + kFillThreads - 1) / kFillThreads;
+    tables_small_kernel<<<dim3((unsigned)batch + 1, (unsigned)(slices < 1 ? 1 : slices > 16 ? 16 : slices)), kFillThreads, 0, s>>>(a);
+    if (same) tables_count_kernel<<<1, 1, 0, s>>>(static_cast<const int32_t*>(workspace), free_count_out);
+  } else if (a.slot_capacity <= 2048 && batch <= 128) {
     tables_scan_kernel<true><<<1, kScanThreads, 0, s>>>(a);
   } else {
     tables_scan_kernel<false><<<1, kScanThreads, 0, s>>>(a);
