@@ -106,6 +106,57 @@ __device__ __forceinline__ Place find_tile(const Mx4Table& t, const Requests& re
   return at;
 }
 
+// Sum of a lane's numbers over the wave, in all lanes: exchanges inside rows of sixteen lanes, then of rows and halves.
+__device__ __forceinline__ int lanes_sum(int v) {
+  auto with = [&](auto ctrl) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, 0xf, 0xf, true); };
+  v += with(std::integral_constant<int, 0xB1>{});   // quad_perm [1, 0, 3, 2]
+  v += with(std::integral_constant<int, 0x4E>{});   // quad_perm [2, 3, 0, 1]
+  v += with(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  v += with(std::integral_constant<int, 0x140>{});  // row_mirror
+  return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) + __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
+}
+
+// The tile that is the n-th in the order of their units, the largest first, by the whole wave: what starts last is then
+// short.  Of equally long tiles the heads are next to each other, so that an XCD meets few of them.
+template <int TILE, int UNIT>
+__device__ __forceinline__ Place nth_tile(const Mx4Table& t, int n, int lane) {
+  const int g = t.group_heads;
+  Mx4Req q[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) q[i] = t.req[min(i * 64 + lane, t.nreq - 1)];
+  auto longer = [&](int c, int i) { return i * 64 + lane < t.nreq ? mx4_tiles_from(q[i], g, TILE, UNIT, c) : 0; };
+  auto of_all = [&](int c) { return t.kv_heads * lanes_sum(longer(c, 0) + longer(c, 1)); };
+  int low = 1, high = t.most_units + 1;  // the units of the tile: more tiles than n have `low` or more, at most n `high` or more
+  while (high - low > 1) {
+    const int middle = low + (high - low) / 2;
+    (of_all(middle) > n ? low : high) = middle;
+  }
+  int in = n - of_all(high);
+  Place at;
+  at.units = low;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int mine = t.kv_heads * (longer(low, i) - longer(high, i));
+    int upto = mine;
+#pragma unroll
+    for (int by = 1; by < 64; by <<= 1) {
+      const int other = __shfl_up(upto, by);
+      if (lane >= by) upto += other;
+    }
+    const int k = __popcll(__ballot(upto <= in));
+    if (k < 64) {
+      in -= __builtin_amdgcn_readlane(upto - mine, k);
+      at.r = i * 64 + k;
+      at.head = in % t.kv_heads;
+      at.tile = mx4_tiles(t.req[at.r], g, TILE) - __builtin_amdgcn_readlane(longer(low, i), k) + in / t.kv_heads;
+      break;
+    }
+    in -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  at.first = 0;
+  return at;
+}
+
 // A workgroup's share of the units, a tile's part at a time.
 template <int TILE, int UNIT>
 struct Share {
@@ -120,6 +171,15 @@ struct Share {
   int64_t slot;    // partial result, -1: the workgroup has the whole tile
 
   __device__ __forceinline__ Share(const Mx4Table& table, int lane) : t(table) {
+    if (t.by_tile) {
+      group = 0;
+      at = nth_tile<TILE, UNIT>(t, blockIdx.x, lane);
+      begin = at.first;
+      end = begin + at.units;
+      rq = t.req[at.r];
+      part();
+      return;
+    }
     // an XCD takes neighbouring shares, which have rows of the cache in common
     group = (int)(blockIdx.x % kXcdCount) * (int)(gridDim.x / kXcdCount) + (int)(blockIdx.x / kXcdCount);
     begin = end = 0;
@@ -195,14 +255,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
 }
 
-// Chunk swizzles (exclusive or) of a tile's bf16 rows in LDS.  Keys: the operand reads of neighbouring rows take all banks.
-// Values: so do the four rows that a transposing read takes at a time, and for products of 16 rows two such groups.
+// Chunk swizzles (exclusive or) of a tile's bf16 rows in LDS, of which the bank line holds one (D 128) or two.  Keys and values that a
+// workgroup shares: eight lanes write two pieces of 32 elements of each of four rows, word by word, and a wave reads sixteen neighbouring rows' equal
+// chunks (keys) and four neighbouring chunks of each of four rows (values); all of them take all banks.
 template <int D>
-__device__ __forceinline__ int key_swizzle(int row) { return row & (D / 8 - 1); }
+__device__ __forceinline__ int key_swizzle(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
 template <int D>
-__device__ __forceinline__ int value_swizzle(int row) { return (row & (D / 32 - 1)) << 2; }
+__device__ __forceinline__ int value_swizzle(int row) { return D == 128 ? (row & 3) * 5 : (row >> 1 & 3) ^ (row >> 1 & 1) << 2; }
+// Values of a wave's own: the four rows that a transposing read for products of 16 rows takes at a time, and two such groups.
 template <int D>
-__device__ __forceinline__ int value_swizzle16(int row) { return value_swizzle<D>(row) ^ (D == 128 ? ((row >> 2) & 1) << 1 : 0); }
+__device__ __forceinline__ int value_swizzle16(int row) { return D == 128 ? (row & 3) << 2 ^ (row >> 2 & 1) << 1 : (row & 1) << 2; }
 
 // One wave writes and reads its own LDS: the accesses are in order, the compiler is told by the fences.
 __device__ __forceinline__ void own_writes() {
@@ -632,20 +694,35 @@ __global__ __launch_bounds__(kThreads) void mx4_few_join_kernel(const Mx4FewArgs
 }
 
 // --- many rows --------------------------------------------------------------------------------------------------------------
-// 128 query rows, 32 of them a wave's.  A tile of 64 keys and values is converted once for all of them on its way from memory
-// to LDS (a thread has 16 bytes of a row's codes), one tile ahead.
-template <int D>
+// Four waves of 32 query rows.  The codes of 64 keys and values are converted once for all of them on their way to LDS (a thread
+// takes 16 bytes of a row's codes from memory, two rounds ahead).
+//
+// A wave works off its keys in halves of 32, three at a time: while the scores of half n are turned into probabilities, the
+// products form the scores of n + 1 and add the values of n - 1, and the thread converts its share of what the next round of two
+// halves reads.  The waves meet once a round.  A unit holds two workgroups, so that each computes through the other's meetings,
+// first loads and last stores.
+//
+// SMALL: pages of fewer rows than a wave converts.
+template <int D, bool SMALL>
 __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args args, const uint16_t* __restrict__ q,
                                                                const uint8_t* __restrict__ k_cache, const uint8_t* __restrict__ v_cache,
                                                                const int32_t* __restrict__ block_table) {
-  constexpr int kSteps = D / 16;
-  constexpr int kBlocks = D / 32;
-  constexpr int kRowBytes = 2 * D;
-  constexpr int kMatrixBytes = kMx4ManyKeys * kRowBytes;
-  constexpr int kStageBytes = 2 * kMatrixBytes;  // keys, values
-  constexpr int kLanes = D / 32;                 // threads of a row
-  constexpr int kLoads = 2 * kMx4ManyKeys * kLanes / kThreads;  // of a thread: keys and values (D 128), either (D 64)
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStageBytes];
+  constexpr int kTile = 32 * kWaves;
+  static_assert(kTile == kMx4ManyRows, "the plan's");
+  constexpr int kSteps = D / 16, kBlocks = D / 32;
+  constexpr int kProducts = kSteps + 2 * kBlocks, kAhead = 4;
+  constexpr int kExps = 16 / kProducts;            // probabilities beside a product
+  constexpr int kRowBytes = 2 * D;                 // of a bf16 row in LDS
+  constexpr int kHalfBytes = 32 * kRowBytes, kStageBytes = 2 * kHalfBytes, kRingBytes = 2 * kStageBytes;
+  constexpr int kPieces = D / 32;                    // of 16 bytes, of a row's codes
+  constexpr int kWaveRows = 64 / kPieces;            // that a wave converts
+  constexpr int kIds = SMALL ? kWaveRows / 8 : 1;    // of pages, of those
+  constexpr int kChunks = 128 * kPieces / kThreads;  // of a thread: both matrices' or one
+  constexpr int kWords = 4;                          // of a chunk
+  constexpr int kHalfWords = kChunks * kWords / 2;   // of a thread beside a half
+  constexpr int kTurn = kProducts / (kHalfWords * 4);  // products for each conversion of two codes
+  static_assert(kTurn * kHalfWords * 4 == kProducts && kExps * kProducts == 16, "a half's work is dealt to its products");
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kRingBytes];
   __shared__ uint32_t s_torn[kWaves];  // whether the wave met a value block that is no number
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -655,25 +732,31 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
   const int g = t.group_heads, hq = g * t.kv_heads;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
 
-  // operands in a stage
-  const int blk = lane >> 4, w16 = lane & 15;
-  const int v_key = (blk >> 1) * 4 + (w16 >> 2);
-  const int v_chunk = 2 * (blk & 1) + ((w16 & 3) >> 1);
+  // Operands: the first chunk of the lane's key row, and where a lane of the transposing read begins in the first block.  (The
+  // further ones' places differ in bits that the row's place leaves free.)
+  const uint32_t key_at = lds0 + i32 * kRowBytes + ((hi ^ key_swizzle<D>(i32)) << 4);
+  const int v_key = (lane >> 5) * 4 + ((lane & 15) >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const uint32_t value_at = lds0 + kRingBytes + v_key * kRowBytes + (lane & 1) * 8 + ((v_chunk ^ value_swizzle<D>(v_key)) << 4);
   // what this thread converts
-  const int in_tile = tid / kLanes % kMx4ManyKeys, piece = tid % kLanes;
-  const int first_matrix = kLoads == 2 ? 0 : __builtin_amdgcn_readfirstlane(tid / (kLanes * kMx4ManyKeys));
+  const int first_matrix = kChunks == 2 ? 0 : wave / (kWaves / 2);
+  const int piece = D == 128 ? (lane >> 3 & 1) * 2 + (lane & 1) : lane & 1;
+  const int wave_row = D == 128 ? (lane >> 4) * 4 + (lane >> 1 & 3) : (lane >> 4) * 8 + (lane >> 1 & 3) * 2 + (lane >> 3 & 1);
+  const int first_row = wave * kWaveRows % 64, in_round = first_row + wave_row;
+  const int put_key = ((piece * kWords) ^ key_swizzle<D>(in_round & 31)) << 4, put_value = ((piece * kWords) ^ value_swizzle<D>(in_round & 31)) << 4;
+  const uint32_t put_at = lds0 + in_round * kRowBytes + (first_matrix == 0 ? put_key : kRingBytes + put_value);
+  const uint32_t put_apart = put_key ^ put_value;
 
-  for (Share<kMx4ManyRows, kMx4ManyKeys> it(t, lane); !it.done(); it.advance()) {
+  for (Share<kTile, kMx4ManyKeys> it(t, lane); !it.done(); it.advance()) {
     const Cache<D> cache(k_cache, block_table, t, it.rq.req, it.at.head);
-    const int ntiles = (it.k1 - it.k0 + kMx4ManyKeys - 1) / kMx4ManyKeys;
     const int local = wave * 32 + i32;
     const bool row_ok = local < it.rows;
     const int row = it.row0 + local, tok = row / g;
-    const int visible = row_ok ? it.rq.cached + tok + 1 : 0;
+    const int visible = min(row_ok ? it.rq.cached + tok + 1 : 0, it.k1);
     const int64_t q_off = ((int64_t)(it.rq.row_start + tok) * hq + it.at.head * g + (row - tok * g)) * D;
-    const bool active = wave * 32 < it.rows;  // (wave-uniform)
-    const int least = it.rq.cached + (it.row0 + wave * 32) / g + 1;
-    const int most = it.rq.cached + (it.row0 + min(it.rows, wave * 32 + 32) - 1) / g + 1;
+    // halves of the part; whether the wave has rows, and the keys that all of them see
+    const int rounds = (it.k1 - it.k0 + 31) / 32;
+    const bool rows_here = wave * 32 < it.rows;
+    const int least = min(it.rq.cached + (it.row0 + wave * 32) / g + 1, it.k1);
     bf16x8 qb[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -685,122 +768,264 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+      for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float m_run = kNoReference, l_run = 0.f;
+    f32x16 s0, s1;                                      // scores of an even and an odd half
+    u32x4 p0[2], p1[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // and their probabilities, as operands
     uint32_t torn = 0;
 
-    u32x4 codes[kLoads];
-    uint32_t scales[kLoads];
-    auto key_of = [&](int tile) { return min(it.k0 + tile * kMx4ManyKeys + in_tile, it.k1 - 1); };
-    auto look_up = [&](int tile) { return cache.pages[key_of(tile) >> t.page_shift]; };
-    auto load = [&](int tile, int32_t page) __attribute__((always_inline)) {
-      const int key = key_of(tile);
-      const int64_t at = cache.page_at(page);
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const uint8_t* from = (first_matrix + j == 0 ? k_cache : v_cache) + at;
-        codes[j] = *reinterpret_cast<const u32x4*>(from + cache.code_at(key) + piece * 16);
-        scales[j] = from[cache.scale_at(key) + piece];
-      }
+    // Round u of two halves, 2u and 2u + 1, reads the keys of halves 2u + 1 and 2u + 2 and the values of 2u - 1 and 2u, and converts
+    // those of round u + 1.  (In place of groups of rows that are not the part's its first or last group; what of their rows no query
+    // sees is masked, and the values of half -1 have no weight.)
+    struct Chunk {
+      u32x4 codes[kChunks];
+      uint32_t scales[kChunks];
+      int key[kChunks];  // first of the wave's rows
     };
-    auto convert = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const bool is_v = first_matrix + j == 1;
-        const bool bad = is_v && scales[j] >= kTorn;
-        torn |= bad;
-        const float scale = bad ? 1.f : mx4_scale_value(scales[j]);
-        const uint32_t to = lds0 + (tile & 1) * kStageBytes + is_v * kMatrixBytes + in_tile * kRowBytes;
-        const int swizzle = is_v ? value_swizzle<D>(in_tile) : key_swizzle<D>(in_tile);
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          *(LDS_PTR(mx4_words))(uintptr_t)(to + ((piece * 4 + w) ^ swizzle) * 16) = mx4_decode8(bad ? 0u : codes[j][w], scale);
-      }
+    auto group_of = [&](int u, int j) {
+      return max(min(it.k0 + u * 64 + (first_matrix + j == 0 ? 32 : -32) + first_row, (it.k1 - 1) & -kWaveRows), it.k0);
     };
-    load(0, look_up(0));
-    int32_t page = look_up(1);
-    for (int tile = 0; tile < ntiles; ++tile) {
-      convert(tile);
-      if (tile + 1 < ntiles) load(tile + 1, page);
-      page = look_up(tile + 2);
-      __syncthreads();
-      const int key0 = it.k0 + tile * kMx4ManyKeys;
-      if (!active || key0 >= most) continue;
-      const uint32_t k_at = lds0 + (tile & 1) * kStageBytes, v_at = k_at + kMatrixBytes;
-      f32x16 sc[2];
+    struct PageIds {
+      int32_t id[kChunks][kIds];
+    };
+    auto look_up = [&](int u) __attribute__((always_inline)) {
+      PageIds p;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sc[kb][r] = 0.f;
+        for (int i = 0; i < kIds; ++i) p.id[j][i] = cache.page_id(min(group_of(u, j) + 8 * i, it.k1 - 1));
+      return p;
+    };
+    auto load = [&](int u, const PageIds& p, Chunk& c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const bf16x8 ka = *(const LDS_PTR(bf16x8))(uintptr_t)(k_at + (kb * 32 + i32) * kRowBytes + (((2 * s + hi) ^ key_swizzle<D>(i32)) << 4));
-          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[s], sc[kb], 0, 0, 0);
+      for (int j = 0; j < kChunks; ++j) {
+        const uint8_t* matrix = first_matrix + j == 0 ? k_cache : v_cache;
+        c.key[j] = group_of(u, j);
+        if constexpr (SMALL) {
+          int64_t at = cache.page_at(p.id[j][0]);
+#pragma unroll
+          for (int i = 1; i < kIds; ++i) {
+            const int64_t other = cache.page_at(p.id[j][i]);
+            at = wave_row >= 8 * i ? other : at;
+          }
+          const int key = c.key[j] + wave_row;
+          c.codes[j] = *reinterpret_cast<const u32x4*>(matrix + at + cache.code_at(key) + piece * 16);
+          c.scales[j] = matrix[at + cache.scale_at(key) + piece];
+        } else {
+          const uint8_t* page = matrix + cache.page_at(p.id[j][0]);
+          c.codes[j] = *reinterpret_cast<const u32x4*>(page + cache.code_at(c.key[j]) + (uint32_t)(wave_row * kPieces + piece) * 16);
+          c.scales[j] = (page + cache.scale_at(c.key[j]))[(uint32_t)(wave_row * kPieces + piece)];
         }
       }
-      if (key0 + kMx4ManyKeys > min(least, it.k1)) {
-        const int lim = min(visible, it.k1) - key0 - hi * 4;
+    };
+    // Where a round's chunks go, and their scales.  (A value block that is no number: any that are.)
+    struct Target {
+      uint32_t at;
+      float scale[kChunks];
+    };
+    auto target = [&](uint32_t stage, const Chunk& c) __attribute__((always_inline)) {
+      Target to;
+      to.at = put_at + stage;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (kb * 32 + (r >> 2) * 8 + (r & 3) >= lim) sc[kb][r] = -INFINITY;
+      for (int j = 0; j < kChunks; ++j) {
+        const bool bad = first_matrix + j == 1 && c.scales[j] >= kTorn;
+        torn |= bad && wave_row < it.k1 - c.key[j];
+        to.scale[j] = mx4_scale_value(bad ? 127u : c.scales[j]);
       }
-      float top = fmaxf(sc[0][0], sc[1][0]);
+      return to;
+    };
+    constexpr auto kFirst = std::integral_constant<int, 0>{};
+    constexpr auto kSecond = std::integral_constant<int, 1>{};
+    uint32_t here = 0, ahead = kStageBytes;  // the stages of the round and the next one
+    uint32_t made[4];
+    // the n-th conversion of a round
+    auto convert = [&](auto n_c, const Chunk& c, const Target& to) __attribute__((always_inline)) {
+      constexpr int n = decltype(n_c)::value, word = n / 4, j = word / kWords, w = word % kWords;
+      made[n % 4] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c.codes[j][w], to.scale[j], n % 4));
+      if constexpr (n % 4 == 3)
+        *(LDS_PTR(u32x4))(uintptr_t)(((to.at + j * kRingBytes) ^ (j == 0 ? 0u : put_apart)) ^ (uint32_t)(w << 4)) = u32x4{made[0], made[1], made[2], made[3]};
+    };
+    auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+    auto probability = [&](const f32x16& sc, int e) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(sc[e] * args.scale_log2 - m_run); };
+    auto score_product = [&](u32x4 a, int n, f32x16& sn) __attribute__((always_inline)) {
+      f32x16 from = sn;
+      if (n == 0) {
 #pragma unroll
-      for (int r = 1; r < 16; ++r) top = max3(top, sc[0][r], sc[1][r]);
-      top = cross_half_max(top) * args.scale_log2;
-      const bool grow = top > m_run + kSlack;
-      if (__any(grow)) {
-        const float m_next = grow ? top : m_run;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - (m_next == -INFINITY ? 0.f : m_next));
-        l_run *= alpha;
+        for (int e = 0; e < 16; ++e) from[e] = 0.f;
+      }
+      sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qb[n], from, 0, 0, 0);
+    };
+    auto key_operand = [&](uint32_t stage, int second, int n) __attribute__((always_inline)) -> u32x4 {
+      return *(const LDS_PTR(u32x4))(uintptr_t)(((key_at + stage) ^ (uint32_t)(n << 5)) + second * kHalfBytes);
+    };
+    u32x4 staged[kAhead];  // operands of the next products
+    // Products of a half, the first or second of its round: the scores of the stage's keys into `sn`, the stage's values under the
+    // probabilities `pv`; beside them the probabilities of the scores `sc` into `pn`, whose sum is returned, and conversions.
+    auto round = [&](uint32_t stage, auto second, f32x16& sn, const u32x4 (&pv)[2], const f32x16& sc, u32x4 (&pn)[2],
+                     const Chunk& c, const Target& to) __attribute__((always_inline)) -> float {
+      auto operand = [&](int n) __attribute__((always_inline)) -> u32x4 {
+        if (n < kSteps) return key_operand(stage, decltype(second)::value, n);
+        if (n >= kProducts) return key_operand(stage, 1, n - kProducts);  // (of the second half)
+        const int k = (n - kSteps) / kBlocks, d = (n - kSteps) % kBlocks;
+        const uint32_t at = ((value_at + stage) ^ (uint32_t)(d << 6)) + decltype(second)::value * kHalfBytes;
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + 2 * k * 8 * kRowBytes));
+        const bf16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + (2 * k + 1) * 8 * kRowBytes));
+        return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      __builtin_amdgcn_s_setprio(1);
+      __builtin_amdgcn_sched_barrier(0);
+      float sum = 0.f, pair[2];
+      auto step = [&](auto n_c) __attribute__((always_inline)) {
+        constexpr int n = decltype(n_c)::value;
+        if constexpr (n < kSteps) {
+          score_product(staged[n % kAhead], n, sn);
+        } else {
+          constexpr int j = n - kSteps;
+          o[j % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, staged[n % kAhead]),
+                                                                   __builtin_bit_cast(bf16x8, pv[j / kBlocks]), o[j % kBlocks], 0, 0, 0);
+        }
+        if constexpr (n + kAhead < kProducts || !decltype(second)::value) staged[n % kAhead] = operand(n + kAhead);
+#pragma unroll
+        for (int i = 0; i < kExps; ++i) {
+          const int e = n * kExps + i;
+          pair[e & 1] = probability(sc, e);
+          if (e & 1) {
+            const uint32_t two = pack_bf16(pair[0], pair[1]);
+            pn[e >> 3][(e & 7) >> 1] = two;
+            sum = add_pair(two, sum);
+            asm volatile("" : "+v"(sum));  // (keeps the step in its place)
+          }
+        }
+        if constexpr (n % kTurn == kTurn - 1) convert(std::integral_constant<int, decltype(second)::value * kHalfWords * 4 + n / kTurn>{}, c, to);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      [&]<int... N>(std::integer_sequence<int, N...>) __attribute__((always_inline)) { (step(std::integral_constant<int, N>{}), ...); }
+      (std::make_integer_sequence<int, kProducts>{});
+      __builtin_amdgcn_s_setprio(0);
+      return sum;
+    };
+    auto convert_half = [&](auto second, const Chunk& c, const Target& to) __attribute__((always_inline)) {
+      [&]<int... N>(std::integer_sequence<int, N...>) __attribute__((always_inline)) {
+        (convert(std::integral_constant<int, decltype(second)::value * kHalfWords * 4 + N>{}, c, to), ...);
+      }
+      (std::make_integer_sequence<int, kHalfWords * 4>{});
+    };
+    auto row_max = [&](const f32x16& sc) __attribute__((always_inline)) {
+      float mx = sc[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e]);
+      return cross_half_max(mx) * args.scale_log2;
+    };
+    // Where the sum says that a probability may have passed the slack: a reference moves to its row's maximum if that did, and
+    // the probabilities are formed again.
+    auto settle = [&](const f32x16& sc, u32x4 (&pn)[2], float sum) __attribute__((always_inline)) {
+      if (__any(sum >= kOver)) {
+        const float mx = row_max(sc);
+        const float m_new = mx > m_run + kSlack ? mx : m_run;
+        const float f = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= f;
 #pragma unroll
         for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
-        m_run = m_next;
-      }
-      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+          for (int e = 0; e < 16; ++e) o[d][e] *= f;
+        m_run = m_new;
+        sum = 0.f;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        u32x4 p[2];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const float a = __builtin_amdgcn_exp2f(sc[kb][2 * r] * args.scale_log2 - m_use);
-          const float b = __builtin_amdgcn_exp2f(sc[kb][2 * r + 1] * args.scale_log2 - m_use);
-          p[r >> 2][r & 3] = pack_bf16(a, b);
-          l_run = add_pair(p[r >> 2][r & 3], l_run);
+        for (int e = 0; e < 16; e += 2) {
+          const uint32_t two = pack_bf16(probability(sc, e), probability(sc, e + 1));
+          pn[e >> 3][(e & 7) >> 1] = two;
+          sum = add_pair(two, sum);
         }
+      }
+      l_run += sum;
+    };
+    // The n-th half: one that every row sees whole,
+    auto seen_half = [&](int n, auto second, f32x16& sc, f32x16& sn, u32x4 (&pn)[2], u32x4 (&po)[2], const Chunk& c, const Target& to) __attribute__((always_inline)) {
+      if (n == 0) m_run = fmaxf(row_max(sc), kNoReference);
+      settle(sc, pn, round(here, second, sn, po, sc, pn, c, to));
+    };
+    // one that not all rows see, or none (behind the last one there is a round for its values alone),
+    auto half = [&](int n, auto second, f32x16& sc, f32x16& sn, u32x4 (&pn)[2], u32x4 (&po)[2], const Chunk& c, const Target& to) __attribute__((always_inline)) {
+      if (it.k0 + n * 32 + 32 > least) {
+        const int end = visible - it.k0 - n * 32 - hi * 4;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int e = 0; e < 16; ++e)
+          if ((e >> 2) * 8 + (e & 3) >= end) sc[e] = -INFINITY;
+      }
+      seen_half(n, second, sc, sn, pn, po, c, to);
+    };
+    // and one of a wave without rows.
+    auto no_half = [&](int, auto second, f32x16&, f32x16&, u32x4 (&)[2], u32x4 (&)[2], const Chunk& c, const Target& to) __attribute__((always_inline)) {
+      convert_half(second, c, to);
+    };
+
+    Chunk at_hand, next;
+    {
+      Chunk early[2];
+      const PageIds ids[3] = {look_up(-1), look_up(0), look_up(1)};
+      load(-1, ids[0], early[0]);
+      load(0, ids[1], early[1]);
+      load(1, ids[2], at_hand);
 #pragma unroll
-          for (int d = 0; d < kBlocks; ++d) {
-            const uint32_t at = v_at + ((kb * 2 + h) * 16 + v_key) * kRowBytes + (w16 & 1) * 8 + (((d * 4 + v_chunk) ^ value_swizzle<D>(v_key)) << 4);
-            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)at);
-            const bf16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + 8 * kRowBytes));
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7),
-                                                           __builtin_bit_cast(bf16x8, p[h]), o[d], 0, 0, 0);
-          }
+      for (int u = -1; u < 1; ++u) {
+        const Target to = target(u < 0 ? ahead : here, early[u + 1]);
+        convert_half(kFirst, early[u + 1], to);
+        if (u == 0 || kChunks == 1) convert_half(kSecond, early[u + 1], to);  // (of the round in front of the first one the keys are wanted)
       }
     }
+    PageIds pages = look_up(2);
+    meet();
+    if (rows_here) {
+#pragma unroll
+      for (int n = 0; n < kSteps; ++n) score_product(key_operand(ahead, 1, n), n, s0);
+    }
+    auto two_halves = [&](int n, auto&& one) __attribute__((always_inline)) {
+      meet();
+      load(n / 2 + 2, pages, next);
+      pages = look_up(n / 2 + 3);
+      const Target to = target(ahead, at_hand);
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) staged[n] = key_operand(here, 0, n);
+      one(n, kFirst, s0, s1, p0, p1, at_hand, to);
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) asm volatile("" : "+v"(staged[n]));
+      one(n + 1, kSecond, s1, s0, p1, p0, at_hand, to);
+      at_hand = next;
+      const uint32_t done = here;
+      here = ahead;
+      ahead = done;
+    };
+    // First the halves that all rows of the workgroup see, without masks.
+    const int clear = max(0, (min(it.rq.cached + it.row0 / g + 1, it.k1) - it.k0) / 32) & ~1;
+    int n = 0;
+    if (rows_here) {
+      for (; n < clear; n += 2) two_halves(n, seen_half);
+      for (; n <= rounds; n += 2) two_halves(n, half);
+    } else {
+      for (; n <= rounds; n += 2) two_halves(n, no_half);
+    }
+
     const bool met = __any(torn != 0);
     if (lane == 0) s_torn[wave] = met;
-    __syncthreads();  // every wave is done with the stages, and the words are set
+    __syncthreads();  // every wave is done with the rings, and the words are set
     if (row_ok) {
       const float l = cross_half_sum(l_run);
-      if (s_torn[0] | s_torn[1] | s_torn[2] | s_torn[3]) {
+      uint32_t any_torn = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) any_torn |= s_torn[w];
+      if (any_torn) {
         const Cache<D> values(v_cache, block_table, t, it.rq.req, it.at.head);
         uint32_t lost = 0;
-        for (int key = it.k0; key < min(it.k1, visible); ++key) lost |= values.torn_blocks(key);
+        for (int key = it.k0; key < visible; ++key) lost |= values.torn_blocks(key);
 #pragma unroll
         for (int d = 0; d < kBlocks; ++d)
           if (lost >> d & 1)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[d][r] = NAN;
+            for (int e = 0; e < 16; ++e) o[d][e] = NAN;
       }
       const float inv = 1.f / l;
-      const int64_t part = it.slot * kMx4ManyRows + local;
+      const int64_t part = it.slot * kTile + local;
 #pragma unroll
       for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
@@ -820,9 +1045,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
 
 // --- join -------------------------------------------------------------------------------------------------------------------
 // The parts of split tiles: with M = max m_s,  out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, in the order of the keys.  Workgroup
-// i has the tile in which the shares of workgroups i and i + 1 are the first to meet.
+// i has the tile in which the shares of workgroups i and i + 1 are the first to meet.  Bound by latency: four parts at a time.
 template <int D, int TILE, int UNIT>
 __global__ __launch_bounds__(kThreads) void mx4_join_kernel(const Mx4Args args) {
+  constexpr int kAtOnce = 4;
   const Mx4Table& t = args.table;
   const int lane = threadIdx.x & 63;
   const int second = blockIdx.x + 1;  // workgroup that goes on where another's share ends
@@ -834,21 +1060,36 @@ __global__ __launch_bounds__(kThreads) void mx4_join_kernel(const Mx4Args args) 
   const int g = t.group_heads, hq = g * t.kv_heads;
   const int rows = mx4_rows_of(rq, g, TILE, at.tile);
   const int64_t end = at.first + at.units;
+  int last = second;
+  while (last + 1 < t.groups && t.first_unit(last + 1) < end) ++last;
   constexpr int kVec = D / 4;
   const int c = threadIdx.x % kVec * 4;
   for (int r = blockIdx.y * (kThreads / kVec) + threadIdx.x / kVec; r < rows; r += gridDim.y * (kThreads / kVec)) {
-    float m = -INFINITY, l = 0.f;
+    float m = kNoReference, l = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int group = second - 1; group == second - 1 || t.first_unit(group) < end; ++group) {
-      const int64_t part = mx4_slot(group, group >= second) * TILE + r;
-      const f32x2 ml = *reinterpret_cast<const f32x2*>(args.part_ml + part * 2);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(args.part_o + part * D + c);
-      const float m_next = fmaxf(m, ml[0]);
-      const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_next);
-      const float add = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m_next);
-      l = l * old + ml[1] * add;
-      v = v * old + x * add;
-      m = m_next;
+    for (int group = second - 1; group <= last; group += kAtOnce) {
+      f32x2 ml[kAtOnce];
+      f32x4 x[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t part = mx4_slot(min(group + i, last), group + i >= second) * TILE + r;
+        ml[i] = *reinterpret_cast<const f32x2*>(args.part_ml + part * 2);
+        x[i] = *reinterpret_cast<const f32x4*>(args.part_o + part * D + c);
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i][0]);
+      const float back = __builtin_amdgcn_exp2f(m - top);
+      l *= back;
+      v *= back;
+      m = top;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        if (group + i > last) break;
+        const float f = __builtin_amdgcn_exp2f(ml[i][0] - top);
+        l += f * ml[i][1];
+        v += f * x[i];
+      }
     }
     const float inv = 1.f / l;
     const int row = at.tile * TILE + r, tok = row / g;
@@ -894,16 +1135,18 @@ int launch_many(const efim_batch_t* b, const Mx4ManyPlan& plan, const Mx4Tensors
   Mx4Args args;
   args.scale_log2 = x.scale_log2;
   args.part_o = reinterpret_cast<float*>(workspace);
-  args.part_ml = reinterpret_cast<float*>(workspace + mx4_bytes(2 * (size_t)plan.max_groups, kMx4ManyRows, D).off_ml);
+  args.part_ml = reinterpret_cast<float*>(workspace + mx4_bytes(plan.slots, kMx4ManyRows, D).off_ml);
   args.out = x.out;
   constexpr int kAtOnce = kThreads / (D / 4);
   Mx4Cursor at;
   while (mx4_next(b, plan, &at, &args.table)) {
     const int groups = args.table.groups;
-    mx4_many_kernel<D><<<(groups + kXcdCount - 1) / kXcdCount * kXcdCount, kThreads, 0, stream>>>(args, x.q, x.k_cache, x.v_cache, x.block_table);
-    if (groups > 1)
+    const int launched = args.table.by_tile ? groups : (groups + kXcdCount - 1) / kXcdCount * kXcdCount;
+    auto* kernel = b->page_size < 2048 / D ? mx4_many_kernel<D, true> : mx4_many_kernel<D, false>;
+    kernel<<<launched, kThreads, 0, stream>>>(args, x.q, x.k_cache, x.v_cache, x.block_table);
+    if (!args.table.by_tile && groups > 1)
       mx4_join_kernel<D, kMx4ManyRows, kMx4ManyKeys>
-          <<<dim3((unsigned)groups - 1, (kMx4ManyRows + 4 * kAtOnce - 1) / (4 * kAtOnce)), kThreads, 0, stream>>>(args);
+          <<<dim3((unsigned)groups - 1, (kMx4ManyRows + 2 * kAtOnce - 1) / (2 * kAtOnce)), kThreads, 0, stream>>>(args);
     const int rc = last_error();
     if (rc != EFIM_OK) return rc;
   }
@@ -917,7 +1160,7 @@ struct Mx4Work {
   size_t many_at = 0, total = 0;
   explicit Mx4Work(const efim_batch_t* b) : few(plan_mx4_few(b, compute_units())), many(plan_mx4_many(b, compute_units())) {
     if (few.any) many_at = mx4_bytes(few.slots, few.row_tile, b->head_dim).total;
-    total = many_at + (many.any ? mx4_bytes(2 * (size_t)many.max_groups, kMx4ManyRows, b->head_dim).total : 0);
+    total = many_at + (many.any ? mx4_bytes(many.slots, kMx4ManyRows, b->head_dim).total : 0);
     if (total < 256) total = 256;
   }
 };

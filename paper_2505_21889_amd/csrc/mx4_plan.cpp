@@ -69,7 +69,12 @@ Mx4FewPlan plan_mx4_few(const efim_batch_t* b, int compute_units) {
 Mx4ManyPlan plan_mx4_many(const efim_batch_t* b, int compute_units) {
   Mx4ManyPlan plan;
   for (int r = 0; r < b->batch; ++r) plan.any = plan.any || is_many(b, r);
-  plan.max_groups = 2 * compute_units;
+  if (!plan.any) return plan;
+  plan.places = 2 * compute_units;
+  Mx4Cursor at;
+  Mx4Table t;
+  while (mx4_next(b, plan, &at, &t))
+    if (!t.by_tile && 2 * (size_t)t.groups > plan.slots) plan.slots = 2 * (size_t)t.groups;
   return plan;
 }
 
@@ -117,25 +122,40 @@ template bool mx4_next<64>(const efim_batch_t*, const Mx4FewPlan&, Mx4Cursor*, M
 template bool mx4_next<kMx4FewReqs>(const efim_batch_t*, const Mx4FewPlan&, Mx4Cursor*, Mx4FewTable<kMx4FewReqs>*);
 
 bool mx4_next(const efim_batch_t* b, const Mx4ManyPlan& plan, Mx4Cursor* at, Mx4Table* t) {
-  t->nreq = 0;
+  t->nreq = t->most_units = 0;
   t->kv_heads = b->num_kv_heads;
   t->group_heads = group_of(b);
   t->max_pages = b->max_pages_per_req;
   t->page_shift = page_shift_of(b);
-  int64_t units = 0;
+  int64_t units = 0, tiles = 0;
+  int least = INT32_MAX;
   for (; at->req < b->batch && t->nreq < kMx4TableReqs; ++at->req) {
     const int n = b->new_len[at->req];
     if (is_many(b, at->req)) {
       Mx4Req& q = t->req[t->nreq++];
       q = Mx4Req{units, 0, at->req, b->cached_len[at->req], n, (int32_t)at->row};
-      for (int tile = mx4_tiles(q, t->group_heads, kMx4ManyRows) - 1; tile >= 0; --tile)
-        q.units_per_head += mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, tile);
+      const int mine = mx4_tiles(q, t->group_heads, kMx4ManyRows);
+      for (int tile = 0; tile < mine; ++tile) q.units_per_head += mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, tile);
+      const int last = mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, mine - 1);
+      const int first = mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, 0);
+      t->most_units = last > t->most_units ? last : t->most_units;
+      least = first < least ? first : least;
       units += q.units_per_head * t->kv_heads;
+      tiles += (int64_t)mine * t->kv_heads;
     }
     at->row += n;
   }
   if (t->nreq == 0) return false;
-  t->groups = (int32_t)(units < plan.max_groups ? units : plan.max_groups);
+  // What either way takes, in units (us even / whole tiles: 32 requests of 2048..8192 keys and 8..64 tokens, 28/4 heads 121 / 167; one of
+  // 3712 keys, 32 tiles 37 / 74; prompts of 1024..4096 tokens, 32/8 heads 686 / 570; two of 600 tokens 44 / 20).  A tile's start and end
+  // are as long as six units.  Whole tiles, the longest first, end by the shortest one apart at most.  Even shares have up to two parts
+  // more than tiles, which are joined.  Shares of eight units at least: with four or sixteen the one request above takes 42.
+  constexpr int kTileCost = 6, kJoinCost = 14, kLeastShare = 8;
+  const int64_t even = (units + kTileCost * tiles) / plan.places;
+  const int64_t whole = tiles <= plan.places || even + least < t->most_units ? t->most_units : even + least;
+  t->by_tile = whole <= even + kJoinCost;
+  const int64_t most_groups = (units + kLeastShare - 1) / kLeastShare;
+  t->groups = (int32_t)(t->by_tile ? tiles : most_groups < plan.places ? most_groups : plan.places);
   t->share = units / t->groups;
   t->longer = (int32_t)(units - t->share * t->groups);
   return true;

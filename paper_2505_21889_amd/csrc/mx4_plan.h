@@ -58,9 +58,9 @@ struct Mx4FewPlan {
 };
 
 // --- many rows --------------------------------------------------------------------------------------------------------------
-// A tile's work is a unit for each 64 keys in front of and at the last one that its rows see.  The units of all tiles, one behind
-// the other, are dealt evenly to the workgroups: a share is a run of them, which may begin and end inside a tile.  The parts of
-// a tile that several workgroups share are joined by a second kernel.
+// A tile's work is a unit for each 64 keys in front of and at the last one that its rows see.  Either a workgroup has a tile, the
+// longest first; or the units of all tiles, one behind the other, are dealt evenly to the workgroups: a share is a run of them,
+// which may begin and end inside a tile.  The parts of a tile that several workgroups share are joined by a second kernel.
 constexpr int kMx4TableReqs = 96;  // requests of a launch
 
 struct Mx4Req {
@@ -76,7 +76,9 @@ struct Mx4Table {
   Mx4Req req[kMx4TableReqs];
   int64_t share;       // units of a workgroup; the first `longer` have one more
   int32_t longer;
-  int32_t groups;      // workgroups with a share
+  int32_t groups;      // workgroups with a share, or tiles
+  int32_t by_tile;
+  int32_t most_units;  // of a tile
   int32_t nreq;
   int32_t kv_heads;
   int32_t group_heads; // query heads of a kv head
@@ -99,13 +101,21 @@ EFIM_HOST_DEVICE inline int mx4_units_of(const Mx4Req& q, int g, int row_tile, i
   return (mx4_keys_of(q, g, row_tile, tile) + unit_keys - 1) / unit_keys;
 }
 
+// Tiles of a request and kv head that have `units` or more: the last ones.  (A tile has c units where its last row's token lies behind
+// 64 (c - 1) keys; the first such tile is the one of that token's first row.)
+EFIM_HOST_DEVICE inline int mx4_tiles_from(const Mx4Req& q, int g, int row_tile, int unit_keys, int units) {
+  const int token = (units - 1) * unit_keys - q.cached, tiles = mx4_tiles(q, g, row_tile);
+  return token <= 0 ? tiles : token >= q.new_len ? 0 : tiles - token * g / row_tile;
+}
+
 // A workgroup has at most two parts of tiles that it does not have whole: one that goes on where another's ends, and one that
 // begins its tile.
 EFIM_HOST_DEVICE inline int64_t mx4_slot(int group, bool goes_on) { return 2 * (int64_t)group + (goes_on ? 0 : 1); }
 
 struct Mx4ManyPlan {
   bool any = false;
-  int max_groups = 0;  // workgroups to deal to
+  int places = 0;      // workgroups that the device holds
+  size_t slots = 0;    // partial results of the largest launch
 };
 
 // Where the next launch of a class begins.
