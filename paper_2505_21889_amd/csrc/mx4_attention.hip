@@ -44,22 +44,35 @@ struct Mx4Args {
   float scale_log2;  // sm_scale * log2(e)
   float* part_o;     // partial results of split tiles, [slot][row tile][D]: the unnormalised output
   float* part_ml;    // [slot][row tile][2]: reference in log2 units, sum
+  int32_t* splits;   // [workgroup][8]: the tile that its share ends in, for the join: rows (0: ends with a tile, or inside one that began
+                     // in front of it), first row, packed row of the request, head, the last workgroup with a part
   uint16_t* out;
 };
 
-// A lane each (two for each lane), asked for at once: what a unit's request is follows without another load.
+// A lane each (two for each lane), asked for at once: what a unit's request is follows without another load.  (All of the table,
+// whatever it holds: which part of it counts is known at the same time.)
 struct Requests {
   Mx4Req held[2];
   int nreq;
   __device__ __forceinline__ Requests(const Mx4Table& t, int lane) : nreq(t.nreq) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) held[i] = t.req[min(i * 64 + lane, t.nreq - 1)];
+    for (int i = 0; i < 2; ++i) held[i] = t.req[min(i * 64 + lane, kMx4TableReqs - 1)];
   }
   __device__ __forceinline__ int find(int64_t unit, int lane) const {
     int r = -1;
 #pragma unroll
     for (int i = 0; i < 2; ++i) r += __popcll(__ballot(i * 64 + lane < nreq && held[i].unit_start <= unit));
     return __builtin_amdgcn_readfirstlane(r);
+  }
+  __device__ __forceinline__ Mx4Req get(int r) const {
+    const bool upper = r >= 64;
+    auto of = [&](int low, int high) { return __builtin_amdgcn_readlane(upper ? high : low, r & 63); };
+    auto of2 = [&](int64_t low, int64_t high) {
+      return (int64_t)((uint64_t)(uint32_t)of((int)(low >> 32), (int)(high >> 32)) << 32 | (uint32_t)of((int)low, (int)high));
+    };
+    return Mx4Req{of2(held[0].unit_start, held[1].unit_start), of2(held[0].units_per_head, held[1].units_per_head),
+                  of(held[0].req, held[1].req), of(held[0].cached, held[1].cached), of(held[0].new_len, held[1].new_len),
+                  of(held[0].row_start, held[1].row_start)};
   }
 };
 
@@ -71,11 +84,11 @@ struct Place {
   int units;      // of the tile
   int64_t first;  // unit of the launch at which it begins
 };
-template <int TILE, int UNIT>
+template <int TILE>
 __device__ __forceinline__ Place find_tile(const Mx4Table& t, const Requests& requests, int64_t unit, int lane) {
   Place at;
   at.r = requests.find(unit, lane);
-  const Mx4Req q = t.req[at.r];
+  const Mx4Req q = requests.get(at.r);
   const int64_t in = unit - q.unit_start;
   // (fewer than 2^32 units in nearly all launches: a 64-bit division takes hundreds of cycles)
   at.head = (in | q.units_per_head) >> 32 == 0 ? (int)((uint32_t)in / (uint32_t)q.units_per_head) : (int)(in / q.units_per_head);
@@ -83,10 +96,10 @@ __device__ __forceinline__ Place find_tile(const Mx4Table& t, const Requests& re
   at.first = q.unit_start + at.head * q.units_per_head;
   at.tile = 0;
   const int tiles = mx4_tiles(q, t.group_heads, TILE);
-  at.units = mx4_units_of(q, t.group_heads, TILE, UNIT, 0);
+  at.units = mx4_units_of(q, t.group_heads, TILE, t.unit_shift, 0);
   if (tiles == 1) return at;
   for (int t0 = 0; t0 < tiles; t0 += 64) {
-    const int mine = t0 + lane < tiles ? mx4_units_of(q, t.group_heads, TILE, UNIT, t0 + lane) : 0;
+    const int mine = t0 + lane < tiles ? mx4_units_of(q, t.group_heads, TILE, t.unit_shift, t0 + lane) : 0;
     int upto = mine;  // of the lanes up to this one
 #pragma unroll
     for (int by = 1; by < 64; by <<= 1) {
@@ -118,13 +131,11 @@ __device__ __forceinline__ int lanes_sum(int v) {
 
 // The tile that is the n-th in the order of their units, the largest first, by the whole wave: what starts last is then
 // short.  Of equally long tiles the heads are next to each other, so that an XCD meets few of them.
-template <int TILE, int UNIT>
-__device__ __forceinline__ Place nth_tile(const Mx4Table& t, int n, int lane) {
+template <int TILE>
+__device__ __forceinline__ Place nth_tile(const Mx4Table& t, const Requests& requests, int n, int lane) {
   const int g = t.group_heads;
-  Mx4Req q[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) q[i] = t.req[min(i * 64 + lane, t.nreq - 1)];
-  auto longer = [&](int c, int i) { return i * 64 + lane < t.nreq ? mx4_tiles_from(q[i], g, TILE, UNIT, c) : 0; };
+  const auto& q = requests.held;
+  auto longer = [&](int c, int i) { return i * 64 + lane < t.nreq ? mx4_tiles_from(q[i], g, TILE, t.unit_shift, c) : 0; };
   auto of_all = [&](int c) { return t.kv_heads * lanes_sum(longer(c, 0) + longer(c, 1)); };
   int low = 1, high = t.most_units + 1;  // the units of the tile: more tiles than n have `low` or more, at most n `high` or more
   while (high - low > 1) {
@@ -148,7 +159,7 @@ __device__ __forceinline__ Place nth_tile(const Mx4Table& t, int n, int lane) {
       in -= __builtin_amdgcn_readlane(upto - mine, k);
       at.r = i * 64 + k;
       at.head = in % t.kv_heads;
-      at.tile = mx4_tiles(t.req[at.r], g, TILE) - __builtin_amdgcn_readlane(longer(low, i), k) + in / t.kv_heads;
+      at.tile = mx4_tiles(requests.get(at.r), g, TILE) - __builtin_amdgcn_readlane(longer(low, i), k) + in / t.kv_heads;
       break;
     }
     in -= __builtin_amdgcn_readlane(upto, 63);
@@ -158,7 +169,7 @@ __device__ __forceinline__ Place nth_tile(const Mx4Table& t, int n, int lane) {
 }
 
 // A workgroup's share of the units, a tile's part at a time.
-template <int TILE, int UNIT>
+template <int TILE>
 struct Share {
   const Mx4Table& t;
   Place at;
@@ -171,12 +182,13 @@ struct Share {
   int64_t slot;    // partial result, -1: the workgroup has the whole tile
 
   __device__ __forceinline__ Share(const Mx4Table& table, int lane) : t(table) {
+    const Requests requests(table, lane);
     if (t.by_tile) {
       group = 0;
-      at = nth_tile<TILE, UNIT>(t, blockIdx.x, lane);
+      at = nth_tile<TILE>(t, requests, blockIdx.x, lane);
       begin = at.first;
       end = begin + at.units;
-      rq = t.req[at.r];
+      rq = requests.get(at.r);
       part();
       return;
     }
@@ -186,19 +198,24 @@ struct Share {
     if (group >= t.groups) return;
     begin = t.first_unit(group);
     end = t.first_unit(group + 1);
-    const Requests requests(table, lane);
-    at = find_tile<TILE, UNIT>(t, requests, begin, lane);
-    rq = t.req[at.r];
+    at = find_tile<TILE>(t, requests, begin, lane);
+    rq = requests.get(at.r);
     part();
   }
   __device__ __forceinline__ bool done() const { return begin >= end; }
+  __device__ __forceinline__ bool ends() const { return at.first + at.units >= end; }  // with the part at hand
+  __device__ __forceinline__ int last_group() const {  // with a part of the tile at hand
+    int last = group;
+    while (last + 1 < t.groups && t.first_unit(last + 1) < at.first + at.units) ++last;
+    return last;
+  }
   __device__ __forceinline__ void part() {
     row0 = at.tile * TILE;
     rows = mx4_rows_of(rq, t.group_heads, TILE, at.tile);
     const int u0 = (int)(begin - at.first);
     const int u1 = (int)min((int64_t)at.units, end - at.first);
-    k0 = u0 * UNIT;
-    k1 = min(u1 * UNIT, mx4_keys_of(rq, t.group_heads, TILE, at.tile));
+    k0 = u0 << t.unit_shift;
+    k1 = min((int64_t)u1 << t.unit_shift, (int64_t)mx4_keys_of(rq, t.group_heads, TILE, at.tile));
     slot = u0 == 0 && u1 == at.units ? -1 : mx4_slot(group, u0 > 0);
   }
   __device__ __forceinline__ void advance() {
@@ -212,7 +229,7 @@ struct Share {
         rq = t.req[++at.r];
       }
     }
-    at.units = mx4_units_of(rq, t.group_heads, TILE, UNIT, at.tile);
+    at.units = mx4_units_of(rq, t.group_heads, TILE, t.unit_shift, at.tile);
     part();
   }
 };
@@ -617,8 +634,10 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 3 : 2) void mx4_few_kernel(
   }
 }
 
-// The parts of a split tile: with M = max m_s,  out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A workgroup for each; where it has
-// more threads than the rows need, they share the parts and are joined through LDS.  Bound by latency: four parts at a time.
+// The parts of a split tile: with M = max m_s,  out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  A workgroup for two rows of each, which
+// its threads share by parts and join through LDS.  Bound by latency: four parts at a time.  (us with one, two and four or more rows: 5
+// requests of 28 rows and 5300 keys 9.7, 9.4 and 10.6, one of 4 rows and 2344 keys with its first kernel 10.9, 10.6 and 11.4.)
+constexpr int kJoinRows = 2;
 template <int D, int ROWS, int MAXREQ>
 __global__ __launch_bounds__(kThreads) void mx4_few_join_kernel(const Mx4FewArgs<MAXREQ> args) {
   constexpr int kVec = D / 4;                // threads of a row
@@ -634,10 +653,8 @@ __global__ __launch_bounds__(kThreads) void mx4_few_join_kernel(const Mx4FewArgs
   const int rows = requests.of(requests.new_len, r) * g, row_start = requests.of(requests.row_start, r);
   const int64_t first = requests.of(requests.slot_start, r) + (int64_t)head * parts;
   const int c = threadIdx.x % kVec * 4, place = threadIdx.x / kVec;
-  int at_once = 1;  // rows at a time
-  while (at_once < rows && at_once < kPlaces) at_once *= 2;
+  const int at_once = rows == 1 ? 1 : kJoinRows;
   const int slices = kPlaces / at_once, slice = place / at_once;
-  // (where the rows are fewer than the places they are the first workgroup's, else a workgroup has as many as there are places)
   for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {
     const int row = min(row0 + place % at_once, rows - 1);
     float m = kNoReference, l = 0.f;
@@ -746,7 +763,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
   const uint32_t put_at = lds0 + in_round * kRowBytes + (first_matrix == 0 ? put_key : kRingBytes + put_value);
   const uint32_t put_apart = put_key ^ put_value;
 
-  for (Share<kTile, kMx4ManyKeys> it(t, lane); !it.done(); it.advance()) {
+  for (Share<kTile> it(t, lane); !it.done(); it.advance()) {
     const Cache<D> cache(k_cache, block_table, t, it.rq.req, it.at.head);
     const int local = wave * 32 + i32;
     const bool row_ok = local < it.rows;
@@ -1039,40 +1056,38 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
         }
       if (it.slot >= 0 && hi == 0) *reinterpret_cast<f32x2*>(args.part_ml + part * 2) = f32x2{m_run, l};
     }
+    if (tid == 0 && !t.by_tile && it.ends()) {
+      const bool begins = it.slot == mx4_slot(it.group, false);
+      *reinterpret_cast<u32x4*>(args.splits + 8 * (int64_t)it.group) =
+          u32x4{begins ? (uint32_t)it.rows : 0u, (uint32_t)it.row0, (uint32_t)it.rq.row_start, (uint32_t)it.at.head};
+      args.splits[8 * (int64_t)it.group + 4] = begins ? it.last_group() : 0;
+    }
     __syncthreads();
   }
 }
 
 // --- join -------------------------------------------------------------------------------------------------------------------
 // The parts of split tiles: with M = max m_s,  out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, in the order of the keys.  Workgroup
-// i has the tile in which the shares of workgroups i and i + 1 are the first to meet.  Bound by latency: four parts at a time.
-template <int D, int TILE, int UNIT>
+// i has the tile that begins in share i and ends in a further one.  Bound by latency: what the tile is was left by its first part, and
+// four parts are read at a time.
+template <int D>
 __global__ __launch_bounds__(kThreads) void mx4_join_kernel(const Mx4Args args) {
   constexpr int kAtOnce = 4;
-  const Mx4Table& t = args.table;
-  const int lane = threadIdx.x & 63;
-  const int second = blockIdx.x + 1;  // workgroup that goes on where another's share ends
-  const int64_t unit = t.first_unit(second);
-  const Requests requests(t, lane);
-  const Place at = find_tile<TILE, UNIT>(t, requests, unit, lane);
-  if (at.first == unit || t.first_unit(second - 1) > at.first) return;
-  const Mx4Req rq = t.req[at.r];
-  const int g = t.group_heads, hq = g * t.kv_heads;
-  const int rows = mx4_rows_of(rq, g, TILE, at.tile);
-  const int64_t end = at.first + at.units;
-  int last = second;
-  while (last + 1 < t.groups && t.first_unit(last + 1) < end) ++last;
+  const int g = args.table.group_heads, hq = g * args.table.kv_heads;
+  const auto* split = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(args.splits + 8 * (int64_t)blockIdx.x);  // (scalar loads)
+  const int rows = split[0], row0 = split[1], row_start = split[2], head = split[3], last = split[4];
+  const int first = blockIdx.x;
   constexpr int kVec = D / 4;
   const int c = threadIdx.x % kVec * 4;
   for (int r = blockIdx.y * (kThreads / kVec) + threadIdx.x / kVec; r < rows; r += gridDim.y * (kThreads / kVec)) {
     float m = kNoReference, l = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int group = second - 1; group <= last; group += kAtOnce) {
+    for (int group = first; group <= last; group += kAtOnce) {
       f32x2 ml[kAtOnce];
       f32x4 x[kAtOnce];
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
-        const int64_t part = mx4_slot(min(group + i, last), group + i >= second) * TILE + r;
+        const int64_t part = mx4_slot(min(group + i, last), group + i > first) * kMx4ManyRows + r;
         ml[i] = *reinterpret_cast<const f32x2*>(args.part_ml + part * 2);
         x[i] = *reinterpret_cast<const f32x4*>(args.part_o + part * D + c);
       }
@@ -1092,8 +1107,8 @@ __global__ __launch_bounds__(kThreads) void mx4_join_kernel(const Mx4Args args) 
       }
     }
     const float inv = 1.f / l;
-    const int row = at.tile * TILE + r, tok = row / g;
-    *reinterpret_cast<u32x2*>(args.out + ((int64_t)(rq.row_start + tok) * hq + at.head * g + (row - tok * g)) * D + c) =
+    const int row = row0 + r, tok = row / g;
+    *reinterpret_cast<u32x2*>(args.out + ((int64_t)(row_start + tok) * hq + head * g + (row - tok * g)) * D + c) =
         u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
   }
 }
@@ -1123,7 +1138,7 @@ int launch_few(const efim_batch_t* b, const Mx4FewPlan& plan, const Mx4Tensors& 
   Mx4Cursor at;
   while (mx4_next(b, plan, &at, &args.table)) {
     mx4_few_kernel<D, NB, MAXREQ><<<args.table.groups, kThreads, 0, stream>>>(args, x.q, x.k_cache, x.v_cache, x.block_table);
-    if (args.table.splits > 0) mx4_few_join_kernel<D, 16 * NB, MAXREQ><<<dim3((unsigned)args.table.splits, (16 * NB + kThreads / (D / 4) - 1) / (kThreads / (D / 4))), kThreads, 0, stream>>>(args);
+    if (args.table.splits > 0) mx4_few_join_kernel<D, 16 * NB, MAXREQ><<<dim3((unsigned)args.table.splits, 16 * NB / kJoinRows), kThreads, 0, stream>>>(args);
     const int rc = last_error();
     if (rc != EFIM_OK) return rc;
   }
@@ -1136,6 +1151,7 @@ int launch_many(const efim_batch_t* b, const Mx4ManyPlan& plan, const Mx4Tensors
   args.scale_log2 = x.scale_log2;
   args.part_o = reinterpret_cast<float*>(workspace);
   args.part_ml = reinterpret_cast<float*>(workspace + mx4_bytes(plan.slots, kMx4ManyRows, D).off_ml);
+  args.splits = reinterpret_cast<int32_t*>(workspace + mx4_bytes(plan.slots, kMx4ManyRows, D).total);
   args.out = x.out;
   constexpr int kAtOnce = kThreads / (D / 4);
   Mx4Cursor at;
@@ -1145,8 +1161,8 @@ int launch_many(const efim_batch_t* b, const Mx4ManyPlan& plan, const Mx4Tensors
     auto* kernel = b->page_size < 2048 / D ? mx4_many_kernel<D, true> : mx4_many_kernel<D, false>;
     kernel<<<launched, kThreads, 0, stream>>>(args, x.q, x.k_cache, x.v_cache, x.block_table);
     if (!args.table.by_tile && groups > 1)
-      mx4_join_kernel<D, kMx4ManyRows, kMx4ManyKeys>
-          <<<dim3((unsigned)groups - 1, (kMx4ManyRows + 2 * kAtOnce - 1) / (2 * kAtOnce)), kThreads, 0, stream>>>(args);
+      mx4_join_kernel<D>
+          <<<dim3((unsigned)groups - 1, kMx4ManyRows / kAtOnce), kThreads, 0, stream>>>(args);
     const int rc = last_error();
     if (rc != EFIM_OK) return rc;
   }
@@ -1160,7 +1176,7 @@ struct Mx4Work {
   size_t many_at = 0, total = 0;
   explicit Mx4Work(const efim_batch_t* b) : few(plan_mx4_few(b, compute_units())), many(plan_mx4_many(b, compute_units())) {
     if (few.any) many_at = mx4_bytes(few.slots, few.row_tile, b->head_dim).total;
-    total = many_at + (many.any ? mx4_bytes(many.slots, kMx4ManyRows, b->head_dim).total : 0);
+    total = many_at + (many.any ? mx4_bytes(many.slots, kMx4ManyRows, b->head_dim).total + (many.slots / 2 * 32 + 255) / 256 * 256 : 0);
     if (total < 256) total = 256;
   }
 };

@@ -127,6 +127,8 @@ bool mx4_next(const efim_batch_t* b, const Mx4ManyPlan& plan, Mx4Cursor* at, Mx4
   t->group_heads = group_of(b);
   t->max_pages = b->max_pages_per_req;
   t->page_shift = page_shift_of(b);
+  t->unit_shift = kMx4ManyShift;
+  const int g = t->group_heads;
   int64_t units = 0, tiles = 0;
   int least = INT32_MAX;
   for (; at->req < b->batch && t->nreq < kMx4TableReqs; ++at->req) {
@@ -134,10 +136,10 @@ bool mx4_next(const efim_batch_t* b, const Mx4ManyPlan& plan, Mx4Cursor* at, Mx4
     if (is_many(b, at->req)) {
       Mx4Req& q = t->req[t->nreq++];
       q = Mx4Req{units, 0, at->req, b->cached_len[at->req], n, (int32_t)at->row};
-      const int mine = mx4_tiles(q, t->group_heads, kMx4ManyRows);
-      for (int tile = 0; tile < mine; ++tile) q.units_per_head += mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, tile);
-      const int last = mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, mine - 1);
-      const int first = mx4_units_of(q, t->group_heads, kMx4ManyRows, kMx4ManyKeys, 0);
+      const int mine = mx4_tiles(q, g, kMx4ManyRows);
+      for (int tile = 0; tile < mine; ++tile) q.units_per_head += mx4_units_of(q, g, kMx4ManyRows, kMx4ManyShift, tile);
+      const int last = mx4_units_of(q, g, kMx4ManyRows, kMx4ManyShift, mine - 1);
+      const int first = mx4_units_of(q, g, kMx4ManyRows, kMx4ManyShift, 0);
       t->most_units = last > t->most_units ? last : t->most_units;
       least = first < least ? first : least;
       units += q.units_per_head * t->kv_heads;
@@ -146,16 +148,35 @@ bool mx4_next(const efim_batch_t* b, const Mx4ManyPlan& plan, Mx4Cursor* at, Mx4
     at->row += n;
   }
   if (t->nreq == 0) return false;
-  // What either way takes, in units (us even / whole tiles: 32 requests of 2048..8192 keys and 8..64 tokens, 28/4 heads 121 / 167; one of
-  // 3712 keys, 32 tiles 37 / 74; prompts of 1024..4096 tokens, 32/8 heads 686 / 570; two of 600 tokens 44 / 20).  A tile's start and end
-  // are as long as six units.  Whole tiles, the longest first, end by the shortest one apart at most.  Even shares have up to two parts
-  // more than tiles, which are joined.  Shares of eight units at least: with four or sixteen the one request above takes 42.
-  constexpr int kTileCost = 6, kJoinCost = 14, kLeastShare = 8;
+  // What the ways take, in units of 64 keys (us even shares / whole tiles: 32 requests of 2048..8192 keys and 8..64 tokens, 28/4 heads
+  // 117 / 165; one of 3712 keys, 32 tiles 32 / 74; prompts of 1024..4096 tokens, 32/8 heads 686 / 570; two of 600 tokens 44 / 20).  A tile's
+  // start and end are as long as six units.  Whole tiles, the longest first, end by the shortest one apart at most.  Even
+  // shares have up to two parts more than tiles, which are joined.
+  constexpr int kTileCost = 6, kJoinCost = 14;
   const int64_t even = (units + kTileCost * tiles) / plan.places;
   const int64_t whole = tiles <= plan.places || even + least < t->most_units ? t->most_units : even + least;
   t->by_tile = whole <= even + kJoinCost;
-  const int64_t most_groups = (units + kLeastShare - 1) / kLeastShare;
-  t->groups = (int32_t)(t->by_tile ? tiles : most_groups < plan.places ? most_groups : plan.places);
+  t->groups = (int32_t)(t->by_tile ? tiles : units < plan.places ? units : plan.places);
+  // Where the device has a place for each of the units of eight (or sixteen, ..) times as many keys, and they are not much longer than
+  // an even share with its second part: those.  (The one request above 27 us, in shares that are not cut at tiles' ends 33.)
+  constexpr int kLeast = 8;
+  for (int shift = kMx4ManyShift + 3; !t->by_tile && (1 << (shift - kMx4ManyShift)) <= (even < kLeast ? kLeast : even) + kTileCost; ++shift) {
+    int64_t starts[kMx4TableReqs], heads[kMx4TableReqs], all = 0;
+    for (int k = 0; k < t->nreq; ++k) {
+      starts[k] = all;
+      heads[k] = 0;
+      for (int tile = mx4_tiles(t->req[k], g, kMx4ManyRows) - 1; tile >= 0; --tile) heads[k] += mx4_units_of(t->req[k], g, kMx4ManyRows, shift, tile);
+      all += heads[k] * t->kv_heads;
+    }
+    if (all > plan.places) continue;
+    for (int k = 0; k < t->nreq; ++k) {
+      t->req[k].unit_start = starts[k];
+      t->req[k].units_per_head = heads[k];
+    }
+    t->unit_shift = shift;
+    t->groups = (int32_t)(units = all);
+    break;
+  }
   t->share = units / t->groups;
   t->longer = (int32_t)(units - t->share * t->groups);
   return true;

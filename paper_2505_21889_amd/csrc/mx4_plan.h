@@ -20,7 +20,7 @@ namespace efim {
 constexpr int kMx4FewRows = 32;    // query rows of a request and kv head that the kernel for few rows takes
 constexpr int kMx4FewKeys = 128;   // keys of its units: 32 for each of its four waves
 constexpr int kMx4ManyRows = 128;  // row tile of the kernel for many rows
-constexpr int kMx4ManyKeys = 64;   // keys of its units
+constexpr int kMx4ManyShift = 6;   // log2 of the keys of its units
 
 // --- few rows ---------------------------------------------------------------------------------------------------------------
 // A request is one tile a kv head.  Its keys are cut into parts of as many units, a workgroup each; the parts of a tile that has
@@ -59,8 +59,9 @@ struct Mx4FewPlan {
 
 // --- many rows --------------------------------------------------------------------------------------------------------------
 // A tile's work is a unit for each 64 keys in front of and at the last one that its rows see.  Either a workgroup has a tile, the
-// longest first; or the units of all tiles, one behind the other, are dealt evenly to the workgroups: a share is a run of them,
-// which may begin and end inside a tile.  The parts of a tile that several workgroups share are joined by a second kernel.
+// longest first; or a unit of so many more keys that there is one for each workgroup; or the units of all tiles, one behind the other,
+// are dealt evenly to the workgroups: a share is a run of them, which may begin and end inside a tile.  The parts of a tile that
+// several workgroups share are joined by a second kernel.
 constexpr int kMx4TableReqs = 96;  // requests of a launch
 
 struct Mx4Req {
@@ -79,6 +80,7 @@ struct Mx4Table {
   int32_t groups;      // workgroups with a share, or tiles
   int32_t by_tile;
   int32_t most_units;  // of a tile
+  int32_t unit_shift;  // log2 of a unit's keys
   int32_t nreq;
   int32_t kv_heads;
   int32_t group_heads; // query heads of a kv head
@@ -97,14 +99,14 @@ EFIM_HOST_DEVICE inline int mx4_rows_of(const Mx4Req& q, int g, int row_tile, in
 EFIM_HOST_DEVICE inline int mx4_keys_of(const Mx4Req& q, int g, int row_tile, int tile) {
   return q.cached + (tile * row_tile + mx4_rows_of(q, g, row_tile, tile) - 1) / g + 1;
 }
-EFIM_HOST_DEVICE inline int mx4_units_of(const Mx4Req& q, int g, int row_tile, int unit_keys, int tile) {
-  return (mx4_keys_of(q, g, row_tile, tile) + unit_keys - 1) / unit_keys;
+EFIM_HOST_DEVICE inline int mx4_units_of(const Mx4Req& q, int g, int row_tile, int unit_shift, int tile) {
+  return ((mx4_keys_of(q, g, row_tile, tile) - 1) >> unit_shift) + 1;
 }
 
 // Tiles of a request and kv head that have `units` or more: the last ones.  (A tile has c units where its last row's token lies behind
-// 64 (c - 1) keys; the first such tile is the one of that token's first row.)
-EFIM_HOST_DEVICE inline int mx4_tiles_from(const Mx4Req& q, int g, int row_tile, int unit_keys, int units) {
-  const int token = (units - 1) * unit_keys - q.cached, tiles = mx4_tiles(q, g, row_tile);
+// the keys of c - 1; the first such tile is the one of that token's first row.)
+EFIM_HOST_DEVICE inline int mx4_tiles_from(const Mx4Req& q, int g, int row_tile, int unit_shift, int units) {
+  const int token = ((units - 1) << unit_shift) - q.cached, tiles = mx4_tiles(q, g, row_tile);
   return token <= 0 ? tiles : token >= q.new_len ? 0 : tiles - token * g / row_tile;
 }
 
