@@ -6,12 +6,13 @@
 //
 // Few tokens of the vocabulary have anything done to them, the same ones in all rows of a request.  A first kernel marks them in a
 // bit for each token and lists them, with how often they were made and their bias (counted in whole numbers: no order
-// changes the result).  Behind it the others are taken as they are, and an element costs two bits and the exponential; the listed ones
-// are gone through apart.  A second kernel leaves maximum, sum and place of the maximum of every chunk of a row, a third forms the
+// changes the result).  Behind it the others are taken as they are, and an element costs two bits and the exponential.  A second kernel leaves maximum, sum and place of the maximum of every chunk of a row, a third forms the
 // probabilities from them; in both a wave has a chunk of a row to itself and waits for no other.  Bound by reading the logits, the
 // second time mostly from the caches, and by writing the probabilities.
-// (A workgroup for each row and slice that makes its own list in LDS, two kernels: 15.7 us for 6 rows of 32004 and 271 us for 64
-// requests with 1 to 15 drafts and 128003, where these take 20.4 and 194 us, of it 12 list, 68 statistics and 112 probabilities.)
+// us for 6 rows of 32004 / for 64 requests with 1 to 15 drafts and 128003: 18.0 / 177, of the latter 12 list, 65 statistics (their
+// instructions take 70 % of the issue cycles) and 98 probabilities (415 MB, 4.2 TB/s).  A workgroup for each row and slice that makes its
+// own list, two kernels: 15.7 / 271.  Listed tokens gone through behind the others instead of through LDS: 20.4 / 194.  A wave for a
+// chunk of four rows that loads the list once: 18.5 / 248 (half as many waves at a time).
 #include <cstdint>
 #include <type_traits>
 
@@ -379,14 +380,31 @@ struct Seen {
   }
 };
 
-// A wave for each chunk of each row.  WRITE: the third kernel.  MASKED: there is a mask at least, and a number of one for each row.
+// A wave for each chunk of each row.  What its listed tokens' logits become goes through LDS to the lanes that have their places.  WRITE: the
+// third kernel.  MASKED: there is a mask at least, and a number of one for each row.
 template <bool BF16, bool MASKED, bool WRITE>
 __global__ __launch_bounds__(kThreads) void probs_rows_kernel(const ProbsArgs a) {
 #pragma clang fp contract(off)
-  const int lane = threadIdx.x & 63;
-  const int task = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
+  __shared__ __attribute__((aligned(16))) float s_z[kThreads / 64][kChunk];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int task = blockIdx.x * (kThreads / 64) + wave;
   const int index = task / a.chunks, part = task - index * a.chunks;
   if (index >= a.total) return;
+  const int first = part * kChunk, end = min(first + kChunk, a.vocab);
+  const bool full = end - first == kChunk;
+  float* const touched = s_z[wave];
+  struct Group {
+    Four<BF16> x[kSteps];
+    uint32_t marks[kSteps], allowed[kSteps];
+  };
+  Group group;
+  if (full) {  // (in front of all else: nothing else has to be known for it)
+    // (a wave-uniform address and the lane's place behind it)
+    const char* from = static_cast<const char*>(a.logits) + ((a.row_base + index) * a.logits_stride + first) * Four<BF16>::kBytes;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      group.x[s].x = *reinterpret_cast<const typename Four<BF16>::Words*>(from + s * (kStep * Four<BF16>::kBytes) + lane * (kPerLane * Four<BF16>::kBytes));
+  }
   Row row;
   row.load<MASKED>(a, index);
   const RowInfo& info = row.info;
@@ -395,15 +413,16 @@ __global__ __launch_bounds__(kThreads) void probs_rows_kernel(const ProbsArgs a)
 
   // The chunk's listed tokens, N to a lane from entry j0 of the list on.
   const auto* starts = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.starts + (int64_t)info.request * (a.chunks + 1) + part);
-  const int list_end = starts[1];
+  const int list_begin = starts[0], list_end = starts[1];
   const int64_t list_base = (int64_t)info.request * a.most_listed;
   const int request = a.req_base + info.request;
   efim_sampling_t how = {1.f, 1.f, 0.f, 0.f, 0, 0, 0, 0};
   if (a.params) how = a.params[request];
+  const float* biases = a.bias_values ? a.bias_values + (int64_t)request * a.bias_stride : reinterpret_cast<const float*>(a.listed);
   auto entries_of = [](auto n) {
     struct Entries {
       int token[decltype(n)::value], entry[decltype(n)::value];
-      uint32_t count[decltype(n)::value], word[decltype(n)::value];
+      uint32_t count[decltype(n)::value];
       float z[decltype(n)::value], bias[decltype(n)::value];
     };
     return Entries{};
@@ -423,15 +442,12 @@ __global__ __launch_bounds__(kThreads) void probs_rows_kernel(const ProbsArgs a)
 #pragma unroll
     for (int k = 0; k < decltype(n_c)::value; ++k) {
       l.z[k] = load_logit<BF16>(a.logits, row.at + l.token[k]);
-      l.word[k] = row.allowed_word<MASKED>(l.token[k] >> 5);
-      if (a.bias_values) l.bias[k] = a.bias_values[(int64_t)request * a.bias_stride + max(l.entry[k] - 1, 0)];
+      l.bias[k] = biases[max(l.entry[k] - 1, 0)];
     }
   };
   auto work_listed = [&](auto n_c, int j0, auto& l) __attribute__((always_inline)) {
-    constexpr int N = decltype(n_c)::value;
-    bool in[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
+    for (int k = 0; k < decltype(n_c)::value; ++k) {
       float z = l.z[k];
       uint32_t count = l.count[k];
       if (count & kDrafted) {
@@ -443,81 +459,67 @@ __global__ __launch_bounds__(kThreads) void probs_rows_kernel(const ProbsArgs a)
       const float often = how.frequency * (float)count;
       z = count ? z - often - how.presence : z;
       z = l.entry[k] ? z + l.bias[k] : z;
-      in[k] = (l.word[k] >> (l.token[k] & 31) & 1) != 0;
-      l.z[k] = in[k] && j0 + k * 64 + lane < list_end ? z : -INFINITY;
-    }
-    if constexpr (!WRITE) {
-      seen.take(info, l.z, l.token);
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (j0 + k * 64 + lane < list_end) row.probs[l.token[k]] = in[k] ? whole.probability(info, l.z[k], l.token[k]) : 0.f;
-    }
-  };
-
-  const int first = part * kChunk, end = min(first + kChunk, a.vocab);
-  const bool full = end - first == kChunk;
-  struct Group {
-    Four<BF16> x[kSteps];
-    uint32_t marks[kSteps], allowed[kSteps];
-  };
-  auto load = [&](int at, Group& g) __attribute__((always_inline)) {
-    // (wave-uniform addresses and the lane's place behind them)
-    const char* from = static_cast<const char*>(a.logits) + (row.at + at) * Four<BF16>::kBytes;
-    const char* marks = reinterpret_cast<const char*>(row.marks) + at / 8;
-    const char* masks = reinterpret_cast<const char*>(row.mask) + at / 8;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      g.x[s].x = *reinterpret_cast<const typename Four<BF16>::Words*>(from + s * (kStep * Four<BF16>::kBytes) + lane * (kPerLane * Four<BF16>::kBytes));
-      g.marks[s] = *reinterpret_cast<const uint32_t*>(marks + s * (kStep / 8) + (lane / 8u) * 4u);
-      if constexpr (MASKED) g.allowed[s] = *reinterpret_cast<const uint32_t*>(masks + s * (kStep / 8) + (lane / 8u) * 4u);
-      else g.allowed[s] = 0;
-    }
-  };
-  // (bit selects: a condition for each of the elements would be more than there are registers for conditions)
-  auto all_ones = [](uint32_t bits, int k) { return (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1); };
-  const int shift = lane * kPerLane & 31;
-  auto work = [&](int at, const Group& g) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int token = at + s * kStep + lane * kPerLane;
-      const uint32_t plain = ~g.marks[s] >> shift;
-      const uint32_t in = MASKED ? ((g.allowed[s] | row.all) & row.some) >> shift & plain : row.some & plain;
-      float z[kPerLane];
-      int tokens[kPerLane];
-#pragma unroll
-      for (int k = 0; k < kPerLane; ++k) {
-        const uint32_t m = all_ones(in, k);
-        z[k] = __uint_as_float((m & __float_as_uint(g.x[s][k])) | (~m & 0xFF800000u));
-        tokens[k] = token + k;
-      }
-      if constexpr (!WRITE) {
-        seen.take(info, z, tokens);
-      } else {
-        float p[kPerLane];
-#pragma unroll
-        for (int k = 0; k < kPerLane; ++k) p[k] = __uint_as_float(all_ones(in, k) & __float_as_uint(whole.probability(info, z[k], tokens[k])));
-        // (Listed tokens' are written behind these.  Their logits may lie in the same place and are left there until then.)
-        if constexpr (!BF16) {
-#pragma unroll
-          for (int k = 0; k < kPerLane; ++k) {
-            const uint32_t m = all_ones(plain, k);
-            p[k] = __uint_as_float((m & __float_as_uint(p[k])) | (~m & __float_as_uint(g.x[s][k])));
-          }
-        }
-        *reinterpret_cast<f32x4*>(reinterpret_cast<char*>(row.probs + at + s * kStep) + lane * (kPerLane * 4u)) = f32x4{p[0], p[1], p[2], p[3]};
-      }
+      if (j0 + k * 64 + lane < list_end) touched[l.token[k] - first] = z;
     }
   };
   // (what the list's first entries need is on its way beside the rest)
-  const int list_begin = starts[0];
   auto entries = entries_of(kOne);
   if (list_begin < list_end) load_listed(kOne, list_begin, entries);
-  Group group;
-  if (full) load(first, group);
+  if (full) {
+    const char* marks = reinterpret_cast<const char*>(row.marks) + first / 8;
+    const char* masks = reinterpret_cast<const char*>(row.mask) + first / 8;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      group.marks[s] = *reinterpret_cast<const uint32_t*>(marks + s * (kStep / 8) + (lane / 8u) * 4u);
+      if constexpr (MASKED) group.allowed[s] = *reinterpret_cast<const uint32_t*>(masks + s * (kStep / 8) + (lane / 8u) * 4u);
+      else group.allowed[s] = 0;
+    }
+  }
   if (list_begin < list_end) load_logits(kOne, entries);
   if constexpr (WRITE) whole.load(a, index, info, lane);
-  if (full) work(first, group);
+  if (list_begin < list_end) work_listed(kOne, list_begin, entries);
+  for (int j0 = list_begin + 64; j0 < list_end; j0 += kListed * 64) {
+    auto more = entries_of(kMore);
+    load_listed(kMore, j0, more);
+    load_logits(kMore, more);
+    work_listed(kMore, j0, more);
+  }
+  // (a wave's own places: the accesses are in order, the compiler is told)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+
+  if (full) {
+    // (bit selects: a condition for each of the elements would be more than there are registers for conditions)
+    auto all_ones = [](uint32_t bits, int k) { return (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1); };
+    const int shift = lane * kPerLane & 31;
+    float z[kSteps * kPerLane];
+    int tokens[kSteps * kPerLane];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int token = first + s * kStep + lane * kPerLane;
+      const uint32_t marked = group.marks[s] >> shift;
+      const uint32_t in = MASKED ? ((group.allowed[s] | row.all) & row.some) >> shift : row.some;
+      const f32x4 other = *reinterpret_cast<const f32x4*>(touched + s * kStep + lane * kPerLane);  // (whatever it is where there are no marks)
+      const Four<BF16> own = group.x[s];
+      uint32_t in_bits[kPerLane];
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) {
+        const uint32_t m = all_ones(marked, k);
+        in_bits[k] = all_ones(in, k);
+        const uint32_t y = (m & __float_as_uint(other[k])) | (~m & __float_as_uint(own[k]));
+        z[s * kPerLane + k] = __uint_as_float((in_bits[k] & y) | (~in_bits[k] & 0xFF800000u));
+        tokens[s * kPerLane + k] = token + k;
+      }
+      if constexpr (WRITE) {
+        float p[kPerLane];
+#pragma unroll
+        for (int k = 0; k < kPerLane; ++k) p[k] = __uint_as_float(in_bits[k] & __float_as_uint(whole.probability(info, z[s * kPerLane + k], token + k)));
+        *reinterpret_cast<f32x4*>(reinterpret_cast<char*>(row.probs + first + s * kStep) + lane * (kPerLane * 4u)) = f32x4{p[0], p[1], p[2], p[3]};
+      }
+    }
+    if constexpr (!WRITE) seen.take(info, z, tokens);
+  }
   // the vocabulary's last chunk, an element to a lane
   constexpr int kTail = 4;
   for (int at = full ? end : first + lane; at < end; at += kTail * 64) {
@@ -531,33 +533,20 @@ __global__ __launch_bounds__(kThreads) void probs_rows_kernel(const ProbsArgs a)
       marks[k] = row.marks[tokens[k] >> 5];
       words[k] = row.allowed_word<MASKED>(tokens[k] >> 5);
     }
-    bool mine[kTail], in[kTail];
+    bool in[kTail];
 #pragma unroll
     for (int k = 0; k < kTail; ++k) {
-      mine[k] = at + k * 64 < end && (marks[k] >> (tokens[k] & 31) & 1) == 0;
+      if (marks[k] >> (tokens[k] & 31) & 1) z[k] = touched[tokens[k] - first];
       in[k] = (words[k] >> (tokens[k] & 31) & 1) != 0;
-      if (!mine[k] || !in[k]) z[k] = -INFINITY;
+      if (!in[k] || at + k * 64 >= end) z[k] = -INFINITY;
     }
     if constexpr (!WRITE) {
       seen.take(info, z, tokens);
     } else {
 #pragma unroll
       for (int k = 0; k < kTail; ++k)
-        if (mine[k]) row.probs[tokens[k]] = in[k] ? whole.probability(info, z[k], tokens[k]) : 0.f;
+        if (at + k * 64 < end) row.probs[tokens[k]] = in[k] ? whole.probability(info, z[k], tokens[k]) : 0.f;
     }
-  }
-  if constexpr (WRITE) {
-    // (one wave's stores to one place stay in order)
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  }
-  if (list_begin < list_end) work_listed(kOne, list_begin, entries);
-  for (int j0 = list_begin + 64; j0 < list_end; j0 += kListed * 64) {
-    auto more = entries_of(kMore);
-    load_listed(kMore, j0, more);
-    load_logits(kMore, more);
-    work_listed(kMore, j0, more);
   }
   if constexpr (!WRITE) seen.leave(a.stats + (int64_t)index * a.chunks + part, info, lane);
 }
