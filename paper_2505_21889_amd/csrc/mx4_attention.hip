@@ -279,9 +279,10 @@ template <int D>
 __device__ __forceinline__ int key_swizzle(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
 template <int D>
 __device__ __forceinline__ int value_swizzle(int row) { return D == 128 ? (row & 3) * 5 : (row >> 1 & 3) ^ (row >> 1 & 1) << 2; }
-// Values of a wave's own: the four rows that a transposing read for products of 16 rows takes at a time, and two such groups.
+// Values of a wave's own: the same writes, and two neighbouring chunks of each of eight rows, which the transposing read for products of
+// 16 rows takes.
 template <int D>
-__device__ __forceinline__ int value_swizzle16(int row) { return D == 128 ? (row & 3) << 2 ^ (row >> 2 & 1) << 1 : (row & 1) << 2; }
+__device__ __forceinline__ int value_swizzle16(int row) { return D == 128 ? (row & 7) << 1 | (row >> 1 & 1) : (row >> 1 & 3) << 1 | (row >> 2 & 1); }
 
 // One wave writes and reads its own LDS: the accesses are in order, the compiler is told by the fences.
 __device__ __forceinline__ void own_writes() {
@@ -392,7 +393,8 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 3 : 2) void mx4_few_kernel(
     u32x4 v[kValueLoads];
     uint32_t vs[kValueLoads];
   };
-  const int v_row = lane / kValueLanes, v_piece = lane % kValueLanes;
+  const int v_row = D == 128 ? (lane >> 4) * 4 + (lane >> 1 & 3) : (lane >> 4) * 8 + (lane >> 1 & 3) * 2 + (lane >> 3 & 1);
+  const int v_piece = D == 128 ? (lane >> 3 & 1) * 2 + (lane & 1) : lane & 1;
   const uint32_t k_code = i16 * mx4_code_bytes(D) + q4 * kKeyBytes, k_scale = i16 * mx4_scale_bytes(D) + (D == 128 ? q4 : q4 >> 1);
   const uint32_t v_code = v_row * mx4_code_bytes(D) + v_piece * 16, v_scale = v_row * mx4_scale_bytes(D) + v_piece;
   auto load = [&](int key0, const Pages& p, Chunk& c) __attribute__((always_inline)) {
