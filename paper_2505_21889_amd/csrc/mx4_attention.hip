@@ -454,7 +454,7 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 3 : 2) void mx4_few_kernel(
 
   Chunk even, odd;
   int key0 = k0 + wave * 32;
-  Pages pages = look_up(key0);
+  Pages pages = look_up(min(key0, last & -32));
   // queries
   bf16x8 qb[NB][kSteps];
   int visible[NB];  // keys that the row sees
@@ -569,16 +569,19 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? 3 : 2) void mx4_few_kernel(
       for (int n = 0; n < NB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n], o[n][d], 0, 0, 0);
     }
   };
-  if (key0 < k1) load(key0, pages, even);
-  pages = look_up(key0 + kMx4FewKeys);
+  // (No branch around the loads of a chunk ahead: where the ways meet, they would all be waited for.)
+  const int last_chunk = last & -32;
+  auto fetch = [&](int key, Chunk& c) __attribute__((always_inline)) {
+    load(min(key, last_chunk), pages, c);
+    pages = look_up(min(key + kMx4FewKeys, last_chunk));
+  };
+  fetch(key0, even);
   while (key0 < k1) {
-    if (key0 + kMx4FewKeys < k1) load(key0 + kMx4FewKeys, pages, odd);
-    pages = look_up(key0 + 2 * kMx4FewKeys);
+    fetch(key0 + kMx4FewKeys, odd);
     work(key0, even);
     key0 += kMx4FewKeys;
     if (key0 >= k1) break;
-    if (key0 + kMx4FewKeys < k1) load(key0 + kMx4FewKeys, pages, even);
-    pages = look_up(key0 + 2 * kMx4FewKeys);
+    fetch(key0 + kMx4FewKeys, even);
     work(key0, odd);
     key0 += kMx4FewKeys;
   }
