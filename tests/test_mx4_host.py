@@ -1,5 +1,8 @@
 """CPU tests of the operators of a step over a 4-bit cache: refusals before a device is touched, sizes, and pins of their oracle."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -8,6 +11,8 @@ from oracle import mx4_oracle as M
 from oracle.efim_oracle import bf16_to_f64, f64_to_bf16
 from paper_2505_21889_amd import binding as E
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2505_21889_amd", "csrc")
 FAKE = 0x7F0000001000  # never dereferenced by the host-only paths exercised here
 FREQ = (ctypes.c_double * 64)(*[1.0 / (j + 1) for j in range(64)])
 BAD, UNSUPPORTED, SPACE = E.EFIM_ERR_INVALID_ARG, E.EFIM_ERR_UNSUPPORTED, E.EFIM_ERR_WORKSPACE
@@ -181,3 +186,19 @@ def test_oracle_probabilities_by_hand():
     mask = np.array([[0b0101]], np.uint32)
     got, _ = M.probs([0], logits[:1], np.zeros(1, E.SAMPLING_DTYPE), np.zeros((1, 0), int), [], np.zeros((1, 0), int), np.zeros((1, 0)), mask, [0])
     assert got.tolist() == [[0, 0, 1, 0]]
+
+
+def test_plans_under_sanitizers(tmp_path):
+    gxx = shutil.which("g++")
+    if gxx is None or not os.path.exists("/opt/rocm/include/hip/hip_runtime.h"):
+        pytest.skip("g++ or the HIP headers are not available")
+    exe = str(tmp_path / "fuzz_mx4_plan")
+    cmd = [gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-D__HIP_PLATFORM_AMD__",
+           "-I", "/opt/rocm/include", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+           os.path.join(ROOT, "tests", "native", "fuzz_mx4_plan.cpp"), os.path.join(CSRC, "mx4_plan.cpp"), "-o", exe]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-4000:]
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1", UBSAN_OPTIONS="print_stacktrace=1")
+    env.pop("LD_PRELOAD", None)
+    run = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
+    assert run.returncode == 0 and "4-bit plan ok" in run.stdout, (run.stdout + run.stderr)[-4000:]
