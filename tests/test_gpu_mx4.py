@@ -162,6 +162,28 @@ def test_long_contexts_are_cut_and_joined(E):
     _check(E, X.Step([30000, 5], [6, 6], (8, 2), 64, seed=23))
 
 
+def test_whole_tiles_units_and_even_shares(E):
+    """The ways in which tiles of many rows are dealt: more tiles than places, a unit for each place, shares that end inside tiles."""
+    rng = np.random.default_rng(7)
+    _check(E, X.Step(rng.integers(0, 200, 9), rng.integers(33, 150, 9), (64, 64), 64, seed=61))
+    _check(E, X.Step([3000, 0, 700], [150, 40, 65], (8, 2), 128, seed=62))
+    _check(E, X.Step(rng.integers(2600, 3300, 12), rng.integers(33, 60, 12), (16, 16), 64, seed=63))
+    _check(E, X.Step(rng.integers(2600, 3300, 12), rng.integers(33, 60, 12), (16, 16), 128, 8, seed=64))
+
+
+@pytest.mark.parametrize("new,heads", [(2, (4, 2)), (40, (4, 2)), (40, (64, 32))])
+def test_blocks_that_are_no_numbers_far_back(E, new, heads):
+    """In keys and values whose parts are joined: the rows that see them lose them, and those in front do not."""
+    s = X.Step([2900, 2800], [new, new], heads, 64, seed=71)
+    for r, token, head, block in ((0, 1500, 0, 1), (0, 2900 + new - 1, 1, 0)):
+        page = s.table[r, token // s.page]
+        s.caches[1][page, head, s.page * 32 + token % s.page * 2 + block] = M.NAN_BYTE
+    got = bf16_to_f64(_attend(E, s)).reshape(2, new, heads[1], -1, 64)
+    assert np.isnan(got[0, :, 0, :, 32:]).all() and np.isnan(got[0, -1, 1, :, :32]).all()
+    got[0, :, 0, :, 32:] = got[0, -1, 1, :, :32] = 0.0
+    assert not np.isnan(got).any()
+
+
 def test_a_whole_prompt(E):
     _check(E, X.Step([0], [1100], (4, 1), 128, seed=31))
     _check(E, X.Step([0, 700], [520, 333], (3, 3), 64, seed=32))
