@@ -400,7 +400,7 @@ int efim_rope_append_mx4(const efim_batch_t* batch, const void* q, void* q_out, 
  *             an overlapping call
  * Slots at or beyond C_r + N_r may hold anything.  Blocks that are no numbers in rows that a query row does not see leave it as it
  * is; where it sees them it gets what the formula gives: of a key, no number in the whole row, of a value, none in the block's columns.
- * Errors: as efim_extend_attention; EFIM_ERR_UNSUPPORTED for more than 2^30 query rows (T * Hq).
+ * Errors: as efim_extend_attention; EFIM_ERR_UNSUPPORTED for more than 2^30 query rows (T * Hq) or 2^16 heads of keys.
  * efim_mx4_workspace_bytes is a pure host function: at least 256, 0 for an invalid batch.
  */
 size_t efim_mx4_workspace_bytes(const efim_batch_t* batch);
@@ -448,7 +448,8 @@ int efim_block_tables(int batch, const int32_t* held_len, const int32_t* cached_
  *   z = x;   seen at all:  z = z > 0 ? z / repetition : z * repetition;
  *   seen k > 0 times behind the prompt (drafted tokens count):  z = (z - frequency * k) - presence;
  *   z = z + bias (of several biases of a token the last counts);   p = softmax(z / temperature) over the allowed tokens
- * and 0 for the others.  temperature not above 0 (or NaN): 1 for the first of the largest z, 0 else; below 2^-100 as that.
+ * and 0 for the others.  temperature not above 0 (or NaN): 1 for the first of the largest z, 0 else; below 2^-100 and above 2^100
+ * as those.
  * A row of which nothing is allowed, or all of it at minus infinity, is zero throughout.  Infinities and NaN of tokens
  * that are not allowed do not matter; with a NaN or plus infinity among the allowed ones all of them get NaN (temperature 0: NaN is
  * never the largest).
@@ -487,7 +488,8 @@ typedef struct efim_logits {
  *   workspace DEVICE, 256-byte aligned, efim_logit_workspace_bytes(in) bytes, contents irrelevant
  * Only kernels are launched and no host state is kept: the call may be captured into a HIP graph, which replays num_drafts of the
  * captured call and reads everything else anew.
- * Errors: EFIM_ERR_INVALID_ARG, EFIM_ERR_UNSUPPORTED (more than 63 drafted tokens, a vocabulary above 2^22), EFIM_ERR_WORKSPACE,
+ * Errors: EFIM_ERR_INVALID_ARG, EFIM_ERR_UNSUPPORTED (more than 63 drafted tokens, a vocabulary above 2^22, a history_stride above 2^30 - 64, more
+ * than 2^31 rows), EFIM_ERR_WORKSPACE,
  * EFIM_ERR_LAUNCH.
  */
 size_t efim_logit_workspace_bytes(const efim_logits_t* in);

@@ -1,7 +1,9 @@
 // efim_block_tables: the block tables and the slot map of a step from its requests' lengths, which lie on the device.  Pages behind
 // a request's end go back onto the stack of free pages, missing ones are taken from its top.
 //
-// Bound by latency: a scan over the requests, and behind it the entries, which depend on each other only through the stack.
+// Bound by latency: a scan over the requests, and behind it the entries, which depend on each other only through the stack.  One launch
+// for up to 64 requests: 16 of them with a token each 3.0 us (6.4 with the call), 64 with whole prompts among them 4.5 (6.4); as the scan
+// and the filling apart 14.1 and 17.6 with the call.
 #include <cstdint>
 
 #include "efim_internal.h"

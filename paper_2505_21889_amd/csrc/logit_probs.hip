@@ -5,10 +5,11 @@
 // fp32, each operation rounded by itself; a temperature that is not above zero gives the first of the largest z all of it.
 //
 // Few tokens of the vocabulary have anything done to them, the same ones in all rows of a request.  A first kernel marks them in a
-// bit for each token and lists them, with how often they were made and their bias (counted in whole numbers: no order
-// changes the result).  Behind it the others are taken as they are, and an element costs two bits and the exponential.  A second kernel leaves maximum, sum and place of the maximum of every chunk of a row, a third forms the
-// probabilities from them; in both a wave has a chunk of a row to itself and waits for no other.  Bound by reading the logits, the
-// second time mostly from the caches, and by writing the probabilities.
+// bit for each token and lists them, with how often they were made and their bias (counted in whole numbers: no order changes the
+// result).  Behind it the others are taken as they are, and an element costs two bits and the exponential.  A second kernel leaves
+// maximum, sum and place of the maximum of every chunk of a row, a third forms the probabilities from them; in both a wave has a chunk
+// of a row to itself and waits for no other.  Bound by reading the logits, the second time mostly from the caches, and by writing
+// the probabilities.
 // us for 6 rows of 32004 / for 64 requests with 1 to 15 drafts and 128003: 18.0 / 177, of the latter 12 list, 65 statistics (their
 // instructions take 70 % of the issue cycles) and 98 probabilities (415 MB, 4.2 TB/s).  A workgroup for each row and slice that makes its
 // own list, two kernels: 15.7 / 271.  Listed tokens gone through behind the others instead of through LDS: 20.4 / 194.  A wave for a

@@ -40,13 +40,12 @@ Mx4FewPlan plan_mx4_few(const efim_batch_t* b, int compute_units) {
   }
   if (!plan.any) return plan;
   plan.row_tile = most <= 16 ? 16 : 32;
-  // As many workgroups as the device holds at a time, none longer than it has to be; where the tiles alone are more than those,
-  // the ones of more than the mean work of a place are cut.  us with one, two, three and six times as many as there are compute
-  // units: 32 requests of 2048..8192 keys, 28/4 heads - / 29.3 / 28.2 / 33.5, 16 of 1024..4096 and 24 rows 28.5 / 27.0 / 33.5 / -.
-  // Parts of two units at least: with one the join of one request of 2344 keys, 32/8 heads takes longer (11.5, two 11.0, three 11.4),
-  // and short requests have one.
+  // Two workgroups to a compute unit, none longer than it has to be; where the tiles alone are more than those, the ones of more than
+  // the mean work of a place are cut.  us with one, two, three and six: 32 requests of 2048..8192 keys and a token, 28/4 heads 28.5 / 24.5
+  // / 25.1 / 28.0, 16 of 1024..4096 and 24 rows 23.6 / 21.2 / 24.3 / 30.7.  Parts of two units at least: with one even a step of short
+  // requests has a join (5.7 -> 9.2); one request of 2344 keys takes the same with one, two and three.
   constexpr int kLeastUnits = 2;
-  const int64_t places = (int64_t)compute_units * (plan.row_tile == 16 ? 3 : 2);
+  const int64_t places = 2 * (int64_t)compute_units;
   int low = kLeastUnits, high = longest > low ? longest : low;
   if (tiles >= places) {
     low = high = (int)((units + places - 1) / places);
