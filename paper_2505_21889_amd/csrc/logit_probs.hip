@@ -11,7 +11,7 @@
 // of a row to itself and waits for no other.  Bound by reading the logits, the second time mostly from the caches, and by writing
 // the probabilities.
 // us for 6 rows of 32004 / for 64 requests with 1 to 15 drafts and 128003: 18.0 / 177, of the latter 12 list, 65 statistics (their
-// instructions take 70 % of the issue cycles) and 98 probabilities (415 MB, 4.2 TB/s).  A workgroup for each row and slice that makes its
+// instructions, 22 an element, take three quarters of the issue cycles) and 98 probabilities (415 MB, 4.2 TB/s).  A workgroup for each row and slice that makes its
 // own list, two kernels: 15.7 / 271.  Listed tokens gone through behind the others instead of through LDS: 20.4 / 194.  A wave for a
 // chunk of four rows that loads the list once: 18.5 / 248 (half as many waves at a time).
 #include <cstdint>
