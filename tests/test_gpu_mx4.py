@@ -184,6 +184,15 @@ def test_blocks_that_are_no_numbers_far_back(E, new, heads):
     assert not np.isnan(got).any()
 
 
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(E, seed):
+    rng = np.random.default_rng(900 + seed)
+    heads = [(4, 4), (28, 4), (8, 1), (32, 8), (64, 1), (6, 2)][rng.integers(6)]
+    batch, long = int(rng.integers(1, 12)), int(rng.choice([5, 70, 600, 3000]))
+    new = rng.integers(0, rng.choice([2, 6, 40, 120]), batch)
+    _check(E, X.Step(rng.integers(0, long, batch), new + (new.sum() == 0), heads, int(rng.choice([64, 128])), int(rng.choice([8, 16, 32, 256])), seed=seed))
+
+
 def test_a_whole_prompt(E):
     _check(E, X.Step([0], [1100], (4, 1), 128, seed=31))
     _check(E, X.Step([0, 700], [520, 333], (3, 3), 64, seed=32))
