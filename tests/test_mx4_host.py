@@ -127,6 +127,15 @@ def test_logit_probs_refuse():
     assert E.SAMPLING_DTYPE.itemsize == 32
 
 
+def test_sizes_beyond_the_calls_limits():
+    limit = (1 << 30) - 64
+    assert _logits(history_stride=limit + 1)[0] == UNSUPPORTED and _logits(history_stride=limit, size=0)[0] == SPACE
+    heads = (1 << 16) + 1
+    wide = _desc([10], [1], heads, heads)
+    assert _attend(wide) == UNSUPPORTED and E.efim_mx4_workspace_bytes(wide) == 0
+    assert _attend(_desc([10], [1], 1 << 16, 1 << 16), size=0) == SPACE
+
+
 # --- pins of the oracle --------------------------------------------------------------------------------------------------------
 
 
