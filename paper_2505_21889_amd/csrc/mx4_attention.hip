@@ -272,11 +272,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
 }
 
-// Chunk swizzles (exclusive or) of a tile's bf16 rows in LDS, of which the bank line holds one (D 128) or two.  Keys and values that a
-// workgroup shares: eight lanes write two pieces of 32 elements of each of four rows, word by word, and a wave reads sixteen neighbouring rows' equal
-// chunks (keys) and four neighbouring chunks of each of four rows (values); all of them take all banks.
+// Chunk swizzles (exclusive or) of a tile's bf16 rows in LDS, of which the bank line holds one (D 128) or two.  Keys (D 64) and values that
+// a workgroup shares: eight lanes write two pieces of 32 elements of each of four rows, word by word, and a wave reads sixteen
+// neighbouring rows' equal chunks (keys) and four neighbouring chunks of each of four rows (values); all of them take all banks.
 template <int D>
-__device__ __forceinline__ int key_swizzle(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
+__device__ __forceinline__ int key_swizzle(int row) { return row >> 1 & 7; }
 template <int D>
 __device__ __forceinline__ int value_swizzle(int row) { return D == 128 ? (row & 3) * 5 : (row >> 1 & 3) ^ (row >> 1 & 1) << 2; }
 // Values of a wave's own: the same writes, and two neighbouring chunks of each of eight rows, which the transposing read for products of
@@ -745,7 +745,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
   constexpr int kProducts = kSteps + 2 * kBlocks, kAhead = 4;
   constexpr int kExps = 16 / kProducts;            // probabilities beside a product
   constexpr int kRowBytes = 2 * D;                 // of a bf16 row in LDS
-  constexpr int kHalfBytes = 32 * kRowBytes, kStageBytes = 2 * kHalfBytes, kRingBytes = 2 * kStageBytes;
+  constexpr int kHalfBytes = 32 * kRowBytes, kStageBytes = 2 * kHalfBytes;
+  // (keys, D 128: a chunk more from row to row in place of a swizzle, so that the products' places are offsets of the reads: 22 registers and
+  // 1 % of the time less)
+  constexpr int kKeyRow = D == 128 ? kRowBytes + 16 : kRowBytes, kKeyHalf = 32 * kKeyRow, kKeyRing = 4 * kKeyHalf;
   constexpr int kPieces = D / 32;                    // of 16 bytes, of a row's codes
   constexpr int kWaveRows = 64 / kPieces;            // that a wave converts
   constexpr int kIds = SMALL ? kWaveRows / 8 : 1;    // of pages, of those
@@ -754,7 +757,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
   constexpr int kHalfWords = kChunks * kWords / 2;   // of a thread beside a half
   constexpr int kTurn = kProducts / (kHalfWords * 4);  // products for each conversion of two codes
   static_assert(kTurn * kHalfWords * 4 == kProducts && kExps * kProducts == 16, "a half's work is dealt to its products");
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kRingBytes];
+  __shared__ __attribute__((aligned(1024))) char lds[kKeyRing + 2 * kStageBytes];
   __shared__ uint32_t s_torn[kWaves];  // whether the wave met a value block that is no number
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -766,17 +769,16 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
 
   // Operands: the first chunk of the lane's key row, and where a lane of the transposing read begins in the first block.  (The
   // further ones' places differ in bits that the row's place leaves free.)
-  const uint32_t key_at = lds0 + i32 * kRowBytes + ((hi ^ key_swizzle<D>(i32)) << 4);
+  const uint32_t key_at = lds0 + i32 * kKeyRow + ((hi ^ (D == 128 ? 0 : key_swizzle<D>(i32))) << 4);
   const int v_key = (lane >> 5) * 4 + ((lane & 15) >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-  const uint32_t value_at = lds0 + kRingBytes + v_key * kRowBytes + (lane & 1) * 8 + ((v_chunk ^ value_swizzle<D>(v_key)) << 4);
+  const uint32_t value_at = lds0 + kKeyRing + v_key * kRowBytes + (lane & 1) * 8 + ((v_chunk ^ value_swizzle<D>(v_key)) << 4);
   // what this thread converts
   const int first_matrix = kChunks == 2 ? 0 : wave / (kWaves / 2);
   const int piece = D == 128 ? (lane >> 3 & 1) * 2 + (lane & 1) : lane & 1;
   const int wave_row = D == 128 ? (lane >> 4) * 4 + (lane >> 1 & 3) : (lane >> 4) * 8 + (lane >> 1 & 3) * 2 + (lane >> 3 & 1);
   const int first_row = wave * kWaveRows % 64, in_round = first_row + wave_row;
-  const int put_key = ((piece * kWords) ^ key_swizzle<D>(in_round & 31)) << 4, put_value = ((piece * kWords) ^ value_swizzle<D>(in_round & 31)) << 4;
-  const uint32_t put_at = lds0 + in_round * kRowBytes + (first_matrix == 0 ? put_key : kRingBytes + put_value);
-  const uint32_t put_apart = put_key ^ put_value;
+  const uint32_t put_keys = lds0 + in_round * kKeyRow + (((piece * kWords) ^ (D == 128 ? 0 : key_swizzle<D>(in_round & 31))) << 4);
+  const uint32_t put_values = lds0 + kKeyRing + in_round * kRowBytes + (((piece * kWords) ^ value_swizzle<D>(in_round & 31)) << 4);
 
   for (Share<kTile> it(t, lane); !it.done(); it.advance()) {
     const Cache<D> cache(k_cache, block_table, t, it.rq.req, it.at.head);
@@ -852,14 +854,14 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
     };
     // Where a round's chunks go, and their scales.  (A value block that is no number: any that are.)
     struct Target {
-      uint32_t at;
+      uint32_t at[kChunks];
       float scale[kChunks];
     };
     auto target = [&](uint32_t stage, const Chunk& c) __attribute__((always_inline)) {
       Target to;
-      to.at = put_at + stage;
 #pragma unroll
       for (int j = 0; j < kChunks; ++j) {
+        to.at[j] = first_matrix + j == 0 ? put_keys + stage * (2 * kKeyHalf) : put_values + stage * kStageBytes;
         const bool bad = first_matrix + j == 1 && c.scales[j] >= kTorn;
         torn |= bad && wave_row < it.k1 - c.key[j];
         to.scale[j] = mx4_scale_value(bad ? 127u : c.scales[j]);
@@ -868,14 +870,14 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
     };
     constexpr auto kFirst = std::integral_constant<int, 0>{};
     constexpr auto kSecond = std::integral_constant<int, 1>{};
-    uint32_t here = 0, ahead = kStageBytes;  // the stages of the round and the next one
+    uint32_t here = 0, ahead = 1;  // the stages of the round and the next one
     uint32_t made[4];
     // the n-th conversion of a round
     auto convert = [&](auto n_c, const Chunk& c, const Target& to) __attribute__((always_inline)) {
       constexpr int n = decltype(n_c)::value, word = n / 4, j = word / kWords, w = word % kWords;
       made[n % 4] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c.codes[j][w], to.scale[j], n % 4));
       if constexpr (n % 4 == 3)
-        *(LDS_PTR(u32x4))(uintptr_t)(((to.at + j * kRingBytes) ^ (j == 0 ? 0u : put_apart)) ^ (uint32_t)(w << 4)) = u32x4{made[0], made[1], made[2], made[3]};
+        *(LDS_PTR(u32x4))(uintptr_t)(D == 128 && j == 0 ? to.at[j] + w * 16 : to.at[j] ^ (uint32_t)(w << 4)) = u32x4{made[0], made[1], made[2], made[3]};
     };
     auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
@@ -889,7 +891,8 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
       sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qb[n], from, 0, 0, 0);
     };
     auto key_operand = [&](uint32_t stage, int second, int n) __attribute__((always_inline)) -> u32x4 {
-      return *(const LDS_PTR(u32x4))(uintptr_t)(((key_at + stage) ^ (uint32_t)(n << 5)) + second * kHalfBytes);
+      const uint32_t row = key_at + stage * (2 * kKeyHalf);
+      return *(const LDS_PTR(u32x4))(uintptr_t)((D == 128 ? row + n * 32 : row ^ (uint32_t)(n << 5)) + second * kKeyHalf);
     };
     u32x4 staged[kAhead];  // operands of the next products
     // Products of a half, the first or second of its round: the scores of the stage's keys into `sn`, the stage's values under the
@@ -900,7 +903,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_many_kernel(const Mx4Args arg
         if (n < kSteps) return key_operand(stage, decltype(second)::value, n);
         if (n >= kProducts) return key_operand(stage, 1, n - kProducts);  // (of the second half)
         const int k = (n - kSteps) / kBlocks, d = (n - kSteps) % kBlocks;
-        const uint32_t at = ((value_at + stage) ^ (uint32_t)(d << 6)) + decltype(second)::value * kHalfBytes;
+        const uint32_t at = ((value_at + stage * kStageBytes) ^ (uint32_t)(d << 6)) + decltype(second)::value * kHalfBytes;
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + 2 * k * 8 * kRowBytes));
         const bf16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS_PTR(bf16x4))(uintptr_t)(at + (2 * k + 1) * 8 * kRowBytes));
         return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
