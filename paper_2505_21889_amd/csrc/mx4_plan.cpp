@@ -159,7 +159,10 @@ bool mx4_next(const efim_batch_t* b, const Mx4ManyPlan& plan, Mx4Cursor* at, Mx4
   // Where the device has a place for each of the units of eight (or sixteen, ..) times as many keys, and they are not much longer than
   // an even share with its second part: those.  (The one request above 27 us, in shares that are not cut at tiles' ends 33.)
   constexpr int kLeast = 8;
-  for (int shift = kMx4ManyShift + 3; !t->by_tile && (1 << (shift - kMx4ManyShift)) <= (even < kLeast ? kLeast : even) + kTileCost; ++shift) {
+  // (Up to 2^30 keys, which is all that a request may have: with tiles by the ten thousand an even share is longer than that.)
+  constexpr int kLongest = 30;
+  const int64_t longest_unit = (even < kLeast ? kLeast : even) + kTileCost;
+  for (int shift = kMx4ManyShift + 3; !t->by_tile && shift <= kLongest && (int64_t)1 << (shift - kMx4ManyShift) <= longest_unit; ++shift) {
     int64_t starts[kMx4TableReqs], heads[kMx4TableReqs], all = 0;
     for (int k = 0; k < t->nreq; ++k) {
       starts[k] = all;
