@@ -1,9 +1,11 @@
-"""The launches that batches over a 4-bit cache are cut into, on the host."""
+"""The launches that batches over a 4-bit cache are cut into, on the host: those of the device's tests, and the largest ones allowed."""
 import os
 import shutil
 import subprocess
 
 import pytest
+
+import mx4_batches as B
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2505_21889_amd", "csrc")
@@ -31,6 +33,22 @@ def launches(tmp_path_factory):
         return [(line.split()[0], *map(int, line.split()[1:])) for line in done.stdout.splitlines()[:-1]]
 
     return run
+
+
+@pytest.mark.parametrize("name", B.FEW)
+def test_every_launch_of_few_rows_has_parts(launches, name):
+    cached, new, heads, _ = B.few(name)
+    got = launches(cached, new, heads)
+    assert [x[0] for x in got] == ["few"] * 3 and [x[2] for x in got] == [120, 120, 10]
+    assert all(x[1] == int(name.split()[0]) and x[4] > 0 for x in got)
+
+
+def test_every_launch_of_many_rows_has_parts(launches):
+    got = launches(*B.many())
+    many, few = [x for x in got if x[0] == "many"], [x for x in got if x[0] == "few"]
+    assert [x[1] for x in many] == [96, 44] and len(few) == 1 and few[0][4] > 0
+    # shares of a whole number of units; in the first launch of 64 keys, which end inside tiles, in the second larger ones
+    assert [x[2] for x in many] == [0, 0] and many[0][3] == 6 and many[1][3] > 6 and all(x[5] == 1 for x in many)
 
 
 # (keys of a request are at most 2^30, query rows in all as many)
