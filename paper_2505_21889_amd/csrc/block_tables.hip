@@ -2,8 +2,9 @@
 // a request's end go back onto the stack of free pages, missing ones are taken from its top.
 //
 // Bound by latency: a scan over the requests, and behind it the entries, which depend on each other only through the stack.  One launch
-// for up to 64 requests: 16 of them with a token each 3.0 us (6.4 with the call), 64 with whole prompts among them 4.5 (6.4); as the scan
-// and the filling apart 14.1 and 17.6 with the call.
+// for up to 64 requests: 16 of them with a token each 3.5 us (6.3 with the call), 64 with whole prompts among them 4.8 (6.4); as the scan
+// and the filling apart 14.1 and 17.6 with the call.  More requests, the scan and the filling: 65 to 256 with a token each 14.5
+// with the call.  (The scan's workgroup filling too takes 15.5 for 65, 16.6 for 96 and 17.7 for 128.)
 #include <cstdint>
 
 #include "efim_internal.h"
@@ -68,8 +69,6 @@ __device__ __forceinline__ void fill_request(const TablesArgs& a, int r, int64_t
   }
 }
 
-// FILL: the entries too, by the same workgroup (steps of few tokens).
-template <bool FILL>
 __global__ __launch_bounds__(kScanThreads) void tables_scan_kernel(const TablesArgs a) {
   __shared__ Sums s_wave[kScanThreads / 64];
   __shared__ int32_t s_bad;
@@ -147,16 +146,6 @@ __global__ __launch_bounds__(kScanThreads) void tables_scan_kernel(const TablesA
       int32_t* to = a.free_pages + count + a.plan[1 + a.batch + r];
       for (int64_t j = lane; j < q.returned(); j += 64) to[j] = row[j];
     }
-  if constexpr (FILL) {
-    __threadfence_block();
-    __syncthreads();
-    const int64_t stacked = ok ? count + all.returned : -1;
-    if (ok)
-      for (int r = wave; r < a.batch; r += kScanThreads / 64)
-        fill_request(a, r, stacked, a.plan[1 + r], a.row_start[r], lane, 64);
-    if (a.slots)
-      for (int64_t t = (stacked >= 0 ? all.tokens : 0) + tid; t < a.slot_capacity; t += kScanThreads) a.slots[t] = -1;
-  }
 }
 
 // Workgroup x of the first `batch` has a request; the others the slots behind the last token.
@@ -312,10 +301,8 @@ int efim_block_tables(int batch, const int32_t* held_len, const int32_t* cached_
     const int64_t slices = (a.slot_capacity / batch * 2 + kFillThreads - 1) / kFillThreads;
     tables_small_kernel<<<dim3((unsigned)batch + 1, (unsigned)(slices < 1 ? 1 : slices > 16 ? 16 : slices)), kFillThreads, 0, s>>>(a);
     if (same) tables_count_kernel<<<1, 1, 0, s>>>(static_cast<const int32_t*>(workspace), free_count_out);
-  } else if (a.slot_capacity <= 2048 && batch <= 128) {
-    tables_scan_kernel<true><<<1, kScanThreads, 0, s>>>(a);
   } else {
-    tables_scan_kernel<false><<<1, kScanThreads, 0, s>>>(a);
+    tables_scan_kernel<<<1, kScanThreads, 0, s>>>(a);
     tables_fill_kernel<<<dim3((unsigned)batch + 1, 4), kFillThreads, 0, s>>>(a);
   }
   const hipError_t e = hipGetLastError();

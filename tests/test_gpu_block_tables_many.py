@@ -1,5 +1,4 @@
-"""efim_block_tables with more requests than a wave has lanes: the scan that fills by itself (up to 128 requests and 2048 slots), the one
-with a launch behind it, and what either refuses."""
+"""efim_block_tables with more requests than a wave has lanes: a scan and a launch that fills behind it, and what they refuse."""
 import numpy as np
 import pytest
 import torch
@@ -10,7 +9,7 @@ from test_gpu_block_tables import E, _check, _dev, _state  # noqa: F401 (E is a 
 
 pytestmark = pytest.mark.gpu
 
-#: places of the slot map: the scan fills by itself up to 2048, where there are at most 128 requests
+#: places of the slot map: few, more than there are tokens by far, and between them
 ROOMS = (600, 2048, 2049, 5000)
 
 
