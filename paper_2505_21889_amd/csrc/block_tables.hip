@@ -3,8 +3,9 @@
 //
 // Bound by latency: a scan over the requests, and behind it the entries, which depend on each other only through the stack.  One launch
 // for up to 64 requests: 16 of them with a token each 3.5 us (6.3 with the call), 64 with whole prompts among them 4.8 (6.4); as the scan
-// and the filling apart 14.1 and 17.6 with the call.  More requests, the scan and the filling: 65 to 256 with a token each 14.5
-// with the call.  (The scan's workgroup filling too takes 15.5 for 65, 16.6 for 96 and 17.7 for 128.)
+// and the filling apart 14.1 and 17.6 with the call.  More requests, the scan and the filling: 65 to 256 with a token each 11.1 with the
+// call, 1024 12.3, 96 with 24 prompts among them 14.6.  (The scan's workgroup filling too takes 10.2 for 65, 11.1 for 96 and 12.3 for 128: not
+// worth a kernel.)
 #include <cstdint>
 
 #include "efim_internal.h"
@@ -116,6 +117,7 @@ __global__ __launch_bounds__(kScanThreads) void tables_scan_kernel(const TablesA
       if (lane == 63) s_wave[wave] = upto;
       __syncthreads();
       Sums before = front;
+#pragma unroll 4  // (all sixteen waves' sums at once do not fit the registers of so many threads)
       for (int w = 0; w < kScanThreads / 64; ++w) {
         if (w < wave) {
           before.taken += s_wave[w].taken;
