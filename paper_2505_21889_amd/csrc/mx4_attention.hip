@@ -338,7 +338,7 @@ struct FewLanes {
 // as their conversions and products (37 % and 15 % of the cycles), and the four waves' join 1.5.  One request of 2344 keys: latency,
 // 5.7 and 3.3.  Three units in flight instead of two: 4 % slower in the first case, 5 % in the second.
 template <int D, int NB, int MAXREQ>
-__global__ __launch_bounds__(kThreads, NB == 1 ? 3 : 2) void mx4_few_kernel(
+__global__ __launch_bounds__(kThreads, 2) void mx4_few_kernel(
     const Mx4FewArgs<MAXREQ> args, const uint16_t* __restrict__ q, const uint8_t* __restrict__ k_cache,
     const uint8_t* __restrict__ v_cache, const int32_t* __restrict__ block_table) {
   constexpr int kSteps = D / 32;           // products over the head dimension
