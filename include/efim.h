@@ -408,9 +408,10 @@ int efim_extend_attention_mx4(const efim_batch_t* batch, const void* q, const vo
                               void* out, float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
- * efim_block_tables -- the block tables and the slot map of a step, built on the device from lengths that lie there: what a step
- * of efim_batch_t needs in front of it, where an engine's lengths (and how many drafted tokens were refused) are known to
- * the device alone.
+ * efim_block_tables -- the block tables and the slot map of a step, built on the device from lengths that lie there (how many drafted
+ * tokens were refused is known to the device first).  The other calls read block_table as this one leaves it; their lengths they
+ * take from the host (efim_batch_t), so a step that goes on with them brings the lengths there, and a captured one replays those
+ * that it was captured with.  slot_map and row_start are for kernels of the caller's own: no call here reads them.
  * For request r with pages for held_len[r] tokens, cached_len[r] tokens that stay and new_len[r] to come, with
  * held = ceil(held_len / P) and wanted = ceil((cached_len + new_len) / P):
  *   columns wanted .. held - 1 of its block table row go back onto the stack of free pages, those of request 0 first, each in
