@@ -8,11 +8,11 @@
 // bit for each token and lists them, with how often they were made and their bias (counted in whole numbers: no order changes the
 // result).  Behind it the others are taken as they are, and an element costs two bits and the exponential.  A second kernel leaves
 // maximum, sum and place of the maximum of every chunk of a row, a third forms the probabilities from them; in both a wave has a chunk
-// of a row to itself and waits for no other.  Bound by reading the logits, the second time mostly from the caches, and by writing
-// the probabilities.
-// us for 6 rows of 32004 / for 64 requests with 1 to 15 drafts and 128003: 18.0 / 177, of the latter 12 list, 65 statistics (their
-// instructions, 22 an element, take three quarters of the issue cycles) and 98 probabilities (415 MB, 4.2 TB/s).  A workgroup for each row and slice that makes its
-// own list, two kernels: 15.7 / 271.  Listed tokens gone through behind the others instead of through LDS: 20.4 / 194.  A wave for a
+// of a row to itself and waits for no other.  Bound by the instructions of the statistics, by reading the logits a second time and by
+// writing the probabilities.
+// us for 6 rows of 32004 / for 64 requests with 1 to 15 drafts and 128003: 18.0 / 178, of the latter 13 list, 70 statistics (their
+// instructions, 22 an element, take three quarters of the issue cycles; 196 MB come from memory, 2.8 TB/s) and 104 probabilities (212 MB from
+// memory and 329 MB to it, 5.2 TB/s: a copy's rate).  A workgroup for each row and slice that makes its own list, two kernels: 15.7 / 271.  Listed tokens gone through behind the others instead of through LDS: 20.4 / 194.  A wave for a
 // chunk of four rows that loads the list once: 18.5 / 248 (half as many waves at a time).
 #include <cstdint>
 #include <type_traits>

@@ -2,7 +2,7 @@
 // over the tokens' rows.  The rotation is the bf16 append's (fp64, rounded once), so the queries are the same bits; what that
 // append would have stored is rounded block by block to 4 bits.
 // Streaming kernel, bound by HBM bandwidth: (4 Hq + 2 Hkv (2 + 17/32 + 2 where the stored rows are asked for)) D bytes a token.
-// 64 requests, half of them whole prompts of 1024..4096 tokens, 32/8 heads: 2054 MB in 363 us, 5.7 TB/s (a copy: 5.1); 16 single tokens: 4.1 us.
+// 64 requests, half of them whole prompts of 1024..4096 tokens, 32/8 heads: 2054 MB in 363 us, 5.7 TB/s (a copy: 5.1); 16 single tokens: 4.5 us.
 #include <type_traits>
 
 #include "append_table.h"

@@ -333,10 +333,10 @@ struct FewLanes {
 // own, and their sums are combined at the part's end.  A wave's keys go from memory to registers, where they are the product's
 // operands as they are converted; a lane has 16 (D 128; 8) bytes of a row's codes, all under one scale, and the query operands
 // follow that order of elements.
-// Bound by HBM where there are many: 32 requests of 2048..8192 keys, one token each, 28/4 heads 20.2 us for 96 MB (4.8 TB/s) and 3.5 for
-// the join.  16 requests of 1024..4096 keys and 24 rows 16.5 for 48 MB: the first two units of all waves take 2 us to come, five more as long
+// Bound by HBM where there are many: 32 requests of 2048..8192 keys, one token each, 28/4 heads 20.4 us for 96 MB (4.7 TB/s) and 4.7 for
+// the join.  16 requests of 1024..4096 keys and 24 rows 17.8 for 48 MB: the first two units of all waves take 2 us to come, five more as long
 // as their conversions and products (37 % and 15 % of the cycles), and the four waves' join 1.5.  One request of 2344 keys: latency,
-// 5.7 and 3.3.  Three units in flight instead of two: 4 % slower in the first case, 5 % in the second.
+// 6.1 and 4.1.  Three units in flight instead of two: 4 % slower in the first case, 5 % in the second.
 template <int D, int NB, int MAXREQ>
 __global__ __launch_bounds__(kThreads, 2) void mx4_few_kernel(
     const Mx4FewArgs<MAXREQ> args, const uint16_t* __restrict__ q, const uint8_t* __restrict__ k_cache,
@@ -733,7 +733,7 @@ __global__ __launch_bounds__(kThreads) void mx4_few_join_kernel(const Mx4FewArgs
 // halves reads.  The waves meet once a round.  A unit holds two workgroups, so that each computes through the other's meetings,
 // first loads and last stores.
 //
-// Bound by the products at the rate that power leaves: 8 prompts of 1024..4096 tokens, 32/8 heads 570 us (943 TFLOP/s that count), products 45 %
+// Bound by the products at the rate that power leaves: 8 prompts of 1024..4096 tokens, 32/8 heads 577 us (931 TFLOP/s that count), products 46 %
 // of the cycles at 2.1 GHz.  With nothing beside the products a half of two waves takes 1490 cycles where 1024 are nominal, with
 // everything 1750.  One workgroup of eight waves and 256 rows, which converts half as often, 602 (without any conversion 557, without
 // exponentials 587): a tile's start and end, 20k of 105k cycles, go by with nothing beside them.  All phases of a tile one
